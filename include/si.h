@@ -318,6 +318,98 @@ size_t si_resample_workspace_bytes(const si_tensor5* x, int32_t kind, int64_t sl
 si_status si_resample_forward(const si_tensor5* x, int32_t kind, const void* w_conv, const void* b_conv, si_tensor5* out,
                               int64_t slice_len, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Heads of a sequence of tokens in device memory: element (b, n, h, c) lies at
+ * ptr + b*stride_b + n*stride_n + h*stride_h + c (strides in elements, channels
+ * contiguous), so that queries, keys and values may be parts of one projection's
+ * rows, of a cache, or head-major.  Strides are not negative, and of dimensions
+ * longer than one a multiple of 16 bytes; the stride of a dimension of length one
+ * is ignored.  dim_head is a multiple of 8, at most 128.  N == 0 is legal (ptr may
+ * then be NULL).  What a call writes must have one address per element. */
+typedef struct {
+  void* ptr; /* device */
+  int32_t dtype;
+  int64_t B, N, heads, dim_head;
+  int64_t stride_b, stride_n, stride_h;
+} si_heads;
+
+/* Rotary positions on three axes: frame, row, column.  The grid has extent[0] x
+ * extent[1] x extent[2] tokens in raster order.  Axis a turns pairs[a] pairs of
+ * channels; pair i of it by the angle
+ *   (origin[a] + step[a] * coordinate) * theta^(-i / pairs[a]).
+ * The pairs of the three axes follow each other; pair number p is
+ *   SI_ROPE_INTERLEAVED  channels 2p and 2p + 1
+ *   SI_ROPE_HALVES       channels p and P + p, P = pairs[0] + pairs[1] + pairs[2]
+ * and (x1, x2) becomes (x1 cos - x2 sin, x1 sin + x2 cos).  Channels from 2P on
+ * are copied.  P is a multiple of 4, at least 4, and 2P <= dim_head; an axis may
+ * have no pairs.  norm_eps >= 0: every head is first divided by
+ * sqrt(mean of its squares + norm_eps) and multiplied by q_gain / k_gain (device,
+ * [dim_head] in the operands' type, NULL = one); norm_eps < 0: it is not.
+ * Angles are formed in float64, everything else in float32 with one rounding.
+ * |origin| and |step| * extent are at most 1e12. */
+typedef enum { SI_ROPE_INTERLEAVED = 0, SI_ROPE_HALVES = 1 } si_rope_layout;
+typedef struct {
+  int64_t extent[3];
+  int32_t pairs[3];
+  int32_t layout; /* si_rope_layout */
+  double theta, origin[3], step[3];
+  float norm_eps;
+  const void *q_gain, *k_gain;
+} si_rope;
+
+/* Rotates q and k (NULL with k_out NULL: q alone) into q_out and k_out.  Token n
+ * of every batch entry is grid point first + n; first + N must lie inside the
+ * grid.  k may have another number of heads than q; B, N, dim_head and dtype are
+ * common.  An output may be its own input (in place); otherwise no element of an
+ * output may lie on one of an input or of the other output. */
+si_status si_rope_forward(const si_heads* q, const si_heads* k, const si_rope* rope, int64_t first, si_heads* q_out,
+                          si_heads* k_out, void* stream);
+
+/* Attention over key blocks that a cheap score selects.
+ *
+ * Queries are taken in runs of q_block consecutive tokens (the last may be
+ * shorter), keys in blocks of k_block (a multiple of 64).  Query head h belongs to
+ * key / value head h / (q->heads / k->heads).  For every batch entry b, key / value
+ * head and run there is one list of key blocks, a bitmap of
+ * si_attn_block_words(k->N, k_block) 32-bit words: block j is bit j % 32 of word
+ * j / 32.  The bitmaps are one device array [B][k->heads][runs][words].
+ *
+ * q_len, k_len (device int32 [B], may be NULL = N): tokens of every batch entry
+ * that count, clamped to [0, N].  What lies behind them is never read as a value,
+ * so it may hold anything. */
+
+/* Words of one list; 0 if the arguments are invalid or there are no keys.  Host-only. */
+int64_t si_attn_block_words(int64_t n_keys, int64_t k_block);
+
+/* Workspace bytes of si_attn_select / si_attn_sparse_forward for these operands;
+ * 0 if the arguments are invalid.  Host-only. */
+size_t si_attn_select_workspace_bytes(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block);
+size_t si_attn_sparse_workspace_bytes(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block);
+
+/* The `keep` (>= 1) key blocks of highest score for every run.  The score of run i
+ * and block j is the inner product of the mean query of the run (over its counted
+ * tokens and the query heads of the key head) with the mean key of the block (over
+ * its counted tokens), in float64; equal scores: the lowest block first; a NaN
+ * ranks as -infinity.  Blocks without a counted token are not listed, nor is
+ * anything for a run without one; with fewer than `keep` blocks all are listed.
+ * Every word of `blocks` is written.  At most 16384 blocks (SI_ERR_SHAPE). */
+si_status si_attn_select(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block, int64_t keep,
+                         const int32_t* q_len, const int32_t* k_len, uint32_t* blocks, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* out[b, n, h] = sum_j softmax_j(scale * <q[b, n, h], k[b, j, hk]>) v[b, j, hk], j over the counted tokens of
+ * the blocks in the list of n's run (blocks NULL: of every block), hk = h / (q->heads / k->heads).
+ * A listed block without a counted token adds nothing; a row whose list leaves no
+ * key gives zeros; rows at and behind q_len are left as they were.
+ * scale > 0.  q, k, v and out have one dtype; v is shaped like k, out like q.  No
+ * element of out may lie on one of q, k or v.  bf16 operands: scores, maxima, sums
+ * and outputs in float32, probabilities rounded to bf16 for the second product;
+ * float32 operands: float32 throughout.  The same operands give the same bits.
+ * workspace: device, 256-byte aligned, contents ignored; calls that overlap in time
+ * must not share one. */
+si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_heads* v, int64_t q_block, int64_t k_block,
+                                 float scale, const int32_t* q_len, const int32_t* k_len, const uint32_t* blocks,
+                                 si_heads* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Key-step search, Algorithm 1 (Appendix B).  Host only.
  *   S      host, row-major K x K similarity map; only S[i][anchor] entries are read
  *   gamma  threshold, must satisfy gamma <= 1 and gamma <= S[i][i] where visited

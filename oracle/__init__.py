@@ -1,5 +1,5 @@
 """CPU oracle for the sliced transformer-block forward, the Step Rehash test and walks, and the
-Spatial ResBlock operator group with its Up/DownSample.
+Spatial ResBlock operator group with its Up/DownSample, and the operators on heads of video tokens.
 
 TEST INFRASTRUCTURE ONLY.  Plain NumPy in float64, full tensors, one operator
 after the other, no blocking or fusion.  Nothing here is imported by the HIP
@@ -24,4 +24,7 @@ from .rehash_ref import (  # noqa: F401
 from .resblock_ref import (  # noqa: F401
     silu_ref, conv3x3_ref, resblock_forward_ref, sliced_resblock_forward_ref,
     downsample_ref, upsample_ref, sliced_resample_ref,
+)
+from .attn_ref import (  # noqa: F401
+    rope_angles_ref, rms_norm_ref, rope_ref, block_scores_ref, pack_blocks_ref, select_ref, sparse_attention_ref,
 )

@@ -56,6 +56,18 @@ class _ResWeights(C.Structure):
                 + [("c_out", C.c_int32), ("w_skip", C.c_void_p), ("b_skip", C.c_void_p)])
 
 
+class _Heads(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32),
+                ("B", C.c_int64), ("N", C.c_int64), ("heads", C.c_int64), ("dim_head", C.c_int64),
+                ("stride_b", C.c_int64), ("stride_n", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("extent", C.c_int64 * 3), ("pairs", C.c_int32 * 3), ("layout", C.c_int32), ("theta", C.c_double),
+                ("origin", C.c_double * 3), ("step", C.c_double * 3), ("norm_eps", C.c_float),
+                ("q_gain", C.c_void_p), ("k_gain", C.c_void_p)]
+
+
 class _RehashCache(C.Structure):
     _fields_ = [("x_key", C.c_void_p), ("y_key", C.c_void_p), ("valid", C.c_int32)]
 
@@ -97,6 +109,19 @@ def lib() -> C.CDLL:
     L.si_resample_workspace_bytes.argtypes = [C.POINTER(_Tensor5), i32, i64]
     L.si_resample_forward.restype = i32
     L.si_resample_forward.argtypes = [C.POINTER(_Tensor5), i32, vp, vp, C.POINTER(_Tensor5), i64, vp, sz, vp]
+    ph = C.POINTER(_Heads)
+    L.si_rope_forward.restype = i32
+    L.si_rope_forward.argtypes = [ph, ph, C.POINTER(_Rope), i64, ph, ph, vp]
+    L.si_attn_block_words.restype = i64
+    L.si_attn_block_words.argtypes = [i64, i64]
+    L.si_attn_select_workspace_bytes.restype = sz
+    L.si_attn_select_workspace_bytes.argtypes = [ph, ph, i64, i64]
+    L.si_attn_select.restype = i32
+    L.si_attn_select.argtypes = [ph, ph, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    L.si_attn_sparse_workspace_bytes.restype = sz
+    L.si_attn_sparse_workspace_bytes.argtypes = [ph, ph, i64, i64]
+    L.si_attn_sparse_forward.restype = i32
+    L.si_attn_sparse_forward.argtypes = [ph, ph, ph, i64, i64, C.c_float, vp, vp, vp, ph, vp, sz, vp]
     L.si_rehash_scratch_bytes.restype = sz
     L.si_rehash_scratch_bytes.argtypes = [i64]
     L.si_rehash_check.restype = i32
@@ -285,6 +310,133 @@ def si_resample_forward(x, kind: int, w_conv, b_conv, out, slice_len: int, works
                                    workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     if st != 0:
         raise SiError(st, "si_resample_forward")
+
+
+SI_ROPE_INTERLEAVED, SI_ROPE_HALVES = 0, 1
+
+
+class Rope:
+    """Rotary positions on the axes (frame, row, column) of a grid: si_rope.  Keeps the gains alive.
+
+    norm_eps: None, or the heads are RMS-normalised (times q_gain / k_gain) before they turn."""
+
+    def __init__(self, extent: Sequence[int], pairs: Sequence[int], *, theta: float = 1e4, layout: int = SI_ROPE_INTERLEAVED,
+                 origin: Sequence[float] = (0.0, 0.0, 0.0), step: Sequence[float] = (1.0, 1.0, 1.0), norm_eps: Optional[float] = None,
+                 q_gain=None, k_gain=None):
+        self.gains = (q_gain, k_gain)
+        s = _Rope()
+        s.extent[:], s.pairs[:], s.origin[:], s.step[:] = list(extent), list(pairs), list(origin), list(step)
+        s.layout, s.theta, s.norm_eps = layout, theta, -1.0 if norm_eps is None else norm_eps
+        if norm_eps is not None and norm_eps < 0:
+            raise ValueError("norm_eps must not be negative")
+        for g in self.gains:
+            if g is not None and (norm_eps is None or g.dim() != 1 or not g.is_contiguous()):
+                raise ValueError("gains are contiguous [dim_head] tensors and need norm_eps")
+        s.q_gain, s.k_gain = (None if g is None else g.data_ptr() for g in self.gains)
+        self.struct = s
+
+
+def _heads(t) -> _Heads:
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError("heads must be a [B, N, heads, dim_head] tensor with contiguous channels")
+    B, N, h, d = t.shape
+    sb, sn, sh, _ = t.stride()
+    return _Heads(t.data_ptr(), _dtype_code(t), B, N, h, d, sb, sn, sh)
+
+
+class _on_device:
+    """The operands' device as the current one, and the stream to enqueue on, for one call."""
+
+    def __init__(self, stream, first, *others):
+        import torch
+        if first.device.type != "cuda" or any(t is not None and t.device != first.device for t in others):
+            raise ValueError("all tensors must be on one GPU")
+        self.device = first.device
+        self.guard = None if first.device.index == torch.cuda.current_device() else torch.cuda.device(first.device)
+        self.stream = _stream_ptr(torch.cuda.current_stream(first.device) if stream is None else stream)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _lengths(t, B: int) -> Optional[int]:
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != B or not t.is_contiguous():
+        raise ValueError("lengths must be a contiguous int32 tensor [B]")
+    return t.data_ptr()
+
+
+def _bitmap(t, q, k, q_block: int, k_block: int) -> Optional[int]:
+    if t is None:
+        return None
+    import torch
+    if q_block < 1 or k_block < 1:
+        raise SiError(2, "key blocks")
+    shape = (q.shape[0], k.shape[2], -(-q.shape[1] // q_block), -(-(-(-k.shape[1] // k_block)) // 32))
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"blocks must be a contiguous int32 tensor {list(shape)}")
+    return t.data_ptr()
+
+
+def si_rope_forward(q, k, rope: Rope, q_out, k_out, first: int = 0, stream=None) -> None:
+    """Rotates the heads of q [B,N,heads,dim_head] and k (or None) into q_out and k_out; token n is grid point first + n."""
+    for g in rope.gains:
+        if g is not None and (g.shape[0] != q.shape[3] or g.dtype != q.dtype):
+            raise ValueError("gains must be [dim_head] in the operands' dtype")
+    qd, qo = _heads(q), _heads(q_out)
+    kd, ko = (None if t is None else C.byref(_heads(t)) for t in (k, k_out))
+    with _on_device(stream, q, k, q_out, k_out, *rope.gains) as st:
+        status = lib().si_rope_forward(C.byref(qd), kd, C.byref(rope.struct), first, C.byref(qo), ko, st)
+    if status != 0:
+        raise SiError(status, "si_rope_forward")
+
+
+def si_attn_block_words(n_keys: int, k_block: int) -> int:
+    return int(lib().si_attn_block_words(n_keys, k_block))
+
+
+def si_attn_select_workspace_bytes(q, k, q_block: int, k_block: int) -> int:
+    qd, kd = _heads(q), _heads(k)
+    return int(lib().si_attn_select_workspace_bytes(C.byref(qd), C.byref(kd), q_block, k_block))
+
+
+def si_attn_select(q, k, q_block: int, k_block: int, keep: int, blocks, workspace, q_len=None, k_len=None, stream=None) -> None:
+    """Writes the `keep` best key blocks of every run of q_block queries as bitmaps: blocks int32
+    [B, k heads, runs, si_attn_block_words(N of k, k_block)]."""
+    qd, kd = _heads(q), _heads(k)
+    ql, kl, bits = _lengths(q_len, q.shape[0]), _lengths(k_len, q.shape[0]), _bitmap(blocks, q, k, q_block, k_block)
+    with _on_device(stream, q, k, blocks, workspace, q_len, k_len) as st:
+        status = lib().si_attn_select(C.byref(qd), C.byref(kd), q_block, k_block, keep, ql, kl, bits, workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), st)
+    if status != 0:
+        raise SiError(status, "si_attn_select")
+
+
+def si_attn_sparse_workspace_bytes(q, k, q_block: int, k_block: int) -> int:
+    qd, kd = _heads(q), _heads(k)
+    return int(lib().si_attn_sparse_workspace_bytes(C.byref(qd), C.byref(kd), q_block, k_block))
+
+
+def si_attn_sparse_forward(q, k, v, q_block: int, k_block: int, blocks, out, workspace, scale: Optional[float] = None, q_len=None,
+                           k_len=None, stream=None) -> None:
+    """Attention of runs of q_block queries over the key blocks in their bitmaps (blocks None: over every key).
+    scale: 1/sqrt(dim_head) unless given."""
+    qd, kd, vd, od = _heads(q), _heads(k), _heads(v), _heads(out)
+    ql, kl, bits = _lengths(q_len, q.shape[0]), _lengths(k_len, q.shape[0]), _bitmap(blocks, q, k, q_block, k_block)
+    with _on_device(stream, q, k, v, blocks, out, workspace, q_len, k_len) as st:
+        status = lib().si_attn_sparse_forward(C.byref(qd), C.byref(kd), C.byref(vd), q_block, k_block,
+                                              q.shape[3] ** -0.5 if scale is None else scale, ql, kl, bits, C.byref(od),
+                                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), st)
+    if status != 0:
+        raise SiError(status, "si_attn_sparse_forward")
 
 
 class RehashCache:

@@ -56,11 +56,6 @@ __host__ __device__ constexpr int kappa16(int f) { return f < 4 || f >= 12 ? f :
 // sum (16 of a tile's 32 keys); the two halves meet once, after the last tile.
 constexpr float kLazyTrigger = 256.f;  // 2^8: an exponential this large, or 16 of them each above 2^4
 
-__device__ __forceinline__ float dot2_ones(unsigned packed_bf16x2, float acc) {
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, packed_bf16x2), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), acc,
-                                         false);
-}
-
 struct AttnState {
   f32x16_t oacc[2];  // O^T, two 32-channel blocks
   f32x16_t minit;    // -m in every register

@@ -1,0 +1,208 @@
+// Key blocks for runs of queries by a cheap score: the product of the run's mean query and the block's mean key.
+//
+//   block_means_kernel   means over the rows of a run / block (and the heads that share a key / value head), float64
+//   block_select_kernel  scores of 16 runs against every block on the float64 matrix cores, kept in LDS; then, per run,
+//                        the `keep` largest, ties to the lowest block, as a bitmap
+//
+// Everything behind the loads is float64: which block is the last one kept can hang on any digit of its score, and the
+// result is discrete.  The means are bound by HBM (every query and key is read once), the scores take 2 d flop per (run,
+// block) at some 60 TFLOP/s, far less time than the attention over the blocks they choose.
+#pragma once
+#include "k_rope.h"
+
+namespace si {
+
+typedef double f64x2_t __attribute__((ext_vector_type(2)));
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kMeanPieces = 32, kMeanSlices = 8;  // 16-byte pieces of a row x rows in flight of one workgroup
+constexpr int kSelectThreads = 512;
+constexpr int kSelectMaxBlocks = 16384;           // one run's scores fill the LDS of a workgroup
+
+struct MeansArgs {
+  HeadsView x;
+  const int* len;
+  double* out;  // [B][heads_kv][runs][d]
+  int N, heads_kv, group, d, block, runs;
+  int chunks;      // of kMeanPieces pieces of a row
+  int64_t work;    // B * runs * chunks
+};
+
+template <typename T>
+__global__ __launch_bounds__(kMeanPieces* kMeanSlices) void block_means_kernel(MeansArgs a) {
+  constexpr int VEC = 16 / sizeof(T);
+  __shared__ double part[kMeanSlices][kMeanPieces][VEC];
+  const int px = threadIdx.x % kMeanPieces, slice = threadIdx.x / kMeanPieces;
+  const int per_head = a.d / VEC;
+  for (int64_t work = blockIdx.x; work < a.work; work += gridDim.x) {
+    const int chunk = (int)(work % a.chunks), run = (int)(work / a.chunks % a.runs), b = (int)(work / a.chunks / a.runs);
+    const int item = chunk * kMeanPieces + px;
+    const bool live = item < a.heads_kv * per_head;
+    const int hk = live ? item / per_head : 0, ch = live ? (item - hk * per_head) * VEC : 0;
+    const int len = a.len ? min(max(a.len[b], 0), a.N) : a.N;
+    const int64_t n0 = (int64_t)run * a.block;
+    const int rows = (int)min((int64_t)a.block, max((int64_t)0, len - n0));
+    double sum[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum[i] = 0.0;
+    if (live) {
+      const T* p = static_cast<const T*>(a.x.p) + b * a.x.sb + n0 * a.x.sn + (int64_t)hk * a.group * a.x.sh + ch;
+      for (int s = 0; s < a.group; ++s, p += a.x.sh)
+#pragma unroll 4
+        for (int n = slice; n < rows; n += kMeanSlices) {
+          const T* q = p + n * a.x.sn;
+          if constexpr (sizeof(T) == 2) {
+            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              sum[2 * i] += (double)__uint_as_float(v[i] << 16);
+              sum[2 * i + 1] += (double)__uint_as_float(v[i] & 0xffff0000u);
+            }
+          } else {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += (double)v[i];
+          }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) part[slice][px][i] = sum[i];
+    __syncthreads();
+    const double of = rows > 0 ? (double)((int64_t)rows * a.group) : 1.0;
+    for (int e = threadIdx.x; e < kMeanPieces * VEC; e += kMeanPieces * kMeanSlices) {
+      const int it = chunk * kMeanPieces + e / VEC;
+      if (it >= a.heads_kv * per_head) continue;
+      double s = 0.0;
+#pragma unroll
+      for (int k = 0; k < kMeanSlices; ++k) s += part[k][e / VEC][e % VEC];
+      const int h = it / per_head, c = (it - h * per_head) * VEC + e % VEC;
+      a.out[(((int64_t)b * a.heads_kv + h) * a.runs + run) * a.d + c] = s / of;
+    }
+    __syncthreads();
+  }
+}
+
+struct SelectArgs {
+  const double *qm, *km;  // [B][heads_kv][runs][d], [B][heads_kv][blocks][d]
+  unsigned* out;          // [B][heads_kv][runs][words]
+  const int *q_len, *k_len;
+  int Nq, Nk, heads_kv, d, q_block, k_block, runs, blocks, words;
+  int keep, rows;         // blocks to keep; runs of a workgroup
+  int pitch;              // scores of one run in LDS
+  int tiles;              // of `rows` runs; a workgroup takes one tile of one (b, kv head)
+  int64_t work;           // B * heads_kv * tiles
+};
+
+// Order of float64 as unsigned integers: NaN as -infinity, -0 as +0; 0 is below every value.
+__device__ __forceinline__ unsigned long long order_key(double x) {
+  if (!(x == x)) x = -INFINITY;
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, x + 0.0);
+  return b >> 63 ? ~b : b | 0x8000000000000000ull;
+}
+
+// The largest T of 32-bit words with at least `need` values >= T among those that `in` accepts, found from the top bit on:
+// stops early when exactly `need` values are >= the prefix.  Returns T, and in `above` the number of values > T ... >= T.
+template <class Count>
+__device__ __forceinline__ unsigned kth_word(int need, Count count, bool& exact) {
+  unsigned t = 0;
+  exact = false;
+  for (int bit = 31; bit >= 0; --bit) {
+    const unsigned c = t | (1u << bit);
+    const int n = count(c);
+    if (n >= need) {
+      t = c;
+      if (n == need) {
+        exact = true;
+        break;
+      }
+    }
+  }
+  return t;
+}
+
+template <int CAP>  // scores (float64) of a workgroup
+__global__ __launch_bounds__(kSelectThreads) void block_select_kernel(SelectArgs a) {
+  __shared__ unsigned long long keys[CAP];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, nw = kSelectThreads / kWave;
+  for (int64_t work = blockIdx.x; work < a.work; work += gridDim.x) {
+  const int64_t pair = work / a.tiles;  // (b, kv head)
+  const int b = (int)(pair / a.heads_kv), run0 = (int)(work - pair * a.tiles) * a.rows;
+  const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.Nk) : a.Nk;
+  const int nblk = (k_len + a.k_block - 1) / a.k_block;  // blocks with a key
+
+  // ---- scores: 16 blocks (rows) x 16 runs (columns) per step; lane (m, g) supplies row / column m's channels 8 s + 2 g + {0, 1}
+  const int m = lane % 16, g = lane / 16;
+  const int qrow = min(run0 + min(m, a.rows - 1), a.runs - 1);
+  const double* qp = a.qm + (pair * a.runs + qrow) * a.d + 2 * g;
+  for (int j0 = wave * 16; j0 < nblk; j0 += nw * 16) {
+    const double* kp = a.km + (pair * a.blocks + min(j0 + m, a.blocks - 1)) * a.d + 2 * g;
+    f64x4_t acc{0.0, 0.0, 0.0, 0.0};
+    for (int c = 0; c < a.d; c += 8) {
+      const f64x2_t kv = *reinterpret_cast<const f64x2_t*>(kp + c), qv = *reinterpret_cast<const f64x2_t*>(qp + c);
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[0], qv[0], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[1], qv[1], acc, 0, 0, 0);
+    }
+    if (m < a.rows) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // result register i: row 4 i + g
+        const int j = j0 + 4 * i + g;
+        if (j < a.pitch) keys[m * a.pitch + j] = j < nblk ? order_key(acc[i]) : 0ull;
+      }
+    }
+  }
+  __syncthreads();
+
+  // ---- the `keep` largest of each run
+  for (int row = wave; row < a.rows; row += nw) {
+    const int run = run0 + row;
+    if (run >= a.runs) break;
+    unsigned* out = a.out + (pair * a.runs + run) * a.words;
+    const unsigned long long* key = keys + row * a.pitch;
+    const bool none = (int64_t)run * a.q_block >= q_len;
+    if (none || nblk <= a.keep) {  // nothing, or all
+      for (int w = lane; w < a.words; w += kWave) {
+        const int n = none ? 0 : nblk - 32 * w;
+        out[w] = n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u;
+      }
+      continue;
+    }
+    auto tally = [&](auto pred) {
+      int n = 0;
+      for (int j = lane; j < nblk; j += kWave) n += pred(key[j]) ? 1 : 0;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
+      return __builtin_amdgcn_readfirstlane(n);
+    };
+    bool exact;
+    const unsigned hi = kth_word(a.keep, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); }, exact);
+    unsigned long long least = (unsigned long long)hi << 32;  // everything >= least is kept, except some of the equal ones
+    int need_equal = 0;  // of the values == least, when not exact
+    if (!exact) {
+      const int above = tally([&](unsigned long long k) { return (unsigned)(k >> 32) > hi; });
+      const int need = a.keep - above;
+      const unsigned lo = kth_word(
+          need, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) == hi && (unsigned)k >= c; }); }, exact);
+      least |= lo;
+      if (!exact) need_equal = a.keep - tally([&](unsigned long long k) { return k > least; });
+    }
+    int equal = 0;
+    for (int j0 = 0; j0 < 32 * a.words; j0 += kWave) {
+      const int j = j0 + lane;
+      const unsigned long long k = j < nblk ? key[j] : 0ull;
+      bool take = j < nblk && (exact ? k >= least : k > least);
+      if (!exact) {
+        const bool eq = j < nblk && k == least;
+        const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
+        const int rank = equal + __popcll(eqs & ((1ull << lane) - 1ull));
+        take = take || (eq && rank < need_equal);
+        equal += __popcll(eqs);
+      }
+      const unsigned long long bits = __builtin_amdgcn_ballot_w64(take);
+      if (lane < 2 && j0 / 32 + lane < a.words) out[j0 / 32 + lane] = (unsigned)(bits >> (32 * lane));
+    }
+  }
+  __syncthreads();
+  }
+}
+
+}  // namespace si

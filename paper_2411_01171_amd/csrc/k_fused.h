@@ -43,14 +43,6 @@ __device__ __forceinline__ void static_for(F&& f) {
 // Logical k offset inside a 16-wide k-step of hardware slot (g, e).
 __host__ __device__ __forceinline__ int frag_k(int g, int e) { return e < 4 ? 4 * g + e : 8 + 4 * g + (e - 4); }
 
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-
-// two floats -> packed bf16 pair, round-to-nearest-even (one v_cvt_pk_bf16_f32)
-__device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi) {
-  const f32x2_t v = {lo, hi};
-  return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2_t));
-}
 
 // 8 consecutive result registers (two quads) -> column operand of one k-step.
 __device__ __forceinline__ bf16x8_t to_operand(const float* v) {

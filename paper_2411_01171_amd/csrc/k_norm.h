@@ -9,19 +9,6 @@
 
 namespace si {
 
-// Fragment order of a 16-bit activation operand of the ring kernels (k_conv.h): granule
-// act_granule(t, c8) holds the 16 bytes (channels 8*c8 .. +7) of token t; a 1 KiB fragment is the
-// 64 granules of (32-token block, 16-channel step), 16-channel steps fastest; the buffer starts with
-// a 256-byte block of zeros.
-constexpr int kActZeroBytes = 256;
-__host__ __device__ __forceinline__ int64_t act_granule(int64_t t, int c8, int C) {
-  return ((t >> 5) * (C / 16) + (c8 >> 1)) * 64 + (c8 & 1) * 32 + (t & 31);
-}
-// element offset (16-bit elements) of channel c of token t in such a buffer
-__host__ __device__ __forceinline__ int64_t act_offset(int64_t t, int c, int C) {
-  return kActZeroBytes / 2 + act_granule(t, c >> 3, C) * 8 + (c & 7);
-}
-
 // One block per (b, f, g).  Reduces the n_g * P values x[b, g*n_g:(g+1)*n_g, f, :].
 // Sums are taken relative to the group's first element so that a large common
 // offset does not cancel in fp32; per-thread fp32 partials are merged in fp64.

@@ -1,0 +1,182 @@
+// Rotary positions on three axes (frame, row, column) for heads of video tokens, with the heads' root-mean-square norm in
+// the same pass.
+//
+// Token n lies at coordinates (f, y, x) of an F x H x W grid, raster order.  Pair i of an axis turns by
+//   angle = (origin + step * coordinate) * theta^(-i / pairs of that axis),
+// (x1, x2) -> (x1 cos - x2 sin, x1 sin + x2 cos).  The angle is formed in float64 and in revolutions (the host divides the
+// frequencies by 2 pi), so that its whole part drops out exactly before the sine and cosine are taken in float32: positions
+// of 10^6 lose nothing.  Everything else is float32 with one rounding at the store.
+//
+// Bound by HBM: every head is read and written once.  A thread owns eight channels (four pairs) of one token and walks the
+// heads of q and k: the sines of a token are computed once for all of them, and the loads of kRopeHeads heads are in
+// flight together.
+#pragma once
+#include "si_common.h"
+
+namespace si {
+
+constexpr int kRopeThreads = 256, kRopeHeads = 4, kRopeMaxPairs = 64;
+
+struct HeadsView {  // element (b, n, h, c) at p + b*sb + n*sn + h*sh + c
+  void* p;
+  int64_t sb, sn, sh;
+};
+
+struct RopeArgs {
+  HeadsView q, k, qo, ko;
+  const void *q_gain, *k_gain;
+  int64_t tokens;            // B * N
+  int N, H, W, first;        // token n of a batch entry is grid point first + n
+  int heads_q, heads, d;     // heads of q; of q and k
+  int heads_per_wg;          // a workgroup's share of the heads (blockIdx.y)
+  int pairs, end_f, end_y;   // all pairs; pairs [0, end_f) turn with the frame, [end_f, end_y) with the row
+  int tokens_per_wg;         // kRopeThreads / (d / 8)
+  float eps;
+  double origin[3], step[3];
+  double freq[kRopeMaxPairs];  // revolutions per position
+};
+
+template <typename T> struct Raw8;  // eight channels as they lie in memory
+template <> struct Raw8<bf16> { u32x4_t v; };
+template <> struct Raw8<float> { f32x4_t v[2]; };
+
+// channels [c0, c0 + 4) and [c1, c1 + 4) of a head; ONE: c1 == c0 + 4
+template <bool ONE> __device__ __forceinline__ void load8(const bf16* p, int c0, int c1, Raw8<bf16>& r) {
+  if constexpr (ONE) r.v = *reinterpret_cast<const u32x4_t*>(p + c0);
+  else {
+    const uint2 a = *reinterpret_cast<const uint2*>(p + c0), b = *reinterpret_cast<const uint2*>(p + c1);
+    r.v = u32x4_t{a.x, a.y, b.x, b.y};
+  }
+}
+template <bool ONE> __device__ __forceinline__ void load8(const float* p, int c0, int c1, Raw8<float>& r) {
+  r.v[0] = *reinterpret_cast<const f32x4_t*>(p + c0);
+  r.v[1] = *reinterpret_cast<const f32x4_t*>(p + c1);
+}
+__device__ __forceinline__ void unpack8(const Raw8<bf16>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(r.v[i] << 16);
+    x[2 * i + 1] = __uint_as_float(r.v[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = r.v[i / 4][i % 4];
+}
+template <bool ONE> __device__ __forceinline__ void store8(bf16* p, int c0, int c1, const float (&y)[8]) {
+  unsigned w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (unsigned)float_to_bf16_bits(y[2 * i]) | ((unsigned)float_to_bf16_bits(y[2 * i + 1]) << 16);
+  if constexpr (ONE) *reinterpret_cast<u32x4_t*>(p + c0) = u32x4_t{w[0], w[1], w[2], w[3]};
+  else {
+    *reinterpret_cast<uint2*>(p + c0) = make_uint2(w[0], w[1]);
+    *reinterpret_cast<uint2*>(p + c1) = make_uint2(w[2], w[3]);
+  }
+}
+template <bool ONE> __device__ __forceinline__ void store8(float* p, int c0, int c1, const float (&y)[8]) {
+  *reinterpret_cast<f32x4_t*>(p + c0) = f32x4_t{y[0], y[1], y[2], y[3]};
+  *reinterpret_cast<f32x4_t*>(p + c1) = f32x4_t{y[4], y[5], y[6], y[7]};
+}
+
+// HALVES: pair p is channels (p, pairs + p), else (2p, 2p + 1).  The channels behind the pairs pass through.
+template <typename T, bool HALVES, bool NORM>
+__global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
+  __shared__ f32x4_t sums[2][NORM ? kRopeThreads : 1];
+  static_assert(kRopeHeads == 4, "one float4 of partial sums per thread");
+  const int nchunk = a.d / 8, slot = threadIdx.x / nchunk, c = threadIdx.x % nchunk;
+  const int64_t token = (int64_t)blockIdx.x * a.tokens_per_wg + slot;
+  const bool live = slot < a.tokens_per_wg && token < a.tokens;
+  const int64_t tk = live ? token : 0;
+  const int64_t b = tk / a.N;
+  const int n = (int)(tk - b * a.N);
+  const bool turned = 4 * c < a.pairs;
+  // this thread's channels: two runs of four
+  const int c0 = HALVES && turned ? 4 * c : 8 * c, c1 = HALVES && turned ? a.pairs + 4 * c : 8 * c + 4;
+  float cs[4], sn[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+  if (turned) {
+    const int at = a.first + n, row = at / a.W, f = row / a.H, y = row - f * a.H, x = at - row * a.W;
+    const double pf = fma(a.step[0], (double)f, a.origin[0]), py = fma(a.step[1], (double)y, a.origin[1]),
+                 px = fma(a.step[2], (double)x, a.origin[2]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = 4 * c + i;
+      const double rev = (p < a.end_f ? pf : p < a.end_y ? py : px) * a.freq[p];
+      sincospif(2.f * (float)(rev - rint(rev)), &sn[i], &cs[i]);
+    }
+  }
+  float gq[8], gk[8];
+  if constexpr (NORM) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int ch = i < 4 ? c0 + i : c1 + i - 4;
+      gq[i] = param_or(static_cast<const T*>(a.q_gain), ch, 1.f);
+      gk[i] = param_or(static_cast<const T*>(a.k_gain), ch, 1.f);
+    }
+  }
+  const int h_end = min(a.heads, (int)(blockIdx.y + 1) * a.heads_per_wg);
+  int flip = 0;
+  for (int h0 = blockIdx.y * a.heads_per_wg; h0 < h_end; h0 += kRopeHeads, flip ^= 1) {
+    Raw8<T> raw[kRopeHeads] = {};
+#pragma unroll
+    for (int u = 0; u < kRopeHeads; ++u) {
+      const int h = h0 + u < h_end ? h0 + u : h_end - 1;
+      const HeadsView& s = h < a.heads_q ? a.q : a.k;
+      const T* p = static_cast<const T*>(s.p) + b * s.sb + n * s.sn + (h < a.heads_q ? h : h - a.heads_q) * s.sh;
+      if (live) {
+        if (HALVES && turned) load8<false>(p, c0, c1, raw[u]);
+        else load8<true>(p, c0, c1, raw[u]);
+      }
+    }
+    float inv[kRopeHeads];
+    if constexpr (NORM) {
+      f32x4_t part;
+#pragma unroll
+      for (int u = 0; u < kRopeHeads; ++u) {
+        float x[8];
+        unpack8(raw[u], x);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+        part[u] = s;
+      }
+      sums[flip][threadIdx.x] = part;
+      __syncthreads();
+      f32x4_t all{0.f, 0.f, 0.f, 0.f};
+      if (live)
+        for (int i = 0; i < nchunk; ++i) all += sums[flip][slot * nchunk + i];
+#pragma unroll
+      for (int u = 0; u < kRopeHeads; ++u) inv[u] = 1.f / sqrtf(all[u] / (float)a.d + a.eps);
+    }
+    if (!live) continue;
+#pragma unroll
+    for (int u = 0; u < kRopeHeads; ++u) {
+      const int h = h0 + u;
+      if (h >= h_end) break;
+      const bool is_q = h < a.heads_q;
+      float x[8], y[8];
+      unpack8(raw[u], x);
+      if constexpr (NORM) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= inv[u] * (is_q ? gq[i] : gk[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int i1 = HALVES ? i : 2 * i, i2 = HALVES ? i + 4 : 2 * i + 1;
+        y[i1] = x[i1] * cs[i] - x[i2] * sn[i];
+        y[i2] = x[i1] * sn[i] + x[i2] * cs[i];
+      }
+      if (!turned) {  // passes through, also where a value is infinite
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[i];
+      }
+      const HeadsView& s = is_q ? a.qo : a.ko;
+      T* p = static_cast<T*>(s.p) + b * s.sb + n * s.sn + (is_q ? h : h - a.heads_q) * s.sh;
+      if (HALVES && turned) store8<false>(p, c0, c1, y);
+      else store8<true>(p, c0, c1, y);
+    }
+  }
+}
+
+}  // namespace si

@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -25,54 +26,29 @@
 #include "k_gemm.h"
 #include "k_gemm_wide.h"
 #include "k_norm.h"
+#include "si_attn_ops.h"
 #include "si_common.h"
+#include "si_host.h"
 
 namespace si {
 
 // ----------------------------------------------------------------------------- stage timing
 
-struct StageEvent {
-  int stage;
-  hipEvent_t a, b;
-};
-static bool g_timing = false;
+bool g_timing = false;
 static std::vector<std::string> g_stage_names;
-static std::vector<StageEvent> g_events;
+std::vector<StageEvent> g_events;
 
-static int stage_id(const char* name) {
+int stage_id(const char* name) {
   for (size_t i = 0; i < g_stage_names.size(); ++i)
     if (g_stage_names[i] == name) return (int)i;
   g_stage_names.emplace_back(name);
   return (int)g_stage_names.size() - 1;
 }
 
-struct StageScope {
-  hipStream_t st;
-  StageEvent ev;
-  bool on;
-  StageScope(const char* name, hipStream_t s) : st(s), on(g_timing) {
-    if (!on) return;
-    ev.stage = stage_id(name);
-    if (hipEventCreate(&ev.a) != hipSuccess || hipEventCreate(&ev.b) != hipSuccess) {
-      on = false;
-      return;
-    }
-    (void)hipEventRecord(ev.a, st);
-  }
-  ~StageScope() {
-    if (!on) return;
-    (void)hipEventRecord(ev.b, st);
-    g_events.push_back(ev);
-  }
-};
-
 // ----------------------------------------------------------------------------- plan
 
 constexpr int kMaxLanes = 3;  // windows in flight at most (measured: a fourth window in flight gains nothing at 25 slices
                               // and 7 % at 16, where it would take the live bytes past a quarter of the unsliced run's)
-
-static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Column tiles of the ring kernel used as a GEMM on windows of up to Mmax tokens (`lanes` of them in
 // flight) x N columns over K: the widest tile (5, 4, 2 or 1 blocks of 32 columns) that pads N by at
@@ -338,11 +314,6 @@ static si_status make_plan(const si_tensor5* x, const si_block_weights* w, const
 
 // ----------------------------------------------------------------------------- launches
 
-#define SI_CHECK_LAUNCH()                         \
-  do {                                            \
-    if (hipGetLastError() != hipSuccess) return SI_ERR_HIP; \
-  } while (0)
-
 template <typename T, class Epi, int BK, bool F16>
 static void launch_gemm_bf16(const T* A, int64_t lda, const T* Wp, int64_t M, int N, int K, Epi epi, hipStream_t st) {
   // small problems (a slice of a few thousand tokens times a D-wide matrix) get 64 x 64 tiles:
@@ -606,12 +577,6 @@ static si_status launch_layer_norm(const char* stage, const float* h, T* a, int6
   SI_CHECK_LAUNCH();
   return SI_OK;
 }
-
-#define SI_TRY(expr)                  \
-  do {                                \
-    si_status st__ = (expr);          \
-    if (st__ != SI_OK) return st__;   \
-  } while (0)
 
 // Fragment stream of the register-resident kernels (bf16 only) and the frame table, one launch.
 template <int NB>
@@ -1152,11 +1117,6 @@ static bool pack_matches(const void* ws, uint64_t fp) {
   for (const PackRecord& r : g_pack_table)
     if (r.ws == ws) return r.fp == fp;
   return false;
-}
-
-static bool ranges_overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  return a0 < b0 + nb && b0 < a0 + na;
 }
 
 }  // namespace si

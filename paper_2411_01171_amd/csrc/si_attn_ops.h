@@ -1,0 +1,35 @@
+// Operators on heads of video tokens, as the spatial block's path calls them (defined in si_attn_ops.hip).
+#pragma once
+#include "../../include/si.h"
+
+#include <hip/hip_runtime.h>
+
+namespace si {
+
+struct BlocksPlan {
+  int64_t runs, blocks, words;
+  int group;
+};
+
+struct SparsePlan {
+  int nw, ks, ob, nsplit;
+  int64_t tiles_per_run, tiles, work;
+  size_t part_bytes;
+};
+
+si_status check_rope(const si_rope* r, int d);
+si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block, BlocksPlan* p);
+si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, SparsePlan* p);
+size_t select_bytes(const si_heads* q, const si_heads* k, const BlocksPlan& p);
+
+// The operands of these have been checked.  k and ko may be NULL.
+si_status enqueue_rope(const si_heads* q, const si_heads* k, const si_rope* r, int64_t first, const si_heads* qo, const si_heads* ko,
+                       hipStream_t st);
+si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan& p, int64_t q_block, int64_t k_block, int64_t keep,
+                         const int32_t* q_len, const int32_t* k_len, uint32_t* blocks, char* ws, hipStream_t st);
+// o_frag: 0, or out is a fragment-order operand buffer of that many channels per token (bf16)
+si_status enqueue_sparse(const si_heads* q, const si_heads* k, const si_heads* v, const BlocksPlan& b, const SparsePlan& p, int64_t q_block,
+                         int64_t k_block, float scale, const int32_t* q_len, const int32_t* k_len, const uint32_t* blocks,
+                         const si_heads* out, char* ws, hipStream_t st, int o_frag);
+
+}  // namespace si

@@ -59,6 +59,34 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// two floats -> packed bf16 pair, round-to-nearest-even (one v_cvt_pk_bf16_f32)
+__device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi) {
+  const f32x2_t v = {lo, hi};
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2_t));
+}
+
+// sum of a bf16 pair's values onto acc
+__device__ __forceinline__ float dot2_ones(unsigned packed_bf16x2, float acc) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, packed_bf16x2), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), acc,
+                                         false);
+}
+
+// Fragment order of a 16-bit activation operand of the ring kernels (k_conv.h): granule
+// act_granule(t, c8) holds the 16 bytes (channels 8*c8 .. +7) of token t; a 1 KiB fragment is the
+// 64 granules of (32-token block, 16-channel step), 16-channel steps fastest; the buffer starts with
+// a 256-byte block of zeros.
+constexpr int kActZeroBytes = 256;
+__host__ __device__ __forceinline__ int64_t act_granule(int64_t t, int c8, int C) {
+  return ((t >> 5) * (C / 16) + (c8 >> 1)) * 64 + (c8 & 1) * 32 + (t & 31);
+}
+// element offset (16-bit elements) of channel c of token t in such a buffer
+__host__ __device__ __forceinline__ int64_t act_offset(int64_t t, int c, int C) {
+  return kActZeroBytes / 2 + act_granule(t, c >> 3, C) * 8 + (c & 7);
+}
+
 __device__ __forceinline__ float gelu_erf(float u) {
   return 0.5f * u * (1.0f + erff(u * 0.70710678118654752440f));
 }

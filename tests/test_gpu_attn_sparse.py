@@ -1,0 +1,269 @@
+"""si_attn_sparse_forward against the float64 oracle, element by element, within a bound derived from its roundings."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2411_01171_amd as si
+import si_workloads as wl
+from attn_helpers import LAYOUTS, attention_bound, draw, host, lengths, strided
+from gpu_helpers import guarded, guards_intact
+
+pytestmark = pytest.mark.gpu
+
+
+def _forward(dq, dk, dv, q_block, k_block, words, out, scale=None, q_len=None, k_len=None, stream=None):
+    n = si.si_attn_sparse_workspace_bytes(dq, dk, q_block, k_block)
+    assert n > 0
+    buf, ws = guarded(n)
+    si.si_attn_sparse_forward(dq, dk, dv, q_block, k_block, words, out, ws, scale=scale, q_len=lengths(q_len), k_len=lengths(k_len), stream=stream)
+    torch.cuda.synchronize()
+    assert guards_intact(buf, n)
+
+
+def _check(dtype, B, N, Nk, Hq, Hk, d, q_block, k_block, density=0.4, q_len=None, k_len=None, layout="rows", out_layout="rows", scale=None,
+           std=1.0, seed=0, kept=None, dense=False):
+    rng = np.random.default_rng(seed)
+    q, k, v = draw(rng, (B, N, Hq, d), dtype, std), draw(rng, (B, Nk, Hk, d), dtype, std), draw(rng, (B, Nk, Hk, d), dtype)
+    runs, blocks = -(-N // q_block), -(-Nk // k_block)
+    if kept is None and not dense:
+        kept = rng.random((B, Hk, runs, blocks)) < density
+    words = None
+    if not dense:
+        words = oracle.pack_blocks_ref(kept).view(np.uint32)
+        if blocks % 32:  # bits behind the last block mean nothing
+            words[..., -1] |= np.uint32(0xFFFFFFFF) << np.uint32(blocks % 32)
+        words = torch.from_numpy(words.view(np.int32)).to("cuda")
+    dq, dk, dv = (strided(t, dtype, layout) for t in (q, k, v))
+    for b in range(B):  # what does not count may hold anything
+        if q_len is not None:
+            dq[b, min(max(q_len[b], 0), N):] = float("nan")
+        if k_len is not None:
+            dk[b, min(max(k_len[b], 0), Nk):] = float("nan")
+            dv[b, min(max(k_len[b], 0), Nk):] = float("inf")
+    out = strided(np.full(q.shape, 7.0, np.float32), dtype, out_layout)
+    _forward(dq, dk, dv, q_block, k_block, words, out, scale, q_len, k_len)
+    sc = 1 / math.sqrt(d) if scale is None else scale
+    ref, spread, mass = oracle.sparse_attention_ref(q, k, v, kept, q_block, k_block, sc, q_len, k_len)
+    got = host(out)
+    left = np.isnan(ref)
+    assert (got[left] == 7.0).all()  # rows behind the lengths stay
+    tol = attention_bound(q, k, spread, mass, ref, dtype, sc, Nk)
+    err = np.abs(got - ref)
+    assert (err[~left] <= tol[~left]).all(), float(np.max(err[~left] / tol[~left]))
+
+
+HEADS = (8, 16, 24, 32, 40, 48, 56, 64, 72, 80, 88, 96, 104, 112, 120, 128)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", HEADS)
+def test_head_widths(dtype, d):
+    _check(dtype, 1, 130, 333, 2, 2, d, 128, 64)
+    _check(dtype, 1, 9, 333, 2, 2, d, 4, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_block", [1, 2, 7, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 300, 5000])
+def test_run_lengths(dtype, q_block):
+    _check(dtype, 2, 301, 200, 1, 1, 40 if q_block % 2 else 64, q_block, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("keys", [1, 2, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 200, 1000])
+@pytest.mark.parametrize("k_block", [64, 128, 192])
+def test_key_counts(dtype, keys, k_block):
+    _check(dtype, 1, 70, keys, 1, 1, 64, 64, k_block, density=0.7)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", [(2, 1), (8, 2), (7, 1), (32, 1), (48, 1)])
+@pytest.mark.parametrize("q_block", [1, 3, 64])
+def test_heads_shared_by_queries(dtype, heads, q_block):
+    _check(dtype, 2, 65, 300, heads[0], heads[1], 64, q_block, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("out_layout", LAYOUTS)
+def test_strides(dtype, layout, out_layout):
+    _check(dtype, 2, 150, 150, 3, 3, 64, 50, 64, layout=layout, out_layout=out_layout)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_block", [1, 64, 128])
+@pytest.mark.parametrize("q_len,k_len", [([0, 150, 200], [640, 0, 1]), ([1, 64, 65], [64, 65, 63]), ([-3, 999, 128], [7000, -1, 610])])
+def test_padded_batches(dtype, q_block, q_len, k_len):
+    _check(dtype, 3, 200, 650, 2, 1, 64, q_block, 128, density=0.6, q_len=q_len, k_len=k_len)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_block", [1, 128])
+def test_rows_without_keys_give_zeros(dtype, q_block):
+    kept = np.zeros((1, 1, -(-200 // q_block), 5), bool)
+    kept[0, 0, 1, 3] = True
+    _check(dtype, 1, 200, 300, 1, 1, 64, q_block, 64, kept=kept)
+    _check(dtype, 1, 200, 300, 1, 1, 64, q_block, 64, kept=np.zeros_like(kept))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,Nk", [(1, 4000), (300, 1000), (130, 64)])
+def test_without_lists_every_key_counts(dtype, N, Nk):
+    _check(dtype, 2, N, Nk, 2, 1, 64, 128, 64, dense=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("blocks", [3, 40, 2049, 4200])
+@pytest.mark.parametrize("density", [0.02, 1.0])
+def test_single_tokens_against_long_caches(dtype, blocks, density):
+    """The list is dealt out to several workgroups and joined; lists of more than 2048 blocks take several chunks of words."""
+    _check(dtype, 2, 1, 64 * blocks - 5, 4, 2, 32, 1, 64, density=density)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_lists_of_one_workgroup(dtype):
+    """More than 2048 blocks with few of them listed, and enough rows that nothing is dealt out."""
+    rng = np.random.default_rng(1)
+    kept = np.zeros((1, 1, 300, 2200), bool)
+    for i in range(300):
+        kept[0, 0, i, rng.integers(0, 2200, 1 + i % 3)] = True
+    kept[0, 0, 5] = False
+    kept[0, 0, 6, 2199] = True
+    _check(dtype, 1, 900, 64 * 2200, 1, 1, 16, 3, 64, kept=kept)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-3, 1.0])
+@pytest.mark.parametrize("q_block", [1, 128])
+def test_flat_and_peaked_weights(dtype, scale, q_block):
+    """Scores up to some tens: the reference maximum rises many times on the way through the list."""
+    _check(dtype, 1, 140, 1500, 1, 1, 64, q_block, 64, scale=scale, density=0.9)
+
+
+def test_rising_scores():
+    """Every block's scores are far above those of the blocks before it, and the other way round."""
+    d, Nk = 64, 64 * 12
+    for sign in (1, -1):
+        q = np.ones((1, 40, 1, d), np.float32)
+        k = np.zeros((1, Nk, 1, d), np.float32)
+        k[0, :, 0, 0] = sign * 30.0 * (np.arange(Nk) // 64)
+        v = draw(np.random.default_rng(2), (1, Nk, 1, d), "bf16")
+        out = torch.zeros(1, 40, 1, d, device="cuda", dtype=torch.bfloat16)
+        _forward(strided(q, "bf16", "rows"), strided(k, "bf16", "rows"), strided(v, "bf16", "rows"), 40, 64, None, out, scale=1.0)
+        ref, spread, mass = oracle.sparse_attention_ref(q, k, v, None, 40, 64, 1.0)
+        # scores are exact here (one product of small whole numbers)
+        tol = 2.0 ** -8 * 1.01 * (spread + np.abs(ref)) + 2.0 ** -12 * mass
+        assert (np.abs(host(out) - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_of_minus_infinity_weigh_nothing(dtype):
+    """Keys whose score is -inf stand in the first block, a whole block of them even; the others share the weight."""
+    q = np.zeros((1, 3, 1, 64), np.float32)
+    q[..., 0] = 1.0
+    k = np.zeros((1, 192, 1, 64), np.float32)
+    k[0, :64, 0, 0] = -np.inf
+    k[0, 64:100, 0, 0] = -np.inf
+    v = np.ones((1, 192, 1, 64), np.float32)
+    v[0, 100:146] = 3.0
+    out = torch.zeros(1, 3, 1, 64, device="cuda", dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    _forward(strided(q, dtype, "rows"), strided(k, dtype, "rows"), strided(v, dtype, "rows"), 4, 64, None, out)
+    assert np.array_equal(host(out), np.full((1, 3, 1, 64), 2.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_not_finite_where_no_list_looks(dtype):
+    rng = np.random.default_rng(4)
+    q, k, v = (torch.from_numpy(draw(rng, (1, 256, 1, 64), dtype)).to("cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32) for _ in range(3))
+    words = torch.tensor([[[[0b0101]]]], dtype=torch.int32, device="cuda")
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    _forward(q, k, v, 256, 64, words, a)
+    for t in (k, v):
+        t[:, 64:128], t[:, 192:] = float("nan"), float("inf")
+    _forward(q, k, v, 256, 64, words, b)
+    assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+def test_same_bits_every_time_on_any_stream_and_in_a_graph():
+    q, k, v = (torch.randn(2, n, h, 64, device="cuda", dtype=torch.bfloat16) for n, h in ((1, 8), (9000, 2), (9000, 2)))
+    ws = torch.empty(si.si_attn_sparse_workspace_bytes(q, k, 1, 64), dtype=torch.uint8, device="cuda")
+    words = torch.randint(-2 ** 31, 2 ** 31 - 1, (2, 2, 1, si.si_attn_block_words(9000, 64)), dtype=torch.int32, device="cuda")
+    ref, out = torch.empty_like(q), torch.empty_like(q)
+    si.si_attn_sparse_forward(q, k, v, 1, 64, words, ref, ws)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    for s in (None, stream):
+        out.zero_()
+        torch.cuda.synchronize()
+        si.si_attn_sparse_forward(q, k, v, 1, 64, words, out, ws, stream=s)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        si.si_attn_sparse_forward(q, k, v, 1, 64, words, out, ws)
+    for i in range(3):
+        q.normal_()
+        si.si_attn_sparse_forward(q, k, v, 1, 64, words, ref, ws)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref), i
+
+
+def test_offsets_beyond_32_bits():
+    """A cache whose last rows lie more than 2^31 elements (4 GiB) behind its first."""
+    N, H, d = 70000, 480, 64
+    cache = torch.zeros(1, N, H, d, device="cuda", dtype=torch.bfloat16)
+    k, v = cache[:, :, 0:1], cache[:, :, 479:480]
+    k[0, -100:] = torch.randn(100, 1, d, device="cuda")
+    v[0, -100:] = torch.randn(100, 1, d, device="cuda")
+    q = torch.randn(1, 5, 1, d, device="cuda", dtype=torch.bfloat16)
+    blocks = -(-N // 64)
+    kept = np.zeros((1, 1, 1, blocks), bool)
+    kept[..., -2:] = True
+    words = torch.from_numpy(oracle.pack_blocks_ref(kept)).to("cuda")
+    out = torch.empty_like(q)
+    _forward(q, k, v, 8, 64, words, out)
+    first = (blocks - 2) * 64
+    tail = [host(t[:, first:]) for t in (k, v)]
+    ref, spread, mass = oracle.sparse_attention_ref(host(q), *tail, None, 8, 64)
+    tol = attention_bound(host(q), tail[0], spread, mass, ref, "bf16", 0.125, 128)
+    assert (np.abs(host(out) - ref) <= tol).all()
+
+
+def test_rotate_select_attend_together():
+    """The three operators one after the other on the rows of one projection, as an attention layer over video tokens calls
+    them.  The features are clusters, so that the selection has margins that a rounding of q and k cannot bridge."""
+    rng = np.random.default_rng(11)
+    F, H, W, heads, d, q_block, k_block, keep = 4, 8, 12, 2, 64, 64, 64, 2
+    N = F * H * W
+    near = np.repeat(np.tile(rng.standard_normal((1, N // 128, heads, d)), (1, 2, 1, 1)), 64, axis=1)  # blocks j and j + 3 are alike
+    q, k = (draw(rng, (1, N, heads, d), "bf16", 0.3) for _ in range(2))
+    q, k = (wl.round_to_storage((t + 1.5 * near).astype(np.float32), "bf16") for t in (q, k))
+    v = draw(rng, (1, N, heads, d), "bf16")
+    rows = torch.from_numpy(np.concatenate([q, k, v], axis=2)).to("cuda").to(torch.bfloat16)
+    dq, dk, dv = rows[:, :, :heads], rows[:, :, heads:2 * heads], rows[:, :, 2 * heads:]
+    si.si_rope_forward(dq, dk, si.Rope((F, H, W), (4, 6, 6), theta=100.0, step=(0.1, 0.1, 0.1)), dq, dk)
+    ws = torch.empty(max(si.si_attn_select_workspace_bytes(dq, dk, q_block, k_block), si.si_attn_sparse_workspace_bytes(dq, dk, q_block, k_block)),
+                     dtype=torch.uint8, device="cuda")
+    words = torch.empty(1, heads, N // q_block, si.si_attn_block_words(N, k_block), dtype=torch.int32, device="cuda")
+    out = torch.empty(1, N, heads, d, dtype=torch.bfloat16, device="cuda")
+    si.si_attn_select(dq, dk, q_block, k_block, keep, words, ws)
+    si.si_attn_sparse_forward(dq, dk, dv, q_block, k_block, words, out, ws)
+    torch.cuda.synchronize()
+    angles = oracle.rope_angles_ref((F, H, W), (4, 6, 6), 100.0, step=(0.1, 0.1, 0.1))
+    rq, rk = oracle.rope_ref(q, angles), oracle.rope_ref(k, angles)
+    scores = oracle.block_scores_ref(rq, rk, q_block, k_block)
+    # q and k are off by half a bf16 step each: a score moves by at most 2 * 2^-8 of the means' absolute product
+    moved = 2.02 * 2.0 ** -8 * oracle.block_scores_ref(np.abs(rq), np.abs(rk), q_block, k_block)
+    order = np.argsort(-scores, axis=-1)
+    low, high = (np.take_along_axis(t, order, axis=-1) for t in (scores - moved, scores + moved))
+    assert (low[..., :keep].min(axis=-1) > high[..., keep:].max(axis=-1)).all()
+    kept = oracle.select_ref(rq, rk, q_block, k_block, keep)
+    assert np.array_equal(words.cpu().numpy(), oracle.pack_blocks_ref(kept))
+    # the oracle goes on from the rotated heads as they were stored
+    sq, sk = host(dq), host(dk)
+    ref, spread, mass = oracle.sparse_attention_ref(sq, sk, v, kept, q_block, k_block)
+    assert (np.abs(host(out) - ref) <= attention_bound(sq, sk, spread, mass, ref, "bf16", 0.125, N)).all()
