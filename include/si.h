@@ -410,6 +410,26 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
                                  float scale, const int32_t* q_len, const int32_t* k_len, const uint32_t* blocks,
                                  si_heads* out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* A spatial block whose self-attention takes rotary positions and attends over
+ * selected key blocks; everything else as si_block_forward_ex (same flags).
+ *   rope     NULL: queries and keys are not rotated.  Else, after their projection,
+ *            as si_rope_forward does; extent[1], extent[2] are the block's H, W
+ *            (SI_ERR_SHAPE).  The frame axis turns the queries and keys of a frame
+ *            alike and so drops out of a spatial block.
+ *   keep     0: every key.  Else the `keep` best key blocks of every run of q_block
+ *            queries, per frame and head, as si_attn_select and
+ *            si_attn_sparse_forward define them (scale 1/sqrt(dim_head)).
+ * Every slicing of a call gives the same bits.  Temporal blocks -> SI_ERR_ARG. */
+typedef struct {
+  const si_rope* rope;
+  int64_t q_block, k_block, keep;
+} si_attn_options;
+size_t si_block_attn_workspace_bytes(const si_tensor5* x, const si_block_weights* w, const si_context* ctx,
+                                     const si_attn_options* attn, int32_t axis, int64_t slice_len);
+si_status si_block_forward_attn(const si_tensor5* x, const si_block_weights* w, const si_context* ctx,
+                                const si_attn_options* attn, si_tensor5* out, int32_t axis, int64_t slice_len,
+                                void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+
 /* Key-step search, Algorithm 1 (Appendix B).  Host only.
  *   S      host, row-major K x K similarity map; only S[i][anchor] entries are read
  *   gamma  threshold, must satisfy gamma <= 1 and gamma <= S[i][i] where visited

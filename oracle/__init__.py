@@ -27,4 +27,5 @@ from .resblock_ref import (  # noqa: F401
 )
 from .attn_ref import (  # noqa: F401
     rope_angles_ref, rms_norm_ref, rope_ref, block_scores_ref, pack_blocks_ref, select_ref, sparse_attention_ref,
+    block_forward_attn_ref,
 )

@@ -121,3 +121,33 @@ def sparse_attention_ref(q, k, v, kept, q_block, k_block, scale=None, q_len=None
                 for n in range(o.shape[0]):
                     spread[b, rows.start + n, h] = p[n] @ np.abs(vs - o[n])
     return out, spread, mass
+
+
+def block_forward_attn_ref(x, w, hp, ctx, rope=None, q_block=128, k_block=64, keep=0, return_scores=False):
+    """Spatial block (block_ref.block_forward_ref) whose self-attention is rotated and / or restricted to selected blocks.
+
+    rope: keyword arguments (extent, pairs and the rest) of rope_angles_ref, and halves, norm_eps, q_gain, k_gain of rope_ref."""
+    from .block_ref import (attention_ref, feature_from_tokens_ref, gelu_erf_ref, group_norm_ref, layer_norm_ref,
+                            tokens_from_feature_ref)
+    W = {k: np.asarray(v, F64) for k, v in w.items()}
+    x = np.asarray(x, F64)
+    t = tokens_from_feature_ref(group_norm_ref(x, hp.gn_groups, hp.gn_eps, w["gn_g"], w["gn_b"]), "spatial")
+    h = t @ W["w_in"] + W["b_in"]
+    a = layer_norm_ref(h, W["ln1_g"], W["ln1_b"], hp.ln_eps)
+    split = lambda y: y.reshape(y.shape[0], y.shape[1], hp.heads, -1)  # noqa: E731
+    q, k, v = (split(a @ W[n]) for n in ("wq", "wk", "wv"))
+    if rope is not None:
+        turn = {n: rope[n] for n in ("halves", "norm_eps") if n in rope}
+        angles = rope_angles_ref(**{n: rope[n] for n in ("extent", "pairs", "theta", "origin", "step") if n in rope})
+        q, k = (rope_ref(y, angles, gain=rope.get(g), **turn) for y, g in ((q, "q_gain"), (k, "k_gain")))
+    kept = select_ref(q, k, q_block, k_block, keep) if keep else None
+    o = sparse_attention_ref(q, k, v, kept, q_block, k_block)[0].reshape(a.shape[0], a.shape[1], -1)
+    h = h + o @ W["wo"] + W["bo"]
+    a = layer_norm_ref(h, W["ln2_g"], W["ln2_b"], hp.ln_eps)
+    c = np.repeat(np.asarray(ctx, F64), x.shape[2], axis=0)
+    h = h + attention_ref(a @ W["wq2"], c @ W["wk2"], c @ W["wv2"], hp.heads) @ W["wo2"] + W["bo2"]
+    u = layer_norm_ref(h, W["ln3_g"], W["ln3_b"], hp.ln_eps) @ W["w1"] + W["b1"]
+    half = u.shape[-1] // 2
+    h = h + (u[..., :half] * gelu_erf_ref(u[..., half:])) @ W["w2"] + W["b2"]
+    out = x + feature_from_tokens_ref(h @ W["w_out"] + W["b_out"], "spatial", x.shape)
+    return (out, block_scores_ref(q, k, q_block, k_block)) if return_scores else out

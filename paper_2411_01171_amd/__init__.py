@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     Rope, SI_ROPE_INTERLEAVED, SI_ROPE_HALVES, si_rope_forward,
     si_attn_block_words, si_attn_select_workspace_bytes, si_attn_select,
     si_attn_sparse_workspace_bytes, si_attn_sparse_forward,
+    AttnOptions, si_block_attn_workspace_bytes, si_block_forward_attn,
     si_rehash_scratch_bytes, si_rehash_check, si_rehash_check_sync, si_key_step_search,
     si_init_device, si_rehash_check_static,
     si_stage_timing_enable, si_stage_timing_read, si_status_str, si_abi_version,

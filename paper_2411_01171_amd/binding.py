@@ -68,6 +68,10 @@ class _Rope(C.Structure):
                 ("q_gain", C.c_void_p), ("k_gain", C.c_void_p)]
 
 
+class _AttnOptions(C.Structure):
+    _fields_ = [("rope", C.POINTER(_Rope)), ("q_block", C.c_int64), ("k_block", C.c_int64), ("keep", C.c_int64)]
+
+
 class _RehashCache(C.Structure):
     _fields_ = [("x_key", C.c_void_p), ("y_key", C.c_void_p), ("valid", C.c_int32)]
 
@@ -122,6 +126,11 @@ def lib() -> C.CDLL:
     L.si_attn_sparse_workspace_bytes.argtypes = [ph, ph, i64, i64]
     L.si_attn_sparse_forward.restype = i32
     L.si_attn_sparse_forward.argtypes = [ph, ph, ph, i64, i64, C.c_float, vp, vp, vp, ph, vp, sz, vp]
+    po = C.POINTER(_AttnOptions)
+    L.si_block_attn_workspace_bytes.restype = sz
+    L.si_block_attn_workspace_bytes.argtypes = L.si_workspace_bytes.argtypes[:3] + [po, i32, i64]
+    L.si_block_forward_attn.restype = i32
+    L.si_block_forward_attn.argtypes = L.si_block_forward.argtypes[:3] + [po, C.POINTER(_Tensor5), i32, i64, vp, sz, C.c_uint32, vp]
     L.si_rehash_scratch_bytes.restype = sz
     L.si_rehash_scratch_bytes.argtypes = [i64]
     L.si_rehash_check.restype = i32
@@ -437,6 +446,36 @@ def si_attn_sparse_forward(q, k, v, q_block: int, k_block: int, blocks, out, wor
                                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), st)
     if status != 0:
         raise SiError(status, "si_attn_sparse_forward")
+
+
+class AttnOptions:
+    """Self-attention of si_block_forward_attn: rotary positions (a Rope or None) and, with keep > 0, the `keep` best blocks of
+    k_block keys for every run of q_block queries."""
+
+    def __init__(self, rope: Optional[Rope] = None, q_block: int = 128, k_block: int = 64, keep: int = 0):
+        self.rope = rope
+        self.struct = _AttnOptions(None if rope is None else C.pointer(rope.struct), q_block, k_block, keep)
+
+
+def si_block_attn_workspace_bytes(x, weights: BlockWeights, ctx, attn: AttnOptions, axis: int, slice_len: int) -> int:
+    xd = _tensor5(x)
+    pc, _keep = _pctx(ctx)
+    return int(lib().si_block_attn_workspace_bytes(C.byref(xd), C.byref(weights.struct), pc, C.byref(attn.struct), axis, slice_len))
+
+
+def si_block_forward_attn(x, weights: BlockWeights, ctx, attn: AttnOptions, out, axis: int, slice_len: int, workspace, flags: int = 0,
+                          stream=None) -> None:
+    """si_block_forward_ex of a spatial block whose self-attention is the one that `attn` describes."""
+    if attn.rope is not None:
+        for g in attn.rope.gains:
+            if g is not None and (g.shape[0] != weights.struct.dim_head or g.dtype != x.dtype):
+                raise ValueError("gains must be [dim_head] in the feature's dtype")
+    xd, od = _tensor5(x), _tensor5(out)
+    pc, _keep = _pctx(ctx)
+    st = lib().si_block_forward_attn(C.byref(xd), C.byref(weights.struct), pc, C.byref(attn.struct), C.byref(od), axis, slice_len,
+                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), flags, _stream_ptr(stream))
+    if st != 0:
+        raise SiError(st, "si_block_forward_attn")
 
 
 class RehashCache:

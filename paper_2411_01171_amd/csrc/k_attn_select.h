@@ -17,7 +17,6 @@ typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kMeanPieces = 32, kMeanSlices = 8;  // 16-byte pieces of a row x rows in flight of one workgroup
 constexpr int kSelectThreads = 512;
-constexpr int kSelectMaxBlocks = 16384;           // one run's scores fill the LDS of a workgroup
 
 struct MeansArgs {
   HeadsView x;

@@ -131,18 +131,44 @@ struct Plan {
   int lanes;        // slices in flight (many small slices: 2 or 3, each on a stream of its own)
   size_t lane_stride;  // bytes between two lanes' slice intermediates
   int Mcp;          // context tokens rounded up to a multiple of 8 (transposed value copy)
+  const si_attn_options* attn;  // self-attention of a spatial block with rotary positions / over selected key blocks, or NULL
+  BlocksPlan blocks;            // attn: runs and key blocks of a frame
   // workspace offsets (bytes)
   size_t off_stats, off_rehash, off_pe, off_ctxkv, off_ctxvt, off_ml;
   size_t off_w_in, off_wqkv, off_wo, off_wq2, off_wkv2, off_wo2, off_w1, off_w2, off_w_out;
   size_t off_a, off_h, off_big, off_ffn_stream, off_attn_stream, off_pre_stream;
+  size_t off_lists, off_attn_ws;  // attn: bitmaps of a window; workspace of the selection / the attention
   size_t weights_bytes, total_bytes;
 };
 
 // sub-chunks of context fragments per batch entry in the post-attention kernel's stream
 static int post_ctx_sub(const Plan& p) { return (p.D / 64) * kCrossOps / (2 * p.fused_nb); }
 
+// Queries (0), keys (1) and values (2) of a window's frames in the projection's rows, one sequence per frame.
+static si_heads window_heads(const Plan& p, void* rows, int64_t frames, int which) {
+  char* ptr = rows ? static_cast<char*>(rows) + (size_t)which * p.D * p.esize : nullptr;
+  return si_heads{ptr, p.dtype, (int64_t)p.B * frames, p.P, p.heads, p.d, p.P * 3 * p.D, (int64_t)3 * p.D, p.d};
+}
+
+// Options of a spatial block's self-attention; sizes only (`attn` keeps the pointers).
+static si_status plan_attn(const si_attn_options* o, Plan* p) {
+  p->attn = o;
+  if (!o) return SI_OK;
+  if (p->kind != SI_BLOCK_SPATIAL || o->keep < 0) return SI_ERR_ARG;
+  const si_heads q = window_heads(*p, nullptr, p->slice_len, 0), k = window_heads(*p, nullptr, p->slice_len, 1);
+  const si_status s = plan_blocks(&q, &k, o->q_block, o->k_block, &p->blocks);
+  if (s != SI_OK) return s;
+  if (o->keep && p->blocks.blocks > kSelectMaxBlocks) return SI_ERR_SHAPE;
+  if (o->rope) {
+    const si_status r = check_rope(o->rope, p->d);
+    if (r != SI_OK) return r;
+    if (o->rope->extent[1] != p->H || o->rope->extent[2] != p->W) return SI_ERR_SHAPE;
+  }
+  return SI_OK;
+}
+
 static si_status make_plan(const si_tensor5* x, const si_block_weights* w, const si_context* ctx, int32_t axis,
-                           int64_t slice_len, Plan* p) {
+                           int64_t slice_len, Plan* p, const si_attn_options* attn = nullptr) {
   if (!x || !w) return SI_ERR_NULL;
   if (x->dtype != SI_F32 && x->dtype != SI_BF16) return SI_ERR_DTYPE;
   if (w->kind != SI_BLOCK_TEMPORAL && w->kind != SI_BLOCK_SPATIAL) return SI_ERR_ARG;
@@ -180,6 +206,10 @@ static si_status make_plan(const si_tensor5* x, const si_block_weights* w, const
   p->slice_len = slice_len < p->extent ? slice_len : p->extent;
   p->Mmax = axis == SI_AXIS_F ? (int64_t)x->B * p->slice_len * P : (int64_t)x->B * x->F * p->slice_len;
   if (p->Mmax >= (1LL << 31) / 16) return SI_ERR_SHAPE;
+  {
+    const si_status s = plan_attn(attn, p);
+    if (s != SI_OK) return s;
+  }
 
   const size_t es = (size_t)p->esize;
   const size_t C = (size_t)p->C, Dz = (size_t)D;
@@ -212,7 +242,7 @@ static si_status make_plan(const si_tensor5* x, const si_block_weights* w, const
   // a workgroup's 128 tokens share one context (P % 128 == 0: frames are whole workgroups), heads of 64
   // channels (two 32-channel blocks), at most kCrossTiles key tiles
   p->post_fused = p->fused_nb == 10 && p->kind == SI_BLOCK_SPATIAL && p->attn_mfma && p->d == 64 && P % 128 == 0 &&
-                  p->Mc <= 32 * kCrossTiles;
+                  p->Mc <= 32 * kCrossTiles && !p->attn;
   // heads of 64: context values with keys contiguous (the post-attention kernel has its own form)
   p->off_ctxvt = take(p->attn_mfma && !p->post_fused ? (size_t)p->B * Dz * p->Mcp * es : 0);
   // fp32 temporal blocks whose sequences and operands fit a workgroup's LDS take the one-kernel form, except where a
@@ -259,6 +289,12 @@ static si_status make_plan(const si_tensor5* x, const si_block_weights* w, const
   }
   // post_fused: (reference maximum, row sum) of the two key halves
   p->off_ml = take(p->post_fused ? (size_t)2 * p->heads * (p->Mmax / 32) * kWave * sizeof(float2) : 0);
+  p->off_lists = p->off_attn_ws = off;
+  if (p->attn && p->attn->keep) {
+    const si_heads q = window_heads(*p, nullptr, p->slice_len, 0), k = window_heads(*p, nullptr, p->slice_len, 1);
+    p->off_lists = take((size_t)(q.B * q.heads * p->blocks.runs * p->blocks.words) * sizeof(uint32_t));
+    p->off_attn_ws = take(select_bytes(&q, &k, p->blocks));
+  }
   // Cross-slice pipelining (Sec. 4.2.2): with many small slices the kernels of one slice leave CUs
   // idle (under-filled grids, partial last rounds), so several windows run at a time, each on a
   // stream and with intermediates of its own: as many as keep the window intermediates in flight
@@ -736,6 +772,22 @@ static si_status run_block_f32(const Plan& p, const float* X, const si_block_wei
   return SI_OK;
 }
 
+// Self-attention of a spatial window with options: rotates the queries and keys in the projection's rows, selects key blocks,
+// attends.  A frame is a sequence; where its rows lie on the frame axis turns queries and keys alike and drops out.  A run's
+// blocks stay with one workgroup, however few there are, so that every slicing of a call gives the same bits.
+static si_status run_window_attention(const Plan& p, void* rows, void* out, int64_t frames, int o_frag, uint32_t* lists, char* attn_ws,
+                                      float scale, hipStream_t st) {
+  const si_attn_options& o = *p.attn;
+  const si_heads q = window_heads(p, rows, frames, 0), k = window_heads(p, rows, frames, 1), v = window_heads(p, rows, frames, 2);
+  const si_heads y{out, p.dtype, q.B, q.N, q.heads, q.dim_head, p.P * p.D, p.D, p.d};
+  if (o.rope) SI_TRY(enqueue_rope(&q, &k, o.rope, 0, &q, &k, st));
+  if (o.keep) SI_TRY(enqueue_select(&q, &k, p.blocks, o.q_block, o.k_block, o.keep, nullptr, nullptr, lists, attn_ws, st));
+  SparsePlan sp;
+  SI_TRY(plan_sparse(&q, &k, o.q_block, p.blocks, false, &sp));
+  return enqueue_sparse(&q, &k, &v, p.blocks, sp, o.q_block, o.k_block, scale, nullptr, nullptr, o.keep ? lists : nullptr, &y, nullptr, st,
+                        o_frag);
+}
+
 template <typename T>
 static si_status run_block(const Plan& p, const si_tensor5* x, const si_block_weights* w, const si_context* ctx,
                            si_tensor5* out, char* ws, hipStream_t st, bool stats_done = false, bool packed = false) {
@@ -947,7 +999,7 @@ static si_status run_block(const Plan& p, const si_tensor5* x, const si_block_we
       SI_TRY(launch_layer_norm<T>("ln1", h, a, M, D, w->ln1_g, w->ln1_b, w->ln_eps, pe, win.Pw, win.Fw, win.f0, st, ring));
       bool self_done = false;
       if constexpr (sizeof(T) == 2) {
-        if (p.attn_mfma) {  // spatial: sequence (b, f) = rows (b*Fw + f)*Pw + i; the projection writes V transposed
+        if (p.attn_mfma && !p.attn) {  // spatial: sequence (b, f) = rows (b*Fw + f)*Pw + i; the projection writes V transposed
           bf16* vt = reinterpret_cast<bf16*>(big) + 3 * M * D;  // behind the q / k / v rows
           EpiStoreQKVt epi{big, (int64_t)3 * D, vt, D, win.Pw, qscale2};
           SI_TRY((launch_gemm_sel<T, false>("qkv", ring, a, (int64_t)D, wqkv, M, Mx, 3 * D, D, epi, st)));
@@ -961,6 +1013,13 @@ static si_status run_block(const Plan& p, const si_tensor5* x, const si_block_we
           EpiStore<T> epi{big, (int64_t)3 * D, nullptr};
           SI_TRY((launch_gemm_sel<T, false>("qkv", ring, a, (int64_t)D, wqkv, M, Mx, 3 * D, D, epi, st)));
         }
+        if (p.attn) {
+          SI_TRY(run_window_attention(p, big, a, win.Fw, self_frag ? D : 0, reinterpret_cast<uint32_t*>(ws + p.off_lists + lane_off),
+                                      ws + p.off_attn_ws + lane_off, scale, st));
+          self_done = true;
+        }
+      }
+      if (!self_done) {
         AttnArgs at;
         at.q = big; at.k = big + D; at.v = big + 2 * D; at.o = a;
         at.ldq = at.ldk = at.ldv = (int64_t)3 * D; at.ldo = D;
@@ -1167,9 +1226,10 @@ int32_t si_windows_in_flight(const si_tensor5* x, const si_block_weights* w, con
 
 // Argument checks shared by the forward entry points; fills the plan.
 static si_status check_forward(const si_tensor5* x, const si_block_weights* w, const si_context* ctx, si_tensor5* out,
-                               int32_t axis, int64_t slice_len, void* workspace, size_t workspace_bytes, si::Plan& p) {
+                               int32_t axis, int64_t slice_len, void* workspace, size_t workspace_bytes, si::Plan& p,
+                               const si_attn_options* attn = nullptr) {
   if (!x || !w || !out) return SI_ERR_NULL;
-  si_status s = si::make_plan(x, w, ctx, axis, slice_len, &p);
+  si_status s = si::make_plan(x, w, ctx, axis, slice_len, &p, attn);
   if (s != SI_OK) return s;
   if (out->dtype != x->dtype) return SI_ERR_DTYPE;
   if (out->B != x->B || out->C != x->C || out->F != x->F || out->H != x->H || out->W != x->W) return SI_ERR_SHAPE;
@@ -1200,13 +1260,9 @@ static si_status check_forward(const si_tensor5* x, const si_block_weights* w, c
   return SI_OK;
 }
 
-si_status si_block_forward_ex(const si_tensor5* x, const si_block_weights* w, const si_context* ctx, si_tensor5* out,
-                              int32_t axis, int64_t slice_len, void* workspace, size_t workspace_bytes, uint32_t flags,
-                              void* stream) {
-  if (flags & ~(uint32_t)SI_FWD_WEIGHTS_PACKED) return SI_ERR_ARG;
-  si::Plan p;
-  si_status s = check_forward(x, w, ctx, out, axis, slice_len, workspace, workspace_bytes, p);
-  if (s != SI_OK) return s;
+// Checks done: the workspace's record and the launches.
+static si_status start_forward(const si::Plan& p, const si_tensor5* x, const si_block_weights* w, const si_context* ctx, si_tensor5* out,
+                               void* workspace, uint32_t flags, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   const bool packed = (flags & SI_FWD_WEIGHTS_PACKED) != 0;
@@ -1215,6 +1271,34 @@ si_status si_block_forward_ex(const si_tensor5* x, const si_block_weights* w, co
   if (!packed) si::pack_record(workspace, fp);
   if (p.dtype == SI_F32) return si::run_block<float>(p, x, w, ctx, out, ws, st, false, packed);
   return si::run_block<si::bf16>(p, x, w, ctx, out, ws, st, false, packed);
+}
+
+si_status si_block_forward_ex(const si_tensor5* x, const si_block_weights* w, const si_context* ctx, si_tensor5* out,
+                              int32_t axis, int64_t slice_len, void* workspace, size_t workspace_bytes, uint32_t flags,
+                              void* stream) {
+  if (flags & ~(uint32_t)SI_FWD_WEIGHTS_PACKED) return SI_ERR_ARG;
+  si::Plan p;
+  si_status s = check_forward(x, w, ctx, out, axis, slice_len, workspace, workspace_bytes, p);
+  if (s != SI_OK) return s;
+  return start_forward(p, x, w, ctx, out, workspace, flags, stream);
+}
+
+size_t si_block_attn_workspace_bytes(const si_tensor5* x, const si_block_weights* w, const si_context* ctx, const si_attn_options* attn,
+                                     int32_t axis, int64_t slice_len) {
+  si::Plan p;
+  if (!attn || si::make_plan(x, w, ctx, axis, slice_len, &p, attn) != SI_OK) return 0;
+  return p.total_bytes;
+}
+
+si_status si_block_forward_attn(const si_tensor5* x, const si_block_weights* w, const si_context* ctx, const si_attn_options* attn,
+                                si_tensor5* out, int32_t axis, int64_t slice_len, void* workspace, size_t workspace_bytes, uint32_t flags,
+                                void* stream) {
+  if (flags & ~(uint32_t)SI_FWD_WEIGHTS_PACKED) return SI_ERR_ARG;
+  if (!attn) return SI_ERR_NULL;
+  si::Plan p;
+  si_status s = check_forward(x, w, ctx, out, axis, slice_len, workspace, workspace_bytes, p, attn);
+  if (s != SI_OK) return s;
+  return start_forward(p, x, w, ctx, out, workspace, flags, stream);
 }
 
 si_status si_block_forward(const si_tensor5* x, const si_block_weights* w, const si_context* ctx, si_tensor5* out,

@@ -6,6 +6,8 @@
 
 namespace si {
 
+constexpr int64_t kSelectMaxBlocks = 16384;  // one run's scores fill the LDS of a workgroup
+
 struct BlocksPlan {
   int64_t runs, blocks, words;
   int group;
@@ -19,7 +21,7 @@ struct SparsePlan {
 
 si_status check_rope(const si_rope* r, int d);
 si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block, BlocksPlan* p);
-si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, SparsePlan* p);
+si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, bool may_split, SparsePlan* p);
 size_t select_bytes(const si_heads* q, const si_heads* k, const BlocksPlan& p);
 
 // The operands of these have been checked.  k and ko may be NULL.

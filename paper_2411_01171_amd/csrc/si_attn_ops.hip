@@ -260,7 +260,7 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
 
 // Wavefronts of a workgroup and shares of a run's blocks.  A run with up to 32 (64) rows takes one (two) wavefronts.  Blocks
 // are dealt out to several workgroups while there are fewer than two for every CU.
-si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, SparsePlan* p) {
+si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, bool may_split, SparsePlan* p) {
   const int64_t rows = b.group * std::min<int64_t>(q_block, std::max<int64_t>(q->N, 1));
   p->nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
   const int d = (int)q->dim_head;
@@ -271,7 +271,7 @@ si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, con
   p->tiles = q->B * k->heads * b.runs * p->tiles_per_run;
   const int64_t want = p->nw == 1 ? 1024 : 512;
   p->nsplit = 1;
-  if (p->tiles > 0 && p->tiles * 2 <= want) p->nsplit = (int)std::min<int64_t>(std::min<int64_t>(want / p->tiles, 64), std::max<int64_t>(1, b.blocks / 2));
+  if (may_split && p->tiles > 0 && p->tiles * 2 <= want) p->nsplit = (int)std::min<int64_t>(std::min<int64_t>(want / p->tiles, 64), std::max<int64_t>(1, b.blocks / 2));
   p->work = p->tiles * p->nsplit;
   p->part_bytes = p->nsplit > 1 ? (size_t)p->work * p->nw * (p->ob * 4 + 1) * kWave * 16 : 0;
   return SI_OK;
@@ -407,7 +407,7 @@ static si_status check_sparse(const si_heads* q, const si_heads* k, int64_t q_bl
   si_status s = si::check_heads(q, false);
   if (s == SI_OK) s = si::check_heads(k, false);
   if (s == SI_OK) s = si::plan_blocks(q, k, q_block, k_block, b);
-  if (s == SI_OK) s = si::plan_sparse(q, k, q_block, *b, p);
+  if (s == SI_OK) s = si::plan_sparse(q, k, q_block, *b, true, p);
   return s;
 }
 
