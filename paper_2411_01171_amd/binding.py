@@ -346,10 +346,13 @@ class Rope:
 
 
 def _heads(t) -> _Heads:
-    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
-        raise ValueError("heads must be a [B, N, heads, dim_head] tensor with contiguous channels")
-    B, N, h, d = t.shape
-    sb, sn, sh, _ = t.stride()
+    try:
+        B, N, h, d = t.shape
+    except ValueError:
+        raise ValueError("heads must be a [B, N, heads, dim_head] tensor") from None
+    sb, sn, sh, sc = t.stride()
+    if sc != 1 and d > 1:
+        raise ValueError("the channels of heads must be contiguous")
     return _Heads(t.data_ptr(), _dtype_code(t), B, N, h, d, sb, sn, sh)
 
 
@@ -358,11 +361,14 @@ class _on_device:
 
     def __init__(self, stream, first, *others):
         import torch
-        if first.device.type != "cuda" or any(t is not None and t.device != first.device for t in others):
+        index = first.get_device()  # -1: not on a GPU
+        for t in others:
+            if t is not None and t.get_device() != index:
+                index = -1
+        if index < 0:
             raise ValueError("all tensors must be on one GPU")
-        self.device = first.device
-        self.guard = None if first.device.index == torch.cuda.current_device() else torch.cuda.device(first.device)
-        self.stream = _stream_ptr(torch.cuda.current_stream(first.device) if stream is None else stream)
+        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
+        self.stream = _stream_ptr(torch.cuda.current_stream(index) if stream is None else stream)
 
     def __enter__(self):
         if self.guard is not None:

@@ -148,17 +148,18 @@ template <> struct SparseShape<float> {
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
+template <typename V> __device__ __forceinline__ V lds_read(unsigned at) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) V*>((size_t)at);
+}
 // ds_read_b64_tr_b16: of the 16 lanes of a group, lane i reads 8 bytes of its own address (row i / 4, columns
 // 4 (i % 4) .. + 3 of a 4 x 16 tile) and receives column i: four rows' values of one channel
-__device__ __forceinline__ uint2 lds_read_tr(const char* p) {
-  const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) s16x4_t*)(__attribute__((address_space(3))) char*)const_cast<char*>(p));
-  return __builtin_bit_cast(uint2, v);
+__device__ __forceinline__ uint2 lds_read_tr(unsigned at) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4_t*>((size_t)at)));
 }
 
 // Output of one wavefront: lane (r, g) holds query row r's channels 32 b + 8 q + 4 g + j in register 16 b + 4 q + j.
 template <typename T, int OB>
-__device__ __forceinline__ void sparse_store(const SparseArgs& a, const float (&o)[OB * 16], float lsum, int b, int hk, int token, int sub,
+__device__ __forceinline__ void sparse_store(const SparseArgs& a, const f32x16_t (&o)[OB], float lsum, int b, int hk, int token, int sub,
                                              bool valid, int g) {
   if (!valid) return;
   const float inv = lsum > 0.f ? 1.f / lsum : 0.f;  // a row without keys gives zero
@@ -172,7 +173,7 @@ __device__ __forceinline__ void sparse_store(const SparseArgs& a, const float (&
       if (ch >= a.d) continue;
       float y[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = lsum > 0.f ? o[16 * i + 4 * q + j] * inv : 0.f;
+      for (int j = 0; j < 4; ++j) y[j] = lsum > 0.f ? o[i][4 * q + j] * inv : 0.f;
       if constexpr (sizeof(T) == 2) {
         bf16* dst = a.o_frag ? static_cast<bf16*>(a.o) + act_offset((int64_t)b * a.Nq + token, h * a.d + ch, a.o_frag)
                              : reinterpret_cast<bf16*>(row) + ch;
@@ -185,7 +186,7 @@ __device__ __forceinline__ void sparse_store(const SparseArgs& a, const float (&
 
 // KS: head channels in steps of 16 (d <= 16 KS).
 template <typename T, int KS, int NW>
-__global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
+__global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3 : 2) void sparse_attn_kernel(SparseArgs a) {
   using Shape = SparseShape<T>;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int SK = Shape::SK, VEC = Shape::VEC;
@@ -196,13 +197,32 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
   constexpr int HALF = SK * ROW;                                  // bytes of a stage's keys; its values follow
   constexpr int NS = HALF <= 8192 ? 3 : 2;                        // stages in LDS
   constexpr int LOADS = HALF / 1024;                              // wave-wide loads of a stage's keys
-  constexpr int PER = (LOADS + NW - 1) / NW;                      // per wavefront
+  constexpr int PER = LOADS / NW;                                 // per wavefront
+  constexpr int QS = F32 ? KS * 2 : KS;                           // pieces of a query per lane
   static_assert(LOADS % NW == 0, "every wavefront issues the same number of loads, the waits count them");
-  __shared__ u32x4_t ring[NS * 2 * HALF / 16];
-  char* const lds = reinterpret_cast<char*>(&ring[0]);
+  __shared__ __align__(1024) u32x4_t ring[NS * 2 * HALF / 16];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 32, g = lane / 32;
+  auto swizzle = [](int row) { return PR == 4 ? (row >> 1) & 3 : row & 7; };
+
+  // ---- what stays the same through all stages, per lane.  Load i of a half: rows (wave + NW i) (64 / PR) .., lane l takes
+  // slot l % PR of row l / PR of them.
+  unsigned koff[PER], voff[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int row = (wave + NW * i) * (64 / PR) + lane / PR, piece = (lane % PR) ^ swizzle(row);
+    koff[i] = (unsigned)(row * (int)a.kn + piece * VEC) * (unsigned)sizeof(T);  // the host keeps this inside 31 bits
+    voff[i] = (unsigned)(row * (int)a.vn + piece * VEC) * (unsigned)sizeof(T);
+  }
+  const bool whole_rows = a.d == PR * VEC;
+  // LDS addresses of the first fragments; pieces further on are exclusive-ors (rows are aligned to their length)
+  const unsigned kat = lds0 + r * ROW + (g ^ swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
+  // bf16: step t of 16 keys: slots e < 4 of group g are keys 16 t + 4 g + e, the others 16 t + 8 + 4 g + e - 4; channel block i: ^ 64 i
+  // f32: register (q, j) of the scores is key 8 q + 4 g + j; row 4 g + j: + j rows, ^ 16 j; channel block i: ^ 128 i
+  const int vr = F32 ? 4 * g : 4 * g + (lane % 16) / 4;
+  const unsigned vat = lds0 + HALF + vr * ROW +
+                       (F32 ? ((r / 4) ^ vr) * 16 + (r % 4) * 4 : ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ swizzle(vr)) * 16 + (lane % 2) * 8);
 
   // Work goes to the 8 XCDs in contiguous chunks, so that the keys and values of a head are fetched into one L2.
   const int64_t chunk = (a.work + 7) / 8;
@@ -229,11 +249,11 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
     const bool any = first_tok < a.q_block && (int64_t)run * a.q_block + first_tok < q_len;
     walk.begin(mrow, any ? a.words : 0, (k_len + a.k_block - 1) / a.k_block, a.k_block, k_len, part, a.nsplit);
 
-    // ---- stage loads: load i of a half covers rows i * (64 / PR) ..; lane l: row l / PR of them, slot l % PR
     const char* const kbase = static_cast<const char*>(a.k) + ((int64_t)b * a.kb + (int64_t)hk * a.kh) * (int64_t)sizeof(T);
     const char* const vbase = static_cast<const char*>(a.v) + ((int64_t)b * a.vb + (int64_t)hk * a.vh) * (int64_t)sizeof(T);
     int issued = 0, last_keys = SK;
     unsigned islot = 0;
+    // assembly: completion is awaited explicitly, the compiler would wait for all of it before the next LDS read
     auto issue = [&]() {
       const int key0 = walk.next();
       if (key0 < 0) return;
@@ -241,29 +261,37 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
       last_keys = nkeys;
       const char* ksrc = kbase + (int64_t)key0 * a.kn * (int64_t)sizeof(T);
       const char* vsrc = vbase + (int64_t)key0 * a.vn * (int64_t)sizeof(T);
-      const unsigned dst = lds0 + islot * (2 * HALF);
+      const unsigned dst = lds0 + islot + wave * 1024;
+      if (nkeys == SK && whole_rows) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int ld = wave + NW * i, row = ld * (64 / PR) + lane / PR;
-        const int piece = (lane % PR) ^ (PR == 4 ? (row >> 1) & 3 : row & 7);
-        const bool in = row < nkeys && piece * VEC < a.d;
-        const char* ks = in ? ksrc + ((int64_t)row * a.kn + piece * VEC) * (int64_t)sizeof(T) : reinterpret_cast<const char*>(kSparseZero);
-        const char* vs = in ? vsrc + ((int64_t)row * a.vn + piece * VEC) * (int64_t)sizeof(T) : reinterpret_cast<const char*>(kSparseZero);
-        // assembly: completion is awaited explicitly, the compiler would wait for all of it before the next LDS read
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ks), "s"(dst + ld * 1024) : "memory");
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(vs), "s"(dst + HALF + ld * 1024) : "memory");
+        for (int i = 0; i < PER; ++i) {
+          asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(koff[i]), "s"(ksrc), "s"(dst + NW * i * 1024) : "memory");
+          asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff[i]), "s"(vsrc), "s"(dst + HALF + NW * i * 1024) : "memory");
+        }
+      } else {  // keys past the end and channels past the head as zeros
+        int l = lane;
+        asm volatile("" : "+v"(l));  // rows and pieces are formed here again: kept through the loop they cost registers
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int row = (wave + NW * i) * (64 / PR) + l / PR, piece = (l % PR) ^ swizzle(row);
+          const bool in = piece * VEC < a.d && row < nkeys;
+          const char* ks = in ? ksrc + koff[i] : reinterpret_cast<const char*>(kSparseZero);
+          const char* vs = in ? vsrc + voff[i] : reinterpret_cast<const char*>(kSparseZero);
+          asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ks), "s"(dst + NW * i * 1024) : "memory");
+          asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(vs), "s"(dst + HALF + NW * i * 1024) : "memory");
+        }
       }
-      islot = islot + 1 == NS ? 0 : islot + 1;
+      islot = islot == (NS - 1) * 2 * HALF ? 0 : islot + 2 * HALF;
       ++issued;
     };
-
     for (int i = 0; i < NS - 1; ++i) issue();
+
     // ---- this lane's query as column operand: pieces as the keys' fragments have them
-    u32x4_t qop[F32 ? KS * 2 : KS];
+    u32x4_t qop[QS];
     {
       const T* qrow = static_cast<const T*>(a.q) + b * a.qb + (int64_t)token * a.qn + (int64_t)(hk * a.group + (valid ? sub : 0)) * a.qh;
 #pragma unroll
-      for (int s = 0; s < (F32 ? KS * 2 : KS); ++s) {
+      for (int s = 0; s < QS; ++s) {
         const int piece = 2 * s + g;
         qop[s] = u32x4_t{0, 0, 0, 0};
         if (piece * VEC < a.d && q_len > 0) qop[s] = *reinterpret_cast<const u32x4_t*>(qrow + piece * VEC);
@@ -271,9 +299,12 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // the query: nothing that the compiler tracks stays pending in the loop
 
-    float oacc[OB * 16], mref = kSparseLow, lsum = 0.f;
+    f32x16_t oacc[OB];
+    float mref = kSparseLow, lsum = 0.f;
 #pragma unroll
-    for (int i = 0; i < OB * 16; ++i) oacc[i] = 0.f;
+    for (int i = 0; i < OB; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) oacc[i][e] = 0.f;
     unsigned cslot = 0;
     for (int st = 0; st < issued; ++st) {
       const int younger = issued - 1 - st;  // stages in flight behind this one: at most NS - 2
@@ -282,9 +313,6 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
       __syncthreads();  // the stage is there for all, and nobody reads the slot that is filled next
       issue();
       const int nkeys = st + 1 == issued ? last_keys : SK;  // only the list's last stage can hold fewer
-      const char* const kst = lds + cslot * (2 * HALF);
-      const char* const vst = kst + HALF;
-      cslot = cslot + 1 == NS ? 0 : cslot + 1;
 
       // ---- scores of SK / 32 tiles of 32 keys
       f32x16_t sc[SK / 32];
@@ -292,26 +320,48 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
       for (int u = 0; u < SK / 32; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
-      const int fr = PR == 4 ? (r >> 1) & 3 : r & 7;
+      constexpr int KF = F32 ? 1 : QS;  // pieces of a key that are read ahead of the products
+      u32x4_t kf[KF][SK / 32];
 #pragma unroll
-      for (int s = 0; s < (F32 ? KS * 2 : KS); ++s)
+      for (int s = 0; s < QS; ++s) {
+        if (s % KF == 0) {
+#pragma unroll
+          for (int i = 0; i < KF; ++i)
+#pragma unroll
+            for (int u = 0; u < SK / 32; ++u) kf[i][u] = lds_read<u32x4_t>(((kat + cslot) ^ (32 * (s + i))) + 32 * u * ROW);
+          if constexpr (!F32) __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int u = 0; u < SK / 32; ++u) {
-          const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(kst + (32 * u + r) * ROW + (((2 * s + g) ^ fr) * 16));
           if constexpr (F32) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              sc[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[j]), __uint_as_float(qop[s][j]), sc[u], 0, 0, 0);
+              sc[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[0][u][j]), __uint_as_float(qop[s][j]), sc[u], 0, 0, 0);
           } else {
-            sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qop[s]), sc[u], 0, 0, 0);
+            sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s][u]), __builtin_bit_cast(bf16x8_t, qop[s]), sc[u], 0, 0, 0);
           }
         }
+      }
       if (nkeys < SK) {
+        const int lim = nkeys - 4 * g;  // register e of tile u is key 32 u + 8 (e / 4) + e % 4 + 4 g
 #pragma unroll
         for (int u = 0; u < SK / 32; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (32 * u + 8 * (e / 4) + 4 * g + e % 4 >= nkeys) sc[u][e] = -INFINITY;
+            if (32 * u + 8 * (e / 4) + e % 4 >= lim) sc[u][e] = -INFINITY;
+      }
+      // bf16 values on their way while the exponentials are taken
+      constexpr int VT = F32 ? 1 : SK / 16;
+      uint2 vlo[VT][OB], vhi[VT][OB];
+      if constexpr (!F32) {
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+#pragma unroll
+          for (int i = 0; i < OB; ++i) {
+            vlo[t][i] = lds_read_tr(((vat + cslot) ^ (64 * i)) + 16 * t * ROW);
+            vhi[t][i] = lds_read_tr(((vat + cslot) ^ (64 * i)) + (16 * t + 8) * ROW);
+          }
+        __builtin_amdgcn_sched_barrier(0);
       }
 
       // ---- probabilities against the lazy reference maximum: it is raised only when the partial sums say that an
@@ -350,55 +400,33 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
         mref = up;
         lsum *= alpha;
 #pragma unroll
-        for (int i = 0; i < OB * 16; ++i) oacc[i] *= alpha;
+        for (int i = 0; i < OB; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) oacc[i][e] *= alpha;
         rs = exponentiate();
       }
       lsum += rs;
 
       // ---- O^T += V^T P^T
-      f32x16_t acc[OB];
-#pragma unroll
-      for (int i = 0; i < OB; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][e] = oacc[16 * i + e];
       if constexpr (F32) {
-        // register (q, j) of the scores is key 8 q + 4 g + j: one step of two keys, the lane's own and lane ^ 32's
+        // one step of two keys: the lane's own and lane ^ 32's
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int row = 8 * q + 4 * g + j;
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < OB; ++i) {
-              const int piece = 8 * i + r / 4;
-              const float vf = *reinterpret_cast<const float*>(vst + row * ROW + ((piece ^ (row & 7)) * 16) + (r % 4) * 4);
-              acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, pf[4 * q + j], acc[i], 0, 0, 0);
-            }
-          }
+            for (int i = 0; i < OB; ++i)
+              oacc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(lds_read<float>(((vat + cslot) ^ (16 * j + 128 * i)) + (8 * q + j) * ROW), pf[4 * q + j], oacc[i], 0, 0, 0);
       } else {
-        // step t of 16 keys: slots e < 4 of group g are keys 16 t + 4 g + e, the others 16 t + 8 + 4 g + e - 4
-        const int vr = 4 * g + (lane % 16) / 4, vp = 2 * ((lane / 16) % 2) + (lane % 4) / 2;
 #pragma unroll
         for (int t = 0; t < SK / 16; ++t)
 #pragma unroll
           for (int i = 0; i < OB; ++i) {
-            uint2 lo, hi;
-            {
-              const int row = 16 * t + vr, sw = PR == 4 ? (row >> 1) & 3 : row & 7;
-              lo = lds_read_tr(vst + row * ROW + (((4 * i + vp) ^ sw) * 16) + (lane % 2) * 8);
-            }
-            {
-              const int row = 16 * t + 8 + vr, sw = PR == 4 ? (row >> 1) & 3 : row & 7;
-              hi = lds_read_tr(vst + row * ROW + (((4 * i + vp) ^ sw) * 16) + (lane % 2) * 8);
-            }
-            const u32x4_t vf{lo.x, lo.y, hi.x, hi.y};
-            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[t]), acc[i], 0, 0, 0);
+            const u32x4_t vf{vlo[t][i].x, vlo[t][i].y, vhi[t][i].x, vhi[t][i].y};
+            oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[t]), oacc[i], 0, 0, 0);
           }
       }
-#pragma unroll
-      for (int i = 0; i < OB; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) oacc[16 * i + e] = acc[i][e];
+      cslot = cslot == (NS - 1) * 2 * HALF ? 0 : cslot + 2 * HALF;
     }
     lsum += __shfl_xor(lsum, 32, kWave);
     if (a.nsplit == 1) {
@@ -406,7 +434,8 @@ __global__ __launch_bounds__(64 * NW) void sparse_attn_kernel(SparseArgs a) {
     } else {
       f32x4_t* img = reinterpret_cast<f32x4_t*>(a.part) + (work * NW + wave) * (OB * 4 + 1) * kWave + lane;
 #pragma unroll
-      for (int i = 0; i < OB * 4; ++i) img[i * kWave] = f32x4_t{oacc[4 * i], oacc[4 * i + 1], oacc[4 * i + 2], oacc[4 * i + 3]};
+      for (int i = 0; i < OB * 4; ++i)
+        img[i * kWave] = f32x4_t{oacc[i / 4][i % 4 * 4], oacc[i / 4][i % 4 * 4 + 1], oacc[i / 4][i % 4 * 4 + 2], oacc[i / 4][i % 4 * 4 + 3]};
       img[OB * 4 * kWave] = f32x4_t{mref, lsum, 0.f, 0.f};
     }
     __syncthreads();  // the next tile's loads overwrite the ring

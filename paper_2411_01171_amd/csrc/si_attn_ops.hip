@@ -182,7 +182,7 @@ si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int
   if (q_block < 1 || q_block > (1 << 20) || k_block < 64 || k_block > (1 << 20) || k_block % 64) return SI_ERR_SHAPE;
   p->group = (int)(q->heads / k->heads);
   if (p->group * q_block >= (1 << 24)) return SI_ERR_SHAPE;
-  if (k->N > 1 && k->stride_n >= (1LL << 40)) return SI_ERR_SHAPE;
+  if (k->N > 1 && k->stride_n >= (1 << 23)) return SI_ERR_SHAPE;  // 64 rows of keys inside 31 bits of bytes
   p->runs = (q->N + q_block - 1) / q_block;
   p->blocks = (k->N + k_block - 1) / k_block;
   p->words = (p->blocks + 31) / 32;
@@ -429,6 +429,7 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
   if (s != SI_OK) return s;
   if (v->dtype != q->dtype || out->dtype != q->dtype) return SI_ERR_DTYPE;
   if (v->B != k->B || v->N != k->N || v->heads != k->heads || v->dim_head != k->dim_head) return SI_ERR_SHAPE;
+  if (v->N > 1 && v->stride_n >= (1 << 23)) return SI_ERR_SHAPE;
   if (out->B != q->B || out->N != q->N || out->heads != q->heads || out->dim_head != q->dim_head) return SI_ERR_SHAPE;
   if (!(scale > 0.f) || !std::isfinite(scale)) return SI_ERR_ARG;
   const size_t need = p.part_bytes + 256, bits = blocks ? (size_t)(q->B * k->heads * b.runs * b.words) * 4 : 0;
