@@ -9,9 +9,8 @@
 // lane ^ 32's), so the softmax needs no cross-lane traffic in the steady state.
 //
 // Keys and values go from their own rows to LDS with direct global->LDS loads, whole rows by neighbouring lanes (full
-// cache lines), and lie there in rows of PR 16-byte pieces, piece p of row r in slot p ^ (r & 7): eight lanes that read one
-// piece of eight rows hit eight different bank groups.  bf16 values are transposed on their way out of LDS
-// (ds_read_b64_tr_b16), so nothing has to be laid out before the call.
+// cache lines), and lie there in rows of 16-byte pieces that lds_swizzle spreads over the banks.  bf16 values are transposed
+// on their way out of LDS (ds_read_b64_tr_b16), so nothing has to be laid out before the call.
 //
 // When there are few rows (single new tokens) a run's blocks are dealt out to `nsplit` workgroups; each leaves its
 // unnormalised output, maximum and sum, and sparse_join_kernel adds them in a fixed order.
@@ -146,6 +145,19 @@ template <> struct SparseShape<float> {
   static constexpr int SK = 32, VEC = 4;
 };
 
+// Piece p of row r lies in slot p ^ lds_swizzle(r) of its row.  LDS reads 256 bytes per clock.  Keys: 16 lanes read one piece of
+// 16 rows, which have to fall on 16 different groups of four banks.  bf16 values: 32 lanes read four pieces of four rows, so
+// the rows' lowest bits have to move the slot by four; float32 values: 64 lanes read eight pieces of rows that differ in
+// bit 2.  (The first form, p ^ (r & 7), lost half of the LDS's cycles to conflicts: 57600 tokens 1930 us.)
+// Every bit of the row moves bits of the slot by itself: lds_swizzle(a | b) = lds_swizzle(a) ^ lds_swizzle(b) for disjoint a, b.
+template <int ROW, bool F32>
+__device__ constexpr int lds_swizzle(int r) {
+  if (ROW == 64) return (r >> 2) & 3;
+  if (ROW == 128) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1);
+  if (F32) return (r & 3) | ((r >> 3) & 1) << 2 | ((r >> 2) & 1) << 3;
+  return (r & 3) << 2 | ((r >> 2) & 3);
+}
+
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 template <typename V> __device__ __forceinline__ V lds_read(unsigned at) {
@@ -204,7 +216,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 32, g = lane / 32;
-  auto swizzle = [](int row) { return PR == 4 ? (row >> 1) & 3 : row & 7; };
+  auto swizzle = [](int row) { return lds_swizzle<ROW, F32>(row); };
 
   // ---- what stays the same through all stages, per lane.  Load i of a half: rows (wave + NW i) (64 / PR) .., lane l takes
   // slot l % PR of row l / PR of them.
@@ -216,13 +228,14 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
     voff[i] = (unsigned)(row * (int)a.vn + piece * VEC) * (unsigned)sizeof(T);
   }
   const bool whole_rows = a.d == PR * VEC;
-  // LDS addresses of the first fragments; pieces further on are exclusive-ors (rows are aligned to their length)
+  // LDS addresses of the first fragments; pieces further on are exclusive-ors (rows are aligned to their length), and so is
+  // what a row further on changes in the slot
   const unsigned kat = lds0 + r * ROW + (g ^ swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
   // bf16: step t of 16 keys: slots e < 4 of group g are keys 16 t + 4 g + e, the others 16 t + 8 + 4 g + e - 4; channel block i: ^ 64 i
-  // f32: register (q, j) of the scores is key 8 q + 4 g + j; row 4 g + j: + j rows, ^ 16 j; channel block i: ^ 128 i
+  // f32: register (q, j) of the scores is key 8 q + 4 g + j; channel block i: ^ 128 i
   const int vr = F32 ? 4 * g : 4 * g + (lane % 16) / 4;
   const unsigned vat = lds0 + HALF + vr * ROW +
-                       (F32 ? ((r / 4) ^ vr) * 16 + (r % 4) * 4 : ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ swizzle(vr)) * 16 + (lane % 2) * 8);
+                       (F32 ? ((r / 4) ^ swizzle(vr)) * 16 + (r % 4) * 4 : ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ swizzle(vr)) * 16 + (lane % 2) * 8);
 
   // Work goes to the 8 XCDs in contiguous chunks, so that the keys and values of a head are fetched into one L2.
   const int64_t chunk = (a.work + 7) / 8;
@@ -359,7 +372,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
 #pragma unroll
           for (int i = 0; i < OB; ++i) {
             vlo[t][i] = lds_read_tr(((vat + cslot) ^ (64 * i)) + 16 * t * ROW);
-            vhi[t][i] = lds_read_tr(((vat + cslot) ^ (64 * i)) + (16 * t + 8) * ROW);
+            vhi[t][i] = lds_read_tr(((vat + cslot) ^ (64 * i) ^ (lds_swizzle<ROW, F32>(8) * 16)) + (16 * t + 8) * ROW);
           }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -416,7 +429,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < OB; ++i)
-              oacc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(lds_read<float>(((vat + cslot) ^ (16 * j + 128 * i)) + (8 * q + j) * ROW), pf[4 * q + j], oacc[i], 0, 0, 0);
+              oacc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(lds_read<float>(((vat + cslot) ^ (lds_swizzle<ROW, F32>(8 * q + j) * 16) ^ (128 * i)) + (8 * q + j) * ROW), pf[4 * q + j], oacc[i], 0, 0, 0);
       } else {
 #pragma unroll
         for (int t = 0; t < SK / 16; ++t)
