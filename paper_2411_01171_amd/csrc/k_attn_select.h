@@ -18,25 +18,32 @@ typedef double f64x4_t __attribute__((ext_vector_type(4)));
 constexpr int kMeanPieces = 32, kMeanSlices = 8;  // 16-byte pieces of a row x rows in flight of one workgroup
 constexpr int kSelectThreads = 512;
 
-struct MeansArgs {
+struct MeansOf {
   HeadsView x;
   const int* len;
   double* out;  // [B][heads_kv][runs][d]
-  int N, heads_kv, group, d, block, runs;
-  int chunks;      // of kMeanPieces pieces of a row
+  int N, group, block, runs;
   int64_t work;    // B * runs * chunks
+};
+struct MeansArgs {
+  MeansOf of[2];   // queries in runs, keys in blocks: one launch
+  int heads_kv, d;
+  int chunks;      // of kMeanPieces pieces of a row
 };
 
 template <typename T>
-__global__ __launch_bounds__(kMeanPieces* kMeanSlices) void block_means_kernel(MeansArgs a) {
+__global__ __launch_bounds__(kMeanPieces* kMeanSlices) void block_means_kernel(MeansArgs args) {
   constexpr int VEC = 16 / sizeof(T);
   __shared__ double part[kMeanSlices][kMeanPieces][VEC];
   const int px = threadIdx.x % kMeanPieces, slice = threadIdx.x / kMeanPieces;
-  const int per_head = a.d / VEC;
-  for (int64_t work = blockIdx.x; work < a.work; work += gridDim.x) {
-    const int chunk = (int)(work % a.chunks), run = (int)(work / a.chunks % a.runs), b = (int)(work / a.chunks / a.runs);
+  const int per_head = args.d / VEC;
+  for (int64_t w = blockIdx.x; w < args.of[0].work + args.of[1].work; w += gridDim.x) {
+    const bool keys = w >= args.of[0].work;
+    const MeansOf& a = args.of[keys ? 1 : 0];
+    const int64_t work = keys ? w - args.of[0].work : w;
+    const int chunk = (int)(work % args.chunks), run = (int)(work / args.chunks % a.runs), b = (int)(work / args.chunks / a.runs);
     const int item = chunk * kMeanPieces + px;
-    const bool live = item < a.heads_kv * per_head;
+    const bool live = item < args.heads_kv * per_head;
     const int hk = live ? item / per_head : 0, ch = live ? (item - hk * per_head) * VEC : 0;
     const int len = a.len ? min(max(a.len[b], 0), a.N) : a.N;
     const int64_t n0 = (int64_t)run * a.block;
@@ -70,12 +77,12 @@ __global__ __launch_bounds__(kMeanPieces* kMeanSlices) void block_means_kernel(M
     const double of = rows > 0 ? (double)((int64_t)rows * a.group) : 1.0;
     for (int e = threadIdx.x; e < kMeanPieces * VEC; e += kMeanPieces * kMeanSlices) {
       const int it = chunk * kMeanPieces + e / VEC;
-      if (it >= a.heads_kv * per_head) continue;
+      if (it >= args.heads_kv * per_head) continue;
       double s = 0.0;
 #pragma unroll
       for (int k = 0; k < kMeanSlices; ++k) s += part[k][e / VEC][e % VEC];
       const int h = it / per_head, c = (it - h * per_head) * VEC + e % VEC;
-      a.out[(((int64_t)b * a.heads_kv + h) * a.runs + run) * a.d + c] = s / of;
+      a.out[(((int64_t)b * args.heads_kv + h) * a.runs + run) * args.d + c] = s / of;
     }
     __syncthreads();
   }
@@ -99,8 +106,8 @@ __device__ __forceinline__ unsigned long long order_key(double x) {
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
-// The largest T of 32-bit words with at least `need` values >= T among those that `in` accepts, found from the top bit on:
-// stops early when exactly `need` values are >= the prefix.  Returns T, and in `above` the number of values > T ... >= T.
+// The largest T of 32-bit words with at least `need` values >= T, found from the top bit on; count(c) = number of values >= c.
+// Stops early, with `exact`, when exactly `need` values are >= the prefix.
 template <class Count>
 __device__ __forceinline__ unsigned kth_word(int need, Count count, bool& exact) {
   unsigned t = 0;
@@ -119,88 +126,120 @@ __device__ __forceinline__ unsigned kth_word(int need, Count count, bool& exact)
   return t;
 }
 
-template <int CAP>  // scores (float64) of a workgroup
+// CAP: scores (float64) of a workgroup in LDS.  KPL: keys of a run per lane in registers (64 KPL >= blocks), or 0: read from
+// LDS every time.  Counting with a ballot per key and lane beats sums over the lanes from there up to 1024 blocks; the loads of
+// a tile's means are all in flight before its products (900 blocks x 450 runs x 20 heads: 232 -> measured below).
+template <int CAP, int KPL>
 __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(SelectArgs a) {
   __shared__ unsigned long long keys[CAP];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, nw = kSelectThreads / kWave;
-  for (int64_t work = blockIdx.x; work < a.work; work += gridDim.x) {
-  const int64_t pair = work / a.tiles;  // (b, kv head)
-  const int b = (int)(pair / a.heads_kv), run0 = (int)(work - pair * a.tiles) * a.rows;
-  const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.Nk) : a.Nk;
-  const int nblk = (k_len + a.k_block - 1) / a.k_block;  // blocks with a key
+  constexpr int STEPS = 16;  // of 8 channels
+  // the tiles of one (b, kv head) on one XCD: its L2 holds their key means
+  const int64_t chunk = (a.work + 7) / 8;
+  const int64_t chunk_end = min(a.work, ((int64_t)(blockIdx.x % 8) + 1) * chunk);
+  for (int64_t work = (int64_t)(blockIdx.x % 8) * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
+    const int64_t pair = work / a.tiles;  // (b, kv head)
+    const int b = (int)(pair / a.heads_kv), run0 = (int)(work - pair * a.tiles) * a.rows;
+    const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.Nk) : a.Nk;
+    const int nblk = (k_len + a.k_block - 1) / a.k_block;  // blocks with a key
 
-  // ---- scores: 16 blocks (rows) x 16 runs (columns) per step; lane (m, g) supplies row / column m's channels 8 s + 2 g + {0, 1}
-  const int m = lane % 16, g = lane / 16;
-  const int qrow = min(run0 + min(m, a.rows - 1), a.runs - 1);
-  const double* qp = a.qm + (pair * a.runs + qrow) * a.d + 2 * g;
-  for (int j0 = wave * 16; j0 < nblk; j0 += nw * 16) {
-    const double* kp = a.km + (pair * a.blocks + min(j0 + m, a.blocks - 1)) * a.d + 2 * g;
-    f64x4_t acc{0.0, 0.0, 0.0, 0.0};
-    for (int c = 0; c < a.d; c += 8) {
-      const f64x2_t kv = *reinterpret_cast<const f64x2_t*>(kp + c), qv = *reinterpret_cast<const f64x2_t*>(qp + c);
-      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[0], qv[0], acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[1], qv[1], acc, 0, 0, 0);
-    }
-    if (m < a.rows) {
+    // ---- scores: 16 blocks (rows) x 16 runs (columns) per step; lane (m, g) supplies row / column m's channels 8 s + 2 g + {0, 1}
+    {
+      const int m = lane % 16, g = lane / 16;
+      const int qrow = min(run0 + min(m, a.rows - 1), a.runs - 1);
+      const double* qp = a.qm + (pair * a.runs + qrow) * a.d + 2 * g;
+      f64x2_t qv[STEPS];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {  // result register i: row 4 i + g
-        const int j = j0 + 4 * i + g;
-        if (j < a.pitch) keys[m * a.pitch + j] = j < nblk ? order_key(acc[i]) : 0ull;
+      for (int s = 0; s < STEPS; ++s) qv[s] = 8 * s < a.d ? *reinterpret_cast<const f64x2_t*>(qp + 8 * s) : f64x2_t{0.0, 0.0};
+      for (int j0 = wave * 16; j0 < nblk; j0 += nw * 16) {
+        const double* kp = a.km + (pair * a.blocks + min(j0 + m, a.blocks - 1)) * a.d + 2 * g;
+        f64x2_t kv[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+          if (8 * s < a.d) kv[s] = *reinterpret_cast<const f64x2_t*>(kp + 8 * s);
+        f64x4_t acc{0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+          if (8 * s < a.d) {
+            acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][0], qv[s][0], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][1], qv[s][1], acc, 0, 0, 0);
+          }
+        if (m < a.rows) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {  // result register i: row 4 i + g
+            const int j = j0 + 4 * i + g;
+            if (j < a.pitch) keys[m * a.pitch + j] = j < nblk ? order_key(acc[i]) : 0ull;
+          }
+        }
       }
     }
-  }
-  __syncthreads();
+    __syncthreads();
 
-  // ---- the `keep` largest of each run
-  for (int row = wave; row < a.rows; row += nw) {
-    const int run = run0 + row;
-    if (run >= a.runs) break;
-    unsigned* out = a.out + (pair * a.runs + run) * a.words;
-    const unsigned long long* key = keys + row * a.pitch;
-    const bool none = (int64_t)run * a.q_block >= q_len;
-    if (none || nblk <= a.keep) {  // nothing, or all
-      for (int w = lane; w < a.words; w += kWave) {
-        const int n = none ? 0 : nblk - 32 * w;
-        out[w] = n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u;
+    // ---- the `keep` largest of each run
+    for (int row = wave; row < a.rows; row += nw) {
+      const int run = run0 + row;
+      if (run >= a.runs) break;
+      unsigned* out = a.out + (pair * a.runs + run) * a.words;
+      const unsigned long long* key = keys + row * a.pitch;
+      const bool none = (int64_t)run * a.q_block >= q_len;
+      if (none || nblk <= a.keep) {  // nothing, or all
+        for (int w = lane; w < a.words; w += kWave) {
+          const int n = none ? 0 : nblk - 32 * w;
+          out[w] = n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u;
+        }
+        continue;
       }
-      continue;
-    }
-    auto tally = [&](auto pred) {
-      int n = 0;
-      for (int j = lane; j < nblk; j += kWave) n += pred(key[j]) ? 1 : 0;
+      unsigned long long held[KPL ? KPL : 1];
+      if constexpr (KPL > 0) {
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
-      return __builtin_amdgcn_readfirstlane(n);
-    };
-    bool exact;
-    const unsigned hi = kth_word(a.keep, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); }, exact);
-    unsigned long long least = (unsigned long long)hi << 32;  // everything >= least is kept, except some of the equal ones
-    int need_equal = 0;  // of the values == least, when not exact
-    if (!exact) {
-      const int above = tally([&](unsigned long long k) { return (unsigned)(k >> 32) > hi; });
-      const int need = a.keep - above;
-      const unsigned lo = kth_word(
-          need, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) == hi && (unsigned)k >= c; }); }, exact);
-      least |= lo;
-      if (!exact) need_equal = a.keep - tally([&](unsigned long long k) { return k > least; });
-    }
-    int equal = 0;
-    for (int j0 = 0; j0 < 32 * a.words; j0 += kWave) {
-      const int j = j0 + lane;
-      const unsigned long long k = j < nblk ? key[j] : 0ull;
-      bool take = j < nblk && (exact ? k >= least : k > least);
+        for (int i = 0; i < KPL; ++i) held[i] = i * kWave + lane < nblk ? key[i * kWave + lane] : 0ull;  // 0: below every score
+      }
+      auto tally = [&](auto pred) {
+        int n = 0;
+        if constexpr (KPL > 0) {
+#pragma unroll
+          for (int i = 0; i < KPL; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(pred(held[i])));
+        } else {
+          for (int j = lane; j < nblk; j += kWave) n += pred(key[j]) ? 1 : 0;
+#pragma unroll
+          for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
+          n = __builtin_amdgcn_readfirstlane(n);
+        }
+        return n;
+      };
+      bool exact;
+      const unsigned hi = kth_word(a.keep, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); }, exact);
+      unsigned long long least = (unsigned long long)hi << 32;  // everything >= least is kept, except some of the equal ones
+      int need_equal = 0;  // of the values == least, when not exact
       if (!exact) {
-        const bool eq = j < nblk && k == least;
-        const unsigned long long eqs = __builtin_amdgcn_ballot_w64(eq);
-        const int rank = equal + __popcll(eqs & ((1ull << lane) - 1ull));
-        take = take || (eq && rank < need_equal);
-        equal += __popcll(eqs);
+        const int above = tally([&](unsigned long long k) { return (unsigned)(k >> 32) > hi; });
+        const unsigned lo = kth_word(
+            a.keep - above,
+            [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) == hi && (unsigned)k >= c; }); }, exact);
+        least |= lo;
+        if (!exact) need_equal = a.keep - tally([&](unsigned long long k) { return k > least; });
       }
-      const unsigned long long bits = __builtin_amdgcn_ballot_w64(take);
-      if (lane < 2 && j0 / 32 + lane < a.words) out[j0 / 32 + lane] = (unsigned)(bits >> (32 * lane));
+      int equal = 0;
+      auto put = [&](int j0, unsigned long long k) {
+        bool take = exact ? k >= least : k > least;
+        if (!exact) {
+          const unsigned long long eqs = __builtin_amdgcn_ballot_w64(k == least);
+          const int rank = equal + __popcll(eqs & ((1ull << lane) - 1ull));
+          take = take || (k == least && rank < need_equal);
+          equal += __popcll(eqs);
+        }
+        const unsigned long long bits = __builtin_amdgcn_ballot_w64(take);
+        if (lane < 2 && j0 / 32 + lane < a.words) out[j0 / 32 + lane] = (unsigned)(bits >> (32 * lane));
+      };
+      if constexpr (KPL > 0) {
+#pragma unroll
+        for (int i = 0; i < KPL; ++i)
+          if (2 * i < a.words) put(i * kWave, held[i]);
+      } else {
+        for (int j0 = 0; j0 < 32 * a.words; j0 += kWave) put(j0, j0 + lane < nblk ? key[j0 + lane] : 0ull);
+      }
     }
-  }
-  __syncthreads();
+    __syncthreads();
   }
 }
 

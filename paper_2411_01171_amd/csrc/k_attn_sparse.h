@@ -444,7 +444,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
     lsum += __shfl_xor(lsum, 32, kWave);
     if (a.nsplit == 1) {
       sparse_store<T, OB>(a, oacc, lsum, b, hk, token, sub, valid, g);
-    } else {
+    } else if (valid) {  // rows that hold no query are not read back either
       f32x4_t* img = reinterpret_cast<f32x4_t*>(a.part) + (work * NW + wave) * (OB * 4 + 1) * kWave + lane;
 #pragma unroll
       for (int i = 0; i < OB * 4; ++i)

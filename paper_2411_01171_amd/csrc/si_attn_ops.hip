@@ -200,26 +200,8 @@ size_t select_bytes(const si_heads* q, const si_heads* k, const BlocksPlan& p) {
          align_up((size_t)(q->B * k->heads * p.blocks * q->dim_head) * sizeof(double), 256);
 }
 
-static si_status enqueue_means(const si_heads* x, int64_t heads_kv, int64_t block, int64_t runs, const int32_t* len, double* out, hipStream_t st) {
-  MeansArgs a;
-  a.x = view_of(x);
-  a.len = len;
-  a.out = out;
-  a.N = (int)x->N;
-  a.heads_kv = (int)heads_kv;
-  a.group = (int)(x->heads / heads_kv);
-  a.d = (int)x->dim_head;
-  a.block = (int)block;
-  a.runs = (int)runs;
-  const int64_t pieces = heads_kv * x->dim_head * heads_esize(x) / 16;
-  a.chunks = (int)((pieces + kMeanPieces - 1) / kMeanPieces);
-  a.work = x->B * runs * a.chunks;
-  if (a.work == 0) return SI_OK;
-  const unsigned grid = (unsigned)std::min<int64_t>(a.work, kGridMost);
-  if (x->dtype == SI_F32) block_means_kernel<float><<<grid, kMeanPieces * kMeanSlices, 0, st>>>(a);
-  else block_means_kernel<bf16><<<grid, kMeanPieces * kMeanSlices, 0, st>>>(a);
-  SI_CHECK_LAUNCH();
-  return SI_OK;
+static MeansOf means_of(const si_heads* x, int64_t heads_kv, int64_t block, int64_t runs, int64_t chunks, const int32_t* len, double* out) {
+  return MeansOf{view_of(x), len, out, (int)x->N, (int)(x->heads / heads_kv), (int)block, (int)runs, x->B * runs * chunks};
 }
 
 si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan& p, int64_t q_block, int64_t k_block, int64_t keep,
@@ -228,9 +210,16 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
   StageScope scope("attn_select", st);
   double* qm = reinterpret_cast<double*>(ws);
   double* km = reinterpret_cast<double*>(ws + align_up((size_t)(q->B * k->heads * p.runs * q->dim_head) * sizeof(double), 256));
-  si_status s = enqueue_means(q, k->heads, q_block, p.runs, q_len, qm, st);
-  if (s == SI_OK) s = enqueue_means(k, k->heads, k_block, p.blocks, k_len, km, st);
-  if (s != SI_OK) return s;
+  MeansArgs m;
+  m.heads_kv = (int)k->heads;
+  m.d = (int)q->dim_head;
+  m.chunks = (int)((k->heads * q->dim_head * heads_esize(q) / 16 + kMeanPieces - 1) / kMeanPieces);
+  m.of[0] = means_of(q, k->heads, q_block, p.runs, m.chunks, q_len, qm);
+  m.of[1] = means_of(k, k->heads, k_block, p.blocks, m.chunks, k_len, km);
+  const unsigned grid = (unsigned)std::min<int64_t>(m.of[0].work + m.of[1].work, kGridMost);
+  if (q->dtype == SI_F32) block_means_kernel<float><<<grid, kMeanPieces * kMeanSlices, 0, st>>>(m);
+  else block_means_kernel<bf16><<<grid, kMeanPieces * kMeanSlices, 0, st>>>(m);
+  SI_CHECK_LAUNCH();
   SelectArgs a;
   a.qm = qm; a.km = km; a.out = blocks;
   a.q_len = q_len; a.k_len = k_len;
@@ -240,17 +229,20 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
   a.runs = (int)p.runs; a.blocks = (int)p.blocks; a.words = (int)p.words;
   a.keep = (int)std::min<int64_t>(keep, p.blocks);
   a.pitch = (int)((p.blocks + 15) / 16 * 16 + 2);
-  auto launch = [&](auto cap) {
+  auto launch = [&](auto cap, auto kpl) {
     a.rows = std::min(16, cap.value / a.pitch);
     a.tiles = (int)((p.runs + a.rows - 1) / a.rows);
     a.work = q->B * k->heads * a.tiles;
-    block_select_kernel<cap.value><<<(unsigned)std::min<int64_t>(a.work, kGridMost), kSelectThreads, 0, st>>>(a);
+    block_select_kernel<cap.value, kpl.value><<<(unsigned)((std::min<int64_t>(a.work, kGridMost) + 7) / 8 * 8), kSelectThreads, 0, st>>>(a);
   };
   // the smallest store of scores that holds 16 runs, for as many workgroups on a CU as possible
-  if (a.pitch <= 130) launch(std::integral_constant<int, 16 * 130>());
-  else if (a.pitch <= 258) launch(std::integral_constant<int, 16 * 258>());
-  else if (a.pitch <= 514) launch(std::integral_constant<int, 16 * 514>());
-  else launch(std::integral_constant<int, 16 * 1028>());
+  using std::integral_constant;
+  if (p.blocks <= 64) launch(integral_constant<int, 16 * 66>(), integral_constant<int, 1>());
+  else if (p.blocks <= 128) launch(integral_constant<int, 16 * 130>(), integral_constant<int, 2>());
+  else if (p.blocks <= 256) launch(integral_constant<int, 16 * 258>(), integral_constant<int, 4>());
+  else if (p.blocks <= 512) launch(integral_constant<int, 16 * 514>(), integral_constant<int, 8>());
+  else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>());
+  else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>());
   static_assert(16 * 1028 >= kSelectMaxBlocks + 2, "one run of the longest list");
   SI_CHECK_LAUNCH();
   return SI_OK;
