@@ -16,7 +16,6 @@ typedef double f64x2_t __attribute__((ext_vector_type(2)));
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kMeanPieces = 32, kMeanSlices = 8;  // 16-byte pieces of a row x rows in flight of one workgroup
-constexpr int kSelectThreads = 512;
 
 struct MeansOf {
   HeadsView x;
@@ -129,11 +128,11 @@ __device__ __forceinline__ unsigned kth_word(int need, Count count, bool& exact)
 // CAP: scores (float64) of a workgroup in LDS.  KPL: keys of a run per lane in registers (64 KPL >= blocks), or 0: read from
 // LDS every time.  Counting with a ballot per key and lane beats sums over the lanes from there up to 1024 blocks; the loads of
 // a tile's means are all in flight before its products (900 blocks x 450 runs x 20 heads: 232 -> measured below).
-template <int CAP, int KPL>
-__global__ __launch_bounds__(kSelectThreads) void block_select_kernel(SelectArgs a) {
+template <int CAP, int KPL, int NT>
+__global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
   __shared__ unsigned long long keys[CAP];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, nw = kSelectThreads / kWave;
-  constexpr int STEPS = 16;  // of 8 channels
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  constexpr int nw = NT / kWave, STEPS = 8;  // steps of 8 channels whose loads are in flight together
   // the tiles of one (b, kv head) on one XCD: its L2 holds their key means
   const int64_t chunk = (a.work + 7) / 8;
   const int64_t chunk_end = min(a.work, ((int64_t)(blockIdx.x % 8) + 1) * chunk);
@@ -148,22 +147,24 @@ __global__ __launch_bounds__(kSelectThreads) void block_select_kernel(SelectArgs
       const int m = lane % 16, g = lane / 16;
       const int qrow = min(run0 + min(m, a.rows - 1), a.runs - 1);
       const double* qp = a.qm + (pair * a.runs + qrow) * a.d + 2 * g;
-      f64x2_t qv[STEPS];
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) qv[s] = 8 * s < a.d ? *reinterpret_cast<const f64x2_t*>(qp + 8 * s) : f64x2_t{0.0, 0.0};
       for (int j0 = wave * 16; j0 < nblk; j0 += nw * 16) {
         const double* kp = a.km + (pair * a.blocks + min(j0 + m, a.blocks - 1)) * a.d + 2 * g;
-        f64x2_t kv[STEPS];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-          if (8 * s < a.d) kv[s] = *reinterpret_cast<const f64x2_t*>(kp + 8 * s);
         f64x4_t acc{0.0, 0.0, 0.0, 0.0};
+        for (int c = 0; c < a.d; c += 8 * STEPS) {
+          f64x2_t kv[STEPS], qv[STEPS];
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-          if (8 * s < a.d) {
-            acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][0], qv[s][0], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][1], qv[s][1], acc, 0, 0, 0);
-          }
+          for (int s = 0; s < STEPS; ++s)
+            if (c + 8 * s < a.d) {
+              kv[s] = *reinterpret_cast<const f64x2_t*>(kp + c + 8 * s);
+              qv[s] = *reinterpret_cast<const f64x2_t*>(qp + c + 8 * s);
+            }
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s)
+            if (c + 8 * s < a.d) {
+              acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][0], qv[s][0], acc, 0, 0, 0);
+              acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][1], qv[s][1], acc, 0, 0, 0);
+            }
+        }
         if (m < a.rows) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {  // result register i: row 4 i + g

@@ -1,12 +1,12 @@
 // Attention of runs of queries over listed key blocks.
 //
 // A run is q_block consecutive queries of the `group` heads that share a key / value head: group * q_block rows, one list of
-// key blocks (a bitmap).  One workgroup takes NW x 32 rows of a run and walks the run's blocks, a stage of kStageKeys keys at
-// a time, with the running maximum and sum of a softmax:
-//   S^T[key, row] = K Q^T       row operand: 32 keys, column operand: 32 rows (one wavefront's)
+// key blocks (a bitmap).  One workgroup takes NW x 32 rows of a run and walks the run's blocks, a stage of 64 (float32: 32)
+// keys at a time, with the running maximum and sum of a softmax:
+//   S^T[key, row] = K Q^T       row operand: keys, column operand: rows
 //   O^T[chan, row] += V^T P^T   column operand: the softmax result registers as they stand
-// With queries as columns a lane holds 16 scores of one query, its running maximum and its half of the sum (the other half is
-// lane ^ 32's), so the softmax needs no cross-lane traffic in the steady state.
+// With queries as columns a lane holds scores of one query (float32: two), its running maximum and its part of the sum, so
+// the softmax needs no cross-lane traffic in the steady state.
 //
 // Keys and values go from their own rows to LDS with direct global->LDS loads, whole rows by neighbouring lanes (full
 // cache lines), and lie there in rows of 16-byte pieces that lds_swizzle spreads over the banks.  bf16 values are transposed
@@ -31,7 +31,8 @@ struct SparseArgs {
   int64_t work;              // B * heads_kv * runs * tiles_per_run * nsplit
   int nsplit;
   float c;                   // softmax scale * log2(e)
-  float* part;               // nsplit > 1: [work][wave][OB * 4 + 1][64] of 16 bytes
+  float* part;               // nsplit > 1: outputs [query row][nsplit][d], then (maximum, sum) [query row][nsplit]; query row = (b Nq + n) heads + h
+  float2* part_ml;
   int o_frag;                // 0, or o is a fragment-order buffer of that many channels per token
 };
 
@@ -137,26 +138,31 @@ struct BlockWalk {
   }
 };
 
-template <typename T> struct SparseShape;
-template <> struct SparseShape<bf16> {
-  static constexpr int SK = 64, VEC = 8;  // keys of a stage, elements of a 16-byte piece
-};
-template <> struct SparseShape<float> {
-  static constexpr int SK = 32, VEC = 4;
-};
+// What all kernels share: where a head's rows lie in LDS.
+template <typename T, int KS>
+struct SparseGeo {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int SK = F32 ? 32 : 64;                            // keys of a stage
+  static constexpr int VEC = 16 / sizeof(T);                          // elements of a 16-byte piece
+  static constexpr int NP = KS * 16 / VEC;                            // pieces of a padded head
+  static constexpr int PR = NP <= 4 ? 4 : NP <= 8 ? 8 : NP <= 16 ? 16 : 32;  // pieces of a row in LDS
+  static constexpr int ROW = PR * 16;                                 // bytes
+  static constexpr int HALF = SK * ROW;                               // bytes of a stage's keys; its values follow
+  static constexpr int NS = !F32 && HALF <= 8192 ? 3 : 2;             // stages in LDS
+  static constexpr int LOADS = HALF / 1024;                           // wave-wide loads of a stage's keys
 
-// Piece p of row r lies in slot p ^ lds_swizzle(r) of its row.  LDS reads 256 bytes per clock.  Keys: 16 lanes read one piece of
-// 16 rows, which have to fall on 16 different groups of four banks.  bf16 values: 32 lanes read four pieces of four rows, so
-// the rows' lowest bits have to move the slot by four; float32 values: 64 lanes read eight pieces of rows that differ in
-// bit 2.  (The first form, p ^ (r & 7), lost half of the LDS's cycles to conflicts: 57600 tokens 1930 us.)
-// Every bit of the row moves bits of the slot by itself: lds_swizzle(a | b) = lds_swizzle(a) ^ lds_swizzle(b) for disjoint a, b.
-template <int ROW, bool F32>
-__device__ constexpr int lds_swizzle(int r) {
-  if (ROW == 64) return (r >> 2) & 3;
-  if (ROW == 128) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1);
-  if (F32) return (r & 3) | ((r >> 3) & 1) << 2 | ((r >> 2) & 1) << 3;
-  return (r & 3) << 2 | ((r >> 2) & 3);
-}
+  // Piece p of row r lies in slot p ^ swizzle(r) of its row.  LDS reads 256 bytes per clock.  Keys: the lanes of a clock read
+  // one piece of 16 rows, which have to fall on 16 different groups of four banks.  Values: they read the pieces of 32 (bf16)
+  // or 16 (float32) channels of four rows, which differ in bits 0 and 1 (bf16) or 2 and 3 (float32): those bits have to move
+  // the slot by four.  (p ^ (r & 7) lost half of the LDS's cycles to conflicts: heads of 128, padded batch, 429 us against 388.)
+  // Every bit of the row moves bits of the slot by itself: swizzle(a | b) = swizzle(a) ^ swizzle(b) for disjoint a and b.
+  static __host__ __device__ constexpr int swizzle(int r) {
+    return ROW == 64 ? (r >> 2) & 3
+           : ROW == 128 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1)
+           : F32 ? r & 15
+                 : (r & 3) << 2 | ((r >> 2) & 3);
+  }
+};
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
@@ -169,145 +175,182 @@ __device__ __forceinline__ uint2 lds_read_tr(unsigned at) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4_t*>((size_t)at)));
 }
 
-// Output of one wavefront: lane (r, g) holds query row r's channels 32 b + 8 q + 4 g + j in register 16 b + 4 q + j.
-template <typename T, int OB>
-__device__ __forceinline__ void sparse_store(const SparseArgs& a, const f32x16_t (&o)[OB], float lsum, int b, int hk, int token, int sub,
-                                             bool valid, int g) {
-  if (!valid) return;
-  const float inv = lsum > 0.f ? 1.f / lsum : 0.f;  // a row without keys gives zero
-  const int h = hk * a.group + sub;
-  T* row = static_cast<T*>(a.o) + b * a.ob + (int64_t)token * a.on + (int64_t)h * a.oh;
+// One row tile of a run, or a share of its blocks.
+struct SparseTile {
+  int part, tile, run, hk, b, q_len, k_len;
+  __device__ __forceinline__ SparseTile(const SparseArgs& a, int64_t work) {
+    part = (int)(work % a.nsplit);
+    int64_t at = work / a.nsplit;
+    tile = (int)(at % a.tiles_per_run);
+    at /= a.tiles_per_run;
+    run = (int)(at % a.runs);
+    at /= a.runs;
+    hk = (int)(at % a.heads_kv);
+    b = (int)(at / a.heads_kv);
+    q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq;
+    k_len = a.k_len ? min(max(a.k_len[b], 0), a.Nk) : a.Nk;
+  }
+  // token of row `rho` of the run, or -1; sub: its head among those of the key head
+  __device__ __forceinline__ int token(const SparseArgs& a, int rho, int& sub) const {
+    const int in_run = rho / a.group;
+    const int64_t n = (int64_t)run * a.q_block + in_run;
+    sub = rho - in_run * a.group;
+    return in_run < a.q_block && n < q_len ? (int)n : -1;
+  }
+  template <int SK>
+  __device__ __forceinline__ void begin(const SparseArgs& a, int rows, BlockWalk<SK>& walk) const {
+    const unsigned* list = a.mask ? a.mask + (((int64_t)b * a.heads_kv + hk) * a.runs + run) * a.words : nullptr;
+    int sub;
+    const bool any = token(a, tile * rows, sub) >= 0;  // the tile's first row is its earliest token; without one it walks nothing
+    walk.begin(list, any ? a.words : 0, (k_len + a.k_block - 1) / a.k_block, a.k_block, k_len, part, a.nsplit);
+  }
+};
+
+// The stages of a workgroup's list on their way to LDS, by direct global->LDS loads in assembly: their completion is awaited
+// explicitly, the compiler would wait for all of them before the next LDS read.
+template <typename T, int KS, int NW>
+struct StageLoads {
+  using G = SparseGeo<T, KS>;
+  static constexpr int PER = G::LOADS / NW;  // loads of a stage's keys per wavefront, and of its values
+  static_assert(G::LOADS % NW == 0, "every wavefront issues the same number of loads, the waits count them");
+  unsigned lds0, slot;
+  int lane, wave;
+  bool whole_rows;
+  unsigned koff[PER], voff[PER];  // load i: rows (wave + NW i) (64 / PR) .., lane l takes slot l % PR of row l / PR of them
+  const char *kbase, *vbase;
+  int issued, last_keys;
+
+  __device__ __forceinline__ void setup(const SparseArgs& a, unsigned at) {
+    lds0 = at;
+    lane = threadIdx.x % kWave;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    whole_rows = a.d == G::PR * G::VEC;
 #pragma unroll
-  for (int i = 0; i < OB; ++i)
+    for (int i = 0; i < PER; ++i) {
+      const int row = (wave + NW * i) * (64 / G::PR) + lane / G::PR, piece = (lane % G::PR) ^ G::swizzle(row);
+      koff[i] = (unsigned)(row * (int)a.kn + piece * G::VEC) * (unsigned)sizeof(T);  // the host keeps this inside 31 bits
+      voff[i] = (unsigned)(row * (int)a.vn + piece * G::VEC) * (unsigned)sizeof(T);
+    }
+  }
+  __device__ __forceinline__ void begin(const SparseArgs& a, const SparseTile& t) {
+    kbase = static_cast<const char*>(a.k) + ((int64_t)t.b * a.kb + (int64_t)t.hk * a.kh) * (int64_t)sizeof(T);
+    vbase = static_cast<const char*>(a.v) + ((int64_t)t.b * a.vb + (int64_t)t.hk * a.vh) * (int64_t)sizeof(T);
+    issued = 0;
+    last_keys = G::SK;
+    slot = 0;
+  }
+  __device__ __forceinline__ void issue(const SparseArgs& a, BlockWalk<G::SK>& walk) {
+    const int key0 = walk.next();
+    if (key0 < 0) return;
+    const int nkeys = min(G::SK, walk.k_len - key0);
+    last_keys = nkeys;
+    const char* ksrc = kbase + (int64_t)key0 * a.kn * (int64_t)sizeof(T);
+    const char* vsrc = vbase + (int64_t)key0 * a.vn * (int64_t)sizeof(T);
+    const unsigned dst = lds0 + slot + wave * 1024;
+    if (nkeys == G::SK && whole_rows) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int ch = 32 * i + 8 * q + 4 * g;
-      if (ch >= a.d) continue;
-      float y[4];
+      for (int i = 0; i < PER; ++i) {
+        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(koff[i]), "s"(ksrc), "s"(dst + NW * i * 1024) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff[i]), "s"(vsrc), "s"(dst + G::HALF + NW * i * 1024) : "memory");
+      }
+    } else {  // keys past the end and channels past the head as zeros
+      int l = lane;
+      asm volatile("" : "+v"(l));  // rows and pieces are formed here again: kept through the loop they cost registers
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = lsum > 0.f ? o[i][4 * q + j] * inv : 0.f;
-      if constexpr (sizeof(T) == 2) {
-        bf16* dst = a.o_frag ? static_cast<bf16*>(a.o) + act_offset((int64_t)b * a.Nq + token, h * a.d + ch, a.o_frag)
-                             : reinterpret_cast<bf16*>(row) + ch;
-        *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
-      } else {
-        *reinterpret_cast<f32x4_t*>(row + ch) = f32x4_t{y[0], y[1], y[2], y[3]};
+      for (int i = 0; i < PER; ++i) {
+        const int row = (wave + NW * i) * (64 / G::PR) + l / G::PR, piece = (l % G::PR) ^ G::swizzle(row);
+        const bool in = piece * G::VEC < a.d && row < nkeys;
+        const char* ks = in ? ksrc + koff[i] : reinterpret_cast<const char*>(kSparseZero);
+        const char* vs = in ? vsrc + voff[i] : reinterpret_cast<const char*>(kSparseZero);
+        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ks), "s"(dst + NW * i * 1024) : "memory");
+        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(vs), "s"(dst + G::HALF + NW * i * 1024) : "memory");
       }
     }
+    slot = slot == (G::NS - 1) * 2 * G::HALF ? 0 : slot + 2 * G::HALF;
+    ++issued;
+  }
+  // Stage st is there for all, and nobody reads the slot that is filled next; returns its keys.
+  __device__ __forceinline__ int open(const SparseArgs& a, BlockWalk<G::SK>& walk, int st) {
+    const int younger = issued - 1 - st;  // stages in flight behind this one: at most NS - 2
+    if (G::NS == 3 && younger >= 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * PER));
+    else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __syncthreads();
+    issue(a, walk);
+    return st + 1 == issued ? last_keys : G::SK;  // only the list's last stage can hold fewer
+  }
+};
+
+// Four channels of a query row: the result, or (nsplit > 1) its share.
+template <typename T>
+__device__ __forceinline__ void sparse_put(const SparseArgs& a, const SparseTile& t, int token, int sub, int ch, f32x4_t o, float lsum) {
+  const int h = t.hk * a.group + sub;
+  if (a.nsplit > 1) {
+    const int64_t share = (((int64_t)t.b * a.Nq + token) * (a.heads_kv * a.group) + h) * a.nsplit + t.part;
+    *reinterpret_cast<f32x4_t*>(a.part + share * a.d + ch) = o;
+    return;
+  }
+  const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = lsum > 0.f ? o[j] * inv : 0.f;  // a row without keys gives zero
+  T* dst = static_cast<T*>(a.o) + t.b * a.ob + (int64_t)token * a.on + (int64_t)h * a.oh + ch;
+  if constexpr (sizeof(T) == 2) {
+    if (a.o_frag) dst = static_cast<T*>(a.o) + act_offset((int64_t)t.b * a.Nq + token, h * a.d + ch, a.o_frag);
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+  } else {
+    *reinterpret_cast<f32x4_t*>(dst) = o;
+  }
+}
+__device__ __forceinline__ void sparse_put_ml(const SparseArgs& a, const SparseTile& t, int token, int sub, float m, float l) {
+  const int64_t share = (((int64_t)t.b * a.Nq + token) * (a.heads_kv * a.group) + t.hk * a.group + sub) * a.nsplit + t.part;
+  a.part_ml[share] = make_float2(m, l);
 }
 
-// KS: head channels in steps of 16 (d <= 16 KS).
-template <typename T, int KS, int NW>
-__global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3 : 2) void sparse_attn_kernel(SparseArgs a) {
-  using Shape = SparseShape<T>;
-  constexpr bool F32 = sizeof(T) == 4;
-  constexpr int SK = Shape::SK, VEC = Shape::VEC;
-  constexpr int NP = KS * 16 / VEC;                               // 16-byte pieces of a padded head
-  constexpr int PR = NP <= 4 ? 4 : NP <= 8 ? 8 : NP <= 16 ? 16 : 32;  // pieces of a row in LDS
-  constexpr int ROW = PR * 16;                                    // bytes
-  constexpr int OB = (KS + 1) / 2;                                // 32-channel blocks of the output
-  constexpr int HALF = SK * ROW;                                  // bytes of a stage's keys; its values follow
-  constexpr int NS = HALF <= 8192 ? 3 : 2;                        // stages in LDS
-  constexpr int LOADS = HALF / 1024;                              // wave-wide loads of a stage's keys
-  constexpr int PER = LOADS / NW;                                 // per wavefront
-  constexpr int QS = F32 ? KS * 2 : KS;                           // pieces of a query per lane
-  static_assert(LOADS % NW == 0, "every wavefront issues the same number of loads, the waits count them");
-  __shared__ __align__(1024) u32x4_t ring[NS * 2 * HALF / 16];
+// bf16.  KS: head channels in steps of 16 (d <= 16 KS).  v_mfma_f32_32x32x16_bf16: a wavefront's 32 rows are its columns; a
+// result lane (r, g) holds column r and, in register 4 q + j, row 8 q + 4 g + j.
+//
+// Bound by the vector ALUs and the matrix cores together: per 32 rows x 64 keys and head of 64, 512 clocks of MFMA and, beside
+// them, 32 exponentials (8 clocks each), 32 fma (the scale stays in float32: folded into q before a second rounding of q it
+// would save 4 % at 57600 tokens), 16 conversions and 16 sums of pairs; and by power: in long launches the clock falls to
+// 1.9 GHz.  72x128 frame over a quarter of its keys 70 us (780 TFLOP/s), 57600 tokens over a tenth 1906 us (890).  Three
+// workgroups on a CU (two for wide heads) hide each other's waits; s_setprio around either half changes nothing.
+template <int KS, int NW>
+__global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_attn_bf16_kernel(SparseArgs a) {
+  using G = SparseGeo<bf16, KS>;
+  constexpr int SK = G::SK, ROW = G::ROW;
+  constexpr int OB = (KS + 1) / 2;  // 32-channel blocks of the output
+  __shared__ __align__(1024) u32x4_t ring[G::NS * 2 * G::HALF / 16];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int r = lane % 32, g = lane / 32;
-  auto swizzle = [](int row) { return lds_swizzle<ROW, F32>(row); };
-
-  // ---- what stays the same through all stages, per lane.  Load i of a half: rows (wave + NW i) (64 / PR) .., lane l takes
-  // slot l % PR of row l / PR of them.
-  unsigned koff[PER], voff[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int row = (wave + NW * i) * (64 / PR) + lane / PR, piece = (lane % PR) ^ swizzle(row);
-    koff[i] = (unsigned)(row * (int)a.kn + piece * VEC) * (unsigned)sizeof(T);  // the host keeps this inside 31 bits
-    voff[i] = (unsigned)(row * (int)a.vn + piece * VEC) * (unsigned)sizeof(T);
-  }
-  const bool whole_rows = a.d == PR * VEC;
+  StageLoads<bf16, KS, NW> loads;
+  loads.setup(a, lds0);
+  const int lane = loads.lane, r = lane % 32, g = lane / 32;
   // LDS addresses of the first fragments; pieces further on are exclusive-ors (rows are aligned to their length), and so is
   // what a row further on changes in the slot
-  const unsigned kat = lds0 + r * ROW + (g ^ swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
-  // bf16: step t of 16 keys: slots e < 4 of group g are keys 16 t + 4 g + e, the others 16 t + 8 + 4 g + e - 4; channel block i: ^ 64 i
-  // f32: register (q, j) of the scores is key 8 q + 4 g + j; channel block i: ^ 128 i
-  const int vr = F32 ? 4 * g : 4 * g + (lane % 16) / 4;
-  const unsigned vat = lds0 + HALF + vr * ROW +
-                       (F32 ? ((r / 4) ^ swizzle(vr)) * 16 + (r % 4) * 4 : ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ swizzle(vr)) * 16 + (lane % 2) * 8);
+  const unsigned kat = lds0 + r * ROW + (g ^ G::swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
+  // step t of 16 keys: slots e < 4 of group g are keys 16 t + 4 g + e, the others 16 t + 8 + 4 g + e - 4; channel block i: ^ 64 i
+  const int vr = 4 * g + (lane % 16) / 4;
+  const unsigned vat = lds0 + G::HALF + vr * ROW + ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ G::swizzle(vr)) * 16 + (lane % 2) * 8;
 
   // Work goes to the 8 XCDs in contiguous chunks, so that the keys and values of a head are fetched into one L2.
   const int64_t chunk = (a.work + 7) / 8;
   const int64_t chunk_end = min(a.work, ((int64_t)(blockIdx.x % 8) + 1) * chunk);
   for (int64_t work = (int64_t)(blockIdx.x % 8) * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
-    const int part = (int)(work % a.nsplit);
-    int64_t at = work / a.nsplit;
-    const int tile = (int)(at % a.tiles_per_run);
-    at /= a.tiles_per_run;
-    const int run = (int)(at % a.runs);
-    at /= a.runs;
-    const int hk = (int)(at % a.heads_kv), b = (int)(at / a.heads_kv);
-    const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.Nk) : a.Nk;
-    // this lane's query row
-    const int rho = (tile * NW + wave) * 32 + r, in_run = rho / a.group, sub = rho - in_run * a.group;
-    const int64_t token64 = (int64_t)run * a.q_block + in_run;
-    const bool valid = in_run < a.q_block && token64 < q_len;
-    const int token = valid ? (int)token64 : 0;
-
+    const SparseTile t(a, work);
+    int sub;
+    const int token = t.token(a, (t.tile * NW + loads.wave) * 32 + r, sub);  // this lane's query row
     BlockWalk<SK> walk;
-    const unsigned* mrow = a.mask ? a.mask + (((int64_t)b * a.heads_kv + hk) * a.runs + run) * a.words : nullptr;
-    // a tile without a query walks nothing (the first row of the tile is its earliest token)
-    const int first_row = tile * NW * 32, first_tok = first_row / a.group;
-    const bool any = first_tok < a.q_block && (int64_t)run * a.q_block + first_tok < q_len;
-    walk.begin(mrow, any ? a.words : 0, (k_len + a.k_block - 1) / a.k_block, a.k_block, k_len, part, a.nsplit);
-
-    const char* const kbase = static_cast<const char*>(a.k) + ((int64_t)b * a.kb + (int64_t)hk * a.kh) * (int64_t)sizeof(T);
-    const char* const vbase = static_cast<const char*>(a.v) + ((int64_t)b * a.vb + (int64_t)hk * a.vh) * (int64_t)sizeof(T);
-    int issued = 0, last_keys = SK;
-    unsigned islot = 0;
-    // assembly: completion is awaited explicitly, the compiler would wait for all of it before the next LDS read
-    auto issue = [&]() {
-      const int key0 = walk.next();
-      if (key0 < 0) return;
-      const int nkeys = min(SK, k_len - key0);
-      last_keys = nkeys;
-      const char* ksrc = kbase + (int64_t)key0 * a.kn * (int64_t)sizeof(T);
-      const char* vsrc = vbase + (int64_t)key0 * a.vn * (int64_t)sizeof(T);
-      const unsigned dst = lds0 + islot + wave * 1024;
-      if (nkeys == SK && whole_rows) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(koff[i]), "s"(ksrc), "s"(dst + NW * i * 1024) : "memory");
-          asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff[i]), "s"(vsrc), "s"(dst + HALF + NW * i * 1024) : "memory");
-        }
-      } else {  // keys past the end and channels past the head as zeros
-        int l = lane;
-        asm volatile("" : "+v"(l));  // rows and pieces are formed here again: kept through the loop they cost registers
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int row = (wave + NW * i) * (64 / PR) + l / PR, piece = (l % PR) ^ swizzle(row);
-          const bool in = piece * VEC < a.d && row < nkeys;
-          const char* ks = in ? ksrc + koff[i] : reinterpret_cast<const char*>(kSparseZero);
-          const char* vs = in ? vsrc + voff[i] : reinterpret_cast<const char*>(kSparseZero);
-          asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ks), "s"(dst + NW * i * 1024) : "memory");
-          asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(vs), "s"(dst + HALF + NW * i * 1024) : "memory");
-        }
-      }
-      islot = islot == (NS - 1) * 2 * HALF ? 0 : islot + 2 * HALF;
-      ++issued;
-    };
-    for (int i = 0; i < NS - 1; ++i) issue();
+    t.begin(a, NW * 32, walk);
+    loads.begin(a, t);
+    for (int i = 0; i < G::NS - 1; ++i) loads.issue(a, walk);
 
     // ---- this lane's query as column operand: pieces as the keys' fragments have them
-    u32x4_t qop[QS];
+    u32x4_t qop[KS];
     {
-      const T* qrow = static_cast<const T*>(a.q) + b * a.qb + (int64_t)token * a.qn + (int64_t)(hk * a.group + (valid ? sub : 0)) * a.qh;
+      const bf16* qrow = static_cast<const bf16*>(a.q) + t.b * a.qb + (int64_t)max(token, 0) * a.qn + (int64_t)(t.hk * a.group + (token < 0 ? 0 : sub)) * a.qh;
 #pragma unroll
-      for (int s = 0; s < QS; ++s) {
+      for (int s = 0; s < KS; ++s) {
         const int piece = 2 * s + g;
         qop[s] = u32x4_t{0, 0, 0, 0};
-        if (piece * VEC < a.d && q_len > 0) qop[s] = *reinterpret_cast<const u32x4_t*>(qrow + piece * VEC);
+        if (piece * 8 < a.d && t.q_len > 0) qop[s] = *reinterpret_cast<const u32x4_t*>(qrow + piece * 8);
       }
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // the query: nothing that the compiler tracks stays pending in the loop
@@ -319,85 +362,60 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
 #pragma unroll
       for (int e = 0; e < 16; ++e) oacc[i][e] = 0.f;
     unsigned cslot = 0;
-    for (int st = 0; st < issued; ++st) {
-      const int younger = issued - 1 - st;  // stages in flight behind this one: at most NS - 2
-      if (NS == 3 && younger >= 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * PER));
-      else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-      __syncthreads();  // the stage is there for all, and nobody reads the slot that is filled next
-      issue();
-      const int nkeys = st + 1 == issued ? last_keys : SK;  // only the list's last stage can hold fewer
+    for (int st = 0; st < loads.issued; ++st) {
+      const int nkeys = loads.open(a, walk, st);
 
-      // ---- scores of SK / 32 tiles of 32 keys
-      f32x16_t sc[SK / 32];
+      // ---- scores of two tiles of 32 keys; all fragments are on their way before the first product
+      u32x4_t kf[KS][2];
 #pragma unroll
-      for (int u = 0; u < SK / 32; ++u)
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) kf[s][u] = lds_read<u32x4_t>(((kat + cslot) ^ (32 * s)) + 32 * u * ROW);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16_t sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
-      constexpr int KF = F32 ? 1 : QS;  // pieces of a key that are read ahead of the products
-      u32x4_t kf[KF][SK / 32];
 #pragma unroll
-      for (int s = 0; s < QS; ++s) {
-        if (s % KF == 0) {
+      for (int s = 0; s < KS; ++s)
 #pragma unroll
-          for (int i = 0; i < KF; ++i)
-#pragma unroll
-            for (int u = 0; u < SK / 32; ++u) kf[i][u] = lds_read<u32x4_t>(((kat + cslot) ^ (32 * (s + i))) + 32 * u * ROW);
-          if constexpr (!F32) __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int u = 0; u < SK / 32; ++u) {
-          if constexpr (F32) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              sc[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[0][u][j]), __uint_as_float(qop[s][j]), sc[u], 0, 0, 0);
-          } else {
-            sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s][u]), __builtin_bit_cast(bf16x8_t, qop[s]), sc[u], 0, 0, 0);
-          }
-        }
-      }
+        for (int u = 0; u < 2; ++u)
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s][u]), __builtin_bit_cast(bf16x8_t, qop[s]), sc[u], 0, 0, 0);
       if (nkeys < SK) {
         const int lim = nkeys - 4 * g;  // register e of tile u is key 32 u + 8 (e / 4) + e % 4 + 4 g
 #pragma unroll
-        for (int u = 0; u < SK / 32; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (32 * u + 8 * (e / 4) + e % 4 >= lim) sc[u][e] = -INFINITY;
       }
-      // bf16 values on their way while the exponentials are taken
-      constexpr int VT = F32 ? 1 : SK / 16;
-      uint2 vlo[VT][OB], vhi[VT][OB];
-      if constexpr (!F32) {
+      // the values are on their way while the exponentials are taken
+      uint2 vlo[4][OB], vhi[4][OB];
 #pragma unroll
-        for (int t = 0; t < VT; ++t)
+      for (int k16 = 0; k16 < 4; ++k16)
 #pragma unroll
-          for (int i = 0; i < OB; ++i) {
-            vlo[t][i] = lds_read_tr(((vat + cslot) ^ (64 * i)) + 16 * t * ROW);
-            vhi[t][i] = lds_read_tr(((vat + cslot) ^ (64 * i) ^ (lds_swizzle<ROW, F32>(8) * 16)) + (16 * t + 8) * ROW);
-          }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+        for (int i = 0; i < OB; ++i) {
+          vlo[k16][i] = lds_read_tr(((vat + cslot) ^ (64 * i)) + 16 * k16 * ROW);
+          vhi[k16][i] = lds_read_tr(((vat + cslot) ^ (64 * i) ^ (G::swizzle(8) * 16)) + (16 * k16 + 8) * ROW);
+        }
+      __builtin_amdgcn_sched_barrier(0);
 
       // ---- probabilities against the lazy reference maximum: it is raised only when the partial sums say that an
       // exponent has grown past it, so that the steady state has no maximum and no rescaling.  exp2 of up to 2^8 is
-      // harmless in float32 and, relative as bf16 rounds, in bf16.
-      u32x4_t pk[F32 ? 1 : SK / 16];
-      float pf[F32 ? 16 : 1];
+      // harmless in float32 and, relative as bf16 rounds, in bf16.  They are rounded to bf16, the matrix cores' type for V:
+      // half a step of 2^-8 of each weight, which the sums over the keys average out; the row sum is of the rounded
+      // values, those that weigh V.
+      u32x4_t pk[4];
       auto exponentiate = [&]() {
         float rs = 0.f;
 #pragma unroll
-        for (int u = 0; u < SK / 32; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int e = 0; e < 16; e += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[u][e], a.c, -mref)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[u][e + 1], a.c, -mref));
-            if constexpr (F32) {
-              pf[e] = p0;
-              pf[e + 1] = p1;
-              rs += p0 + p1;
-            } else {  // the sum is of the rounded values, those that weigh V
-              const unsigned w = pack_bf16x2(p0, p1);
-              pk[2 * u + e / 8][e % 8 / 2] = w;
-              rs = dot2_ones(w, rs);
-            }
+            const unsigned w = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[u][e], a.c, -mref)), __builtin_amdgcn_exp2f(fmaf(sc[u][e + 1], a.c, -mref)));
+            pk[2 * u + e / 8][e % 8 / 2] = w;
+            rs = dot2_ones(w, rs);
           }
         return rs;
       };
@@ -405,7 +423,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
       if (__builtin_amdgcn_ballot_w64(!(rs <= kSparseTrigger)) != 0) {
         float mx = sc[0][0];
 #pragma unroll
-        for (int u = 0; u < SK / 32; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[u][e]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * a.c;  // both halves of the row agree on the new reference
@@ -421,82 +439,223 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 && sizeof(T) == 2 ? 3
       lsum += rs;
 
       // ---- O^T += V^T P^T
-      if constexpr (F32) {
-        // one step of two keys: the lane's own and lane ^ 32's
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+      for (int k16 = 0; k16 < 4; ++k16)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < OB; ++i)
-              oacc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(lds_read<float>(((vat + cslot) ^ (lds_swizzle<ROW, F32>(8 * q + j) * 16) ^ (128 * i)) + (8 * q + j) * ROW), pf[4 * q + j], oacc[i], 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int t = 0; t < SK / 16; ++t)
-#pragma unroll
-          for (int i = 0; i < OB; ++i) {
-            const u32x4_t vf{vlo[t][i].x, vlo[t][i].y, vhi[t][i].x, vhi[t][i].y};
-            oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[t]), oacc[i], 0, 0, 0);
-          }
-      }
-      cslot = cslot == (NS - 1) * 2 * HALF ? 0 : cslot + 2 * HALF;
+        for (int i = 0; i < OB; ++i) {
+          const u32x4_t vf{vlo[k16][i].x, vlo[k16][i].y, vhi[k16][i].x, vhi[k16][i].y};
+          oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[k16]), oacc[i], 0, 0, 0);
+        }
+      cslot = cslot == (G::NS - 1) * 2 * G::HALF ? 0 : cslot + 2 * G::HALF;
     }
     lsum += __shfl_xor(lsum, 32, kWave);
-    if (a.nsplit == 1) {
-      sparse_store<T, OB>(a, oacc, lsum, b, hk, token, sub, valid, g);
-    } else if (valid) {  // rows that hold no query are not read back either
-      f32x4_t* img = reinterpret_cast<f32x4_t*>(a.part) + (work * NW + wave) * (OB * 4 + 1) * kWave + lane;
+    if (token >= 0) {
 #pragma unroll
-      for (int i = 0; i < OB * 4; ++i)
-        img[i * kWave] = f32x4_t{oacc[i / 4][i % 4 * 4], oacc[i / 4][i % 4 * 4 + 1], oacc[i / 4][i % 4 * 4 + 2], oacc[i / 4][i % 4 * 4 + 3]};
-      img[OB * 4 * kWave] = f32x4_t{mref, lsum, 0.f, 0.f};
+      for (int i = 0; i < OB; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int ch = 32 * i + 8 * q + 4 * g;
+          if (ch < a.d) sparse_put<bf16>(a, t, token, sub, ch, f32x4_t{oacc[i][4 * q], oacc[i][4 * q + 1], oacc[i][4 * q + 2], oacc[i][4 * q + 3]}, lsum);
+        }
+      if (a.nsplit > 1 && g == 0) sparse_put_ml(a, t, token, sub, mref, lsum);
     }
     __syncthreads();  // the next tile's loads overwrite the ring
   }
 }
 
-// The shares of a row tile joined: weights 2^(m - max m), in the order of the shares.  A wavefront takes four channels per
-// lane of one 32-row image; blockIdx.y * 4 + wavefront says which.
-template <typename T, int OB, int NW>
-__global__ __launch_bounds__(256) void sparse_join_kernel(SparseArgs a) {
-  const int lane = threadIdx.x % kWave, i = blockIdx.y * 4 + threadIdx.x / kWave, r = lane % 32, g = lane / 32;
-  const int64_t images = a.work / a.nsplit * NW, pitch = (int64_t)NW * (OB * 4 + 1) * kWave;
-  for (int64_t im = blockIdx.x; im < images; im += gridDim.x) {
-    const int64_t t = im / NW;
-    const int wave = (int)(im % NW);
-    int64_t at = t;
-    const int tile = (int)(at % a.tiles_per_run);
-    at /= a.tiles_per_run;
-    const int run = (int)(at % a.runs);
-    at /= a.runs;
-    const int hk = (int)(at % a.heads_kv), b = (int)(at / a.heads_kv);
-    const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq;
-    const int rho = (tile * NW + wave) * 32 + r, in_run = rho / a.group, sub = rho - in_run * a.group;
-    const int64_t token = (int64_t)run * a.q_block + in_run;
-    const int ch = 32 * (i / 4) + 8 * (i % 4) + 4 * g;
-    if (in_run >= a.q_block || token >= q_len || ch >= a.d) continue;
-    const f32x4_t* img = reinterpret_cast<const f32x4_t*>(a.part) + (t * a.nsplit * NW + wave) * (OB * 4 + 1) * kWave + lane;
-    float top = kSparseLow;
-#pragma unroll 8
-    for (int s = 0; s < a.nsplit; ++s) top = fmaxf(top, img[s * pitch + OB * 4 * kWave][0]);
-    float l = 0.f;
-    f32x4_t o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = 0; s < a.nsplit; ++s) {
-      const f32x4_t ml = img[s * pitch + OB * 4 * kWave], x = img[s * pitch + i * kWave];
-      const float w = __builtin_amdgcn_exp2f(ml[0] - top);
-      l = fmaf(ml[1], w, l);
+// float32 throughout, on v_mfma_f32_16x16x4_f32: a wavefront's 32 rows are two column tiles, so that a key or value operand
+// serves two products; a result lane (c, g), g = lane / 16, holds column c and rows 4 g + j.  Those four keys are, register by
+// register, the column operand of four steps of the second product.  16-channel tiles: heads of 40 contract 40 and produce
+// 48 channels (32 x 32 tiles: 48 and 64).  Bound by the float32 matrix rate, 256 flop per clock and CU.
+template <int KS, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 || KS <= 4 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {
+  using G = SparseGeo<float, KS>;
+  constexpr int SK = G::SK, ROW = G::ROW;
+  __shared__ __align__(1024) u32x4_t ring[G::NS * 2 * G::HALF / 16];
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
+  StageLoads<float, KS, NW> loads;
+  loads.setup(a, lds0);
+  const int lane = loads.lane, c = lane % 16, g = lane / 16;
+  const unsigned kat = lds0 + c * ROW + ((g / 2) ^ G::swizzle(c)) * 16 + (g % 2) * 8;  // channels 8 s + 2 g ..: ^ 32 s
+  const unsigned vat = lds0 + G::HALF + 4 * g * ROW + ((c / 4) ^ G::swizzle(4 * g)) * 16 + (c % 4) * 4;  // channel tile i: ^ 64 i
+
+  const int64_t chunk = (a.work + 7) / 8;  // contiguous per XCD, as above
+  const int64_t chunk_end = min(a.work, ((int64_t)(blockIdx.x % 8) + 1) * chunk);
+  for (int64_t work = (int64_t)(blockIdx.x % 8) * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
+    const SparseTile t(a, work);
+    int token[2], sub[2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = fmaf(x[j], w, o[j]);
+    for (int h = 0; h < 2; ++h) token[h] = t.token(a, (t.tile * NW + loads.wave) * 32 + 16 * h + c, sub[h]);
+    BlockWalk<SK> walk;
+    t.begin(a, NW * 32, walk);
+    loads.begin(a, t);
+    for (int i = 0; i < G::NS - 1; ++i) loads.issue(a, walk);
+
+    float2 qop[2][2 * KS];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float* qrow = static_cast<const float*>(a.q) + t.b * a.qb + (int64_t)max(token[h], 0) * a.qn +
+                          (int64_t)(t.hk * a.group + (token[h] < 0 ? 0 : sub[h])) * a.qh + 2 * g;
+#pragma unroll
+      for (int s = 0; s < 2 * KS; ++s) {
+        qop[h][s] = make_float2(0.f, 0.f);
+        if (8 * s < a.d && t.q_len > 0) qop[h][s] = *reinterpret_cast<const float2*>(qrow + 8 * s);
+      }
     }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // the queries: nothing that the compiler tracks stays pending in the loop
+
+    f32x4_t oacc[2][KS];
+    float mref[2], lsum[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      mref[h] = kSparseLow;
+      lsum[h] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) oacc[h][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    unsigned cslot = 0;
+    for (int st = 0; st < loads.issued; ++st) {
+      const int nkeys = loads.open(a, walk, st);
+      f32x4_t sc[2][2];  // [key tile][column tile]
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) sc[u][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 2 * KS; ++s)
+        if (8 * s < a.d) {
+          f32x2_t kf[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) kf[u] = lds_read<f32x2_t>(((kat + cslot) ^ (32 * s)) + 16 * u * ROW);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                sc[u][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u][j], j ? qop[h][s].y : qop[h][s].x, sc[u][h], 0, 0, 0);
+        }
+      if (nkeys < SK) {
+        const int lim = nkeys - 4 * g;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (16 * u + j >= lim) sc[u][h][j] = -INFINITY;
+      }
+
+      // ---- probabilities against the lazy reference maximum, as above
+      float p[2][2][4], rs[2];
+      auto exponentiate = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          rs[h] = 0.f;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              p[u][h][j] = __builtin_amdgcn_exp2f(fmaf(sc[u][h][j], a.c, -mref[h]));
+              rs[h] += p[u][h][j];
+            }
+        }
+      };
+      exponentiate();
+      if (__builtin_amdgcn_ballot_w64(!(rs[0] <= kSparseTrigger) || !(rs[1] <= kSparseTrigger)) != 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float mx = sc[0][h][0];
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[u][h][j]);
+          mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * a.c;  // the four parts of the row agree on the new reference
+          const float up = fmaxf(mx, mref[h]), alpha = __builtin_amdgcn_exp2f(mref[h] - up);
+          mref[h] = up;
+          lsum[h] *= alpha;
+#pragma unroll
+          for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) oacc[h][i][j] *= alpha;
+        }
+        exponentiate();
+      }
+      lsum[0] += rs[0];
+      lsum[1] += rs[1];
+
+      // ---- O^T += V^T P^T: step (u, j) takes keys 16 u + 4 g + j
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < KS; ++i) {
+            const float vf = lds_read<float>(((vat + cslot) ^ (G::swizzle(j) * 16) ^ (64 * i)) + (16 * u + j) * ROW);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) oacc[h][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, p[u][h][j], oacc[h][i], 0, 0, 0);
+          }
+      cslot = cslot == (G::NS - 1) * 2 * G::HALF ? 0 : cslot + 2 * G::HALF;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      lsum[h] += __shfl_xor(lsum[h], 16, kWave);
+      lsum[h] += __shfl_xor(lsum[h], 32, kWave);
+      if (token[h] >= 0) {
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+          if (16 * i + 4 * g < a.d) sparse_put<float>(a, t, token[h], sub[h], 16 * i + 4 * g, oacc[h][i], lsum[h]);
+        if (a.nsplit > 1 && g == 0) sparse_put_ml(a, t, token[h], sub[h], mref[h], lsum[h]);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The shares of a query row joined: weights 2^(m - max m).  A wavefront per row: its lanes hold one share's maximum and sum
+// each (nsplit <= 64), then 64 / (d / 4) shares' outputs at a time, four channels per lane; the order of the sums is fixed.
+template <typename T>
+__global__ __launch_bounds__(256) void sparse_join_kernel(SparseArgs a, int64_t rows) {
+  const int lane = threadIdx.x % kWave, heads = a.heads_kv * a.group, quads = a.d / 4;
+  // lanes of one share: the next power of two of quads
+  const int width = quads <= 2 ? 2 : quads <= 4 ? 4 : quads <= 8 ? 8 : quads <= 16 ? 16 : 32, at_once = kWave / width;
+  const int quad = lane % width, which = lane / width;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; row < rows; row += (int64_t)gridDim.x * 4) {
+    const int64_t bn = row / heads;
+    const int h = (int)(row - bn * heads), b = (int)(bn / a.Nq);
+    const int64_t token = bn - (int64_t)b * a.Nq;
+    if (a.q_len && token >= a.q_len[b]) continue;
+    const float2 ml = lane < a.nsplit ? a.part_ml[row * a.nsplit + lane] : make_float2(kSparseLow, 0.f);
+    const float w = __builtin_amdgcn_exp2f(ml.x - wave_max(ml.x));
+    const float l = wave_sum(ml.y * w);
+    const float* src = a.part + row * a.nsplit * a.d + 4 * quad;
+    f32x4_t o{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < a.nsplit; s0 += 4 * at_once) {
+      f32x4_t x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int s = s0 + u * at_once + which;
+        x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (s < a.nsplit && quad < quads) x[u] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)s * a.d);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float ws = __shfl(w, (s0 + u * at_once + which) % kWave, kWave);  // past the last share: times zero
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = fmaf(x[u][j], ws, o[j]);
+      }
+    }
+    for (int step = width; step < kWave; step <<= 1)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], step, kWave);
+    if (which != 0 || quad >= quads) continue;
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* dst = static_cast<T*>(a.o) + b * a.ob + token * a.on + (int64_t)(hk * a.group + sub) * a.oh + ch;
-    if constexpr (sizeof(T) == 2) {
-      if (a.o_frag) dst = static_cast<T*>(a.o) + act_offset((int64_t)b * a.Nq + token, (hk * a.group + sub) * a.d + ch, a.o_frag);
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
-    } else {
-      *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = l > 0.f ? o[j] * inv : 0.f;
+    T* dst = static_cast<T*>(a.o) + b * a.ob + token * a.on + (int64_t)h * a.oh + 4 * quad;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+    else *reinterpret_cast<f32x4_t*>(dst) = o;
   }
 }
 

@@ -14,8 +14,9 @@ struct BlocksPlan {
 };
 
 struct SparsePlan {
-  int nw, ks, ob, nsplit;
+  int nw, ks, nsplit;
   int64_t tiles_per_run, tiles, work;
+  int64_t rows;  // of all queries and heads
   size_t part_bytes;
 };
 

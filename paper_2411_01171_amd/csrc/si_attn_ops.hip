@@ -229,20 +229,20 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
   a.runs = (int)p.runs; a.blocks = (int)p.blocks; a.words = (int)p.words;
   a.keep = (int)std::min<int64_t>(keep, p.blocks);
   a.pitch = (int)((p.blocks + 15) / 16 * 16 + 2);
-  auto launch = [&](auto cap, auto kpl) {
+  auto launch = [&](auto cap, auto kpl, auto threads) {
     a.rows = std::min(16, cap.value / a.pitch);
     a.tiles = (int)((p.runs + a.rows - 1) / a.rows);
     a.work = q->B * k->heads * a.tiles;
-    block_select_kernel<cap.value, kpl.value><<<(unsigned)((std::min<int64_t>(a.work, kGridMost) + 7) / 8 * 8), kSelectThreads, 0, st>>>(a);
+    block_select_kernel<cap.value, kpl.value, threads.value><<<(unsigned)((std::min<int64_t>(a.work, kGridMost) + 7) / 8 * 8), threads.value, 0, st>>>(a);
   };
   // the smallest store of scores that holds 16 runs, for as many workgroups on a CU as possible
   using std::integral_constant;
-  if (p.blocks <= 64) launch(integral_constant<int, 16 * 66>(), integral_constant<int, 1>());
-  else if (p.blocks <= 128) launch(integral_constant<int, 16 * 130>(), integral_constant<int, 2>());
-  else if (p.blocks <= 256) launch(integral_constant<int, 16 * 258>(), integral_constant<int, 4>());
-  else if (p.blocks <= 512) launch(integral_constant<int, 16 * 514>(), integral_constant<int, 8>());
-  else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>());
-  else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>());
+  if (p.blocks <= 64) launch(integral_constant<int, 16 * 66>(), integral_constant<int, 1>(), integral_constant<int, 256>());
+  else if (p.blocks <= 128) launch(integral_constant<int, 16 * 130>(), integral_constant<int, 2>(), integral_constant<int, 256>());
+  else if (p.blocks <= 256) launch(integral_constant<int, 16 * 258>(), integral_constant<int, 4>(), integral_constant<int, 256>());
+  else if (p.blocks <= 512) launch(integral_constant<int, 16 * 514>(), integral_constant<int, 8>(), integral_constant<int, 512>());
+  else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>(), integral_constant<int, 1024>());
+  else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>(), integral_constant<int, 1024>());
   static_assert(16 * 1028 >= kSelectMaxBlocks + 2, "one run of the longest list");
   SI_CHECK_LAUNCH();
   return SI_OK;
@@ -257,7 +257,6 @@ si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, con
   p->nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
   const int d = (int)q->dim_head;
   p->ks = d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 80 ? 5 : d <= 96 ? 6 : 8;
-  p->ob = (p->ks + 1) / 2;
   p->tiles_per_run = (rows + 32 * p->nw - 1) / (32 * p->nw);
   if ((double)q->B * k->heads * b.runs * (double)p->tiles_per_run >= 1e12) return SI_ERR_SHAPE;
   p->tiles = q->B * k->heads * b.runs * p->tiles_per_run;
@@ -265,35 +264,37 @@ si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, con
   p->nsplit = 1;
   if (may_split && p->tiles > 0 && p->tiles * 2 <= want) p->nsplit = (int)std::min<int64_t>(std::min<int64_t>(want / p->tiles, 64), std::max<int64_t>(1, b.blocks / 2));
   p->work = p->tiles * p->nsplit;
-  p->part_bytes = p->nsplit > 1 ? (size_t)p->work * p->nw * (p->ob * 4 + 1) * kWave * 16 : 0;
+  p->rows = q->B * q->N * q->heads;
+  p->part_bytes = p->nsplit > 1 ? (size_t)(q->B * q->N * q->heads) * p->nsplit * (q->dim_head + 2) * sizeof(float) : 0;
   return SI_OK;
 }
 
 template <typename T, int KS, int NW>
-static void launch_sparse(const SparseArgs& a, int64_t tiles, hipStream_t st) {
+static void launch_sparse(const SparseArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)((std::min<int64_t>(a.work, kGridMost) + 7) / 8 * 8);
-  sparse_attn_kernel<T, KS, NW><<<grid, 64 * NW, 0, st>>>(a);
-  if (a.nsplit > 1) {
-    constexpr int OB = (KS + 1) / 2;
-    sparse_join_kernel<T, OB, NW><<<dim3((unsigned)std::min<int64_t>(tiles * NW, kGridMost), OB), 256, 0, st>>>(a);
-  }
+  if constexpr (sizeof(T) == 2) sparse_attn_bf16_kernel<KS, NW><<<grid, 64 * NW, 0, st>>>(a);
+  else sparse_attn_f32_kernel<KS, NW><<<grid, 64 * NW, 0, st>>>(a);
 }
 template <typename T>
 static void dispatch_sparse(const SparseArgs& a, const SparsePlan& p, hipStream_t st) {
   auto by_width = [&](auto nw) {
     constexpr int NW = nw.value;
     switch (p.ks) {
-      case 2: launch_sparse<T, 2, NW>(a, p.tiles, st); break;
-      case 3: launch_sparse<T, 3, NW>(a, p.tiles, st); break;
-      case 4: launch_sparse<T, 4, NW>(a, p.tiles, st); break;
-      case 5: launch_sparse<T, 5, NW>(a, p.tiles, st); break;
-      case 6: launch_sparse<T, 6, NW>(a, p.tiles, st); break;
-      default: launch_sparse<T, 8, NW>(a, p.tiles, st); break;
+      case 2: launch_sparse<T, 2, NW>(a, st); break;
+      case 3: launch_sparse<T, 3, NW>(a, st); break;
+      case 4: launch_sparse<T, 4, NW>(a, st); break;
+      case 5: launch_sparse<T, 5, NW>(a, st); break;
+      case 6: launch_sparse<T, 6, NW>(a, st); break;
+      default: launch_sparse<T, 8, NW>(a, st); break;
     }
   };
   if (p.nw == 1) by_width(std::integral_constant<int, 1>());
   else if (p.nw == 2) by_width(std::integral_constant<int, 2>());
   else by_width(std::integral_constant<int, 4>());
+  if (a.nsplit > 1) {
+    const int64_t rows = p.rows;
+    sparse_join_kernel<T><<<(unsigned)std::min<int64_t>((rows + 3) / 4, kGridMost), 256, 0, st>>>(a, rows);
+  }
 }
 
 si_status enqueue_sparse(const si_heads* q, const si_heads* k, const si_heads* v, const BlocksPlan& b, const SparsePlan& p, int64_t q_block,
@@ -316,6 +317,7 @@ si_status enqueue_sparse(const si_heads* q, const si_heads* k, const si_heads* v
   a.work = p.work; a.nsplit = p.nsplit;
   a.c = scale * 1.4426950408889634f;
   a.part = reinterpret_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(a.part + (p.nsplit > 1 ? p.rows * p.nsplit * q->dim_head : 0));
   a.o_frag = o_frag;
   StageScope scope("attn_sparse", st);
   if (q->dtype == SI_F32) dispatch_sparse<float>(a, p, st);
