@@ -22,7 +22,7 @@ struct MeansOf {
   const int* len;
   double* out;  // [B][heads_kv][runs][d]
   int N, group, block, runs;
-  int64_t work;    // B * runs * chunks
+  unsigned work;   // B * runs * chunks
 };
 struct MeansArgs {
   MeansOf of[2];   // queries in runs, keys in blocks: one launch
@@ -36,11 +36,11 @@ __global__ __launch_bounds__(kMeanPieces* kMeanSlices) void block_means_kernel(M
   __shared__ double part[kMeanSlices][kMeanPieces][VEC];
   const int px = threadIdx.x % kMeanPieces, slice = threadIdx.x / kMeanPieces;
   const int per_head = args.d / VEC;
-  for (int64_t w = blockIdx.x; w < args.of[0].work + args.of[1].work; w += gridDim.x) {
+  for (unsigned w = blockIdx.x; w < args.of[0].work + args.of[1].work; w += gridDim.x) {
     const bool keys = w >= args.of[0].work;
     const MeansOf& a = args.of[keys ? 1 : 0];
-    const int64_t work = keys ? w - args.of[0].work : w;
-    const int chunk = (int)(work % args.chunks), run = (int)(work / args.chunks % a.runs), b = (int)(work / args.chunks / a.runs);
+    const unsigned work = keys ? w - args.of[0].work : w, br = work / (unsigned)args.chunks;
+    const int chunk = (int)(work - br * args.chunks), b = (int)(br / (unsigned)a.runs), run = (int)(br - (unsigned)b * a.runs);
     const int item = chunk * kMeanPieces + px;
     const bool live = item < args.heads_kv * per_head;
     const int hk = live ? item / per_head : 0, ch = live ? (item - hk * per_head) * VEC : 0;
@@ -95,7 +95,7 @@ struct SelectArgs {
   int keep, rows;         // blocks to keep; runs of a workgroup
   int pitch;              // scores of one run in LDS
   int tiles;              // of `rows` runs; a workgroup takes one tile of one (b, kv head)
-  int64_t work;           // B * heads_kv * tiles
+  unsigned work;          // B * heads_kv * tiles
 };
 
 // Order of float64 as unsigned integers: NaN as -infinity, -0 as +0; 0 is below every value.
@@ -105,40 +105,55 @@ __device__ __forceinline__ unsigned long long order_key(double x) {
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
-// The largest T of 32-bit words with at least `need` values >= T, found from the top bit on; count(c) = number of values >= c.
-// Stops early, with `exact`, when exactly `need` values are >= the prefix.
-template <class Count>
+// The largest T of 32-bit words with at least `need` values >= T, found from the top bits on; count(c) = number of values >= c.
+// Stops early, with `exact`, when exactly `need` values are >= the prefix.  BITS at a time: 2 where a count is nearly all
+// latency (a few ballots), 1 where it is work.  (Candidates interpolated from the counts, half as many, cost more than they save.)
+template <int BITS, class Count>
 __device__ __forceinline__ unsigned kth_word(int need, Count count, bool& exact) {
   unsigned t = 0;
   exact = false;
-  for (int bit = 31; bit >= 0; --bit) {
-    const unsigned c = t | (1u << bit);
-    const int n = count(c);
-    if (n >= need) {
-      t = c;
-      if (n == need) {
-        exact = true;
-        break;
+  for (int bit = 32 - BITS; bit >= 0; bit -= BITS) {
+    int n[1 << BITS];
+#pragma unroll
+    for (int i = 1; i < 1 << BITS; ++i) n[i] = count(t | ((unsigned)i << bit));
+    unsigned up = 0;
+#pragma unroll
+    for (int i = 1; i < 1 << BITS; ++i)  // counts fall with i
+      if (n[i] >= need) {
+        up = (unsigned)i << bit;
+        exact = n[i] == need;
       }
-    }
+    t |= up;
+    if (exact) break;
   }
   return t;
 }
 
+// Sum over the wavefront's lanes by data-parallel primitives, in a scalar register.
+__device__ __forceinline__ int lanes_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // from lane - 1, - 2, - 4, - 8 of a row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last lane of row 0 to row 1, of row 2 to row 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
 // CAP: scores (float64) of a workgroup in LDS.  KPL: keys of a run per lane in registers (64 KPL >= blocks), or 0: read from
-// LDS every time.  Counting with a ballot per key and lane beats sums over the lanes from there up to 1024 blocks; the loads of
-// a tile's means are all in flight before its products (900 blocks x 450 runs x 20 heads: 232 -> measured below).
-template <int CAP, int KPL, int NT>
+// LDS every time.  NC: channels in steps of 32, so that all loads of a tile's means are in flight before its products.
+template <int CAP, int KPL, int NT, int NC>
 __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
   __shared__ unsigned long long keys[CAP];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  constexpr int nw = NT / kWave, STEPS = 8;  // steps of 8 channels whose loads are in flight together
+  constexpr int nw = NT / kWave, STEPS = 4 * NC;  // of 8 channels
   // the tiles of one (b, kv head) on one XCD: its L2 holds their key means
-  const int64_t chunk = (a.work + 7) / 8;
-  const int64_t chunk_end = min(a.work, ((int64_t)(blockIdx.x % 8) + 1) * chunk);
-  for (int64_t work = (int64_t)(blockIdx.x % 8) * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
-    const int64_t pair = work / a.tiles;  // (b, kv head)
-    const int b = (int)(pair / a.heads_kv), run0 = (int)(work - pair * a.tiles) * a.rows;
+  const unsigned chunk = (a.work + 7) / 8;
+  const unsigned chunk_end = min(a.work, (blockIdx.x % 8 + 1) * chunk);
+  for (unsigned work = blockIdx.x % 8 * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
+    const unsigned pr = work / (unsigned)a.tiles;  // (b, kv head)
+    const int64_t pair = pr;
+    const int b = (int)(pr / (unsigned)a.heads_kv), run0 = (int)(work - pr * a.tiles) * a.rows;
     const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.Nk) : a.Nk;
     const int nblk = (k_len + a.k_block - 1) / a.k_block;  // blocks with a key
 
@@ -147,23 +162,23 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
       const int m = lane % 16, g = lane / 16;
       const int qrow = min(run0 + min(m, a.rows - 1), a.runs - 1);
       const double* qp = a.qm + (pair * a.runs + qrow) * a.d + 2 * g;
+      // channels past the head: any of the head's, made zero on both sides
+      auto means = [&](const double* p, f64x2_t (&v)[STEPS]) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) v[s] = *reinterpret_cast<const f64x2_t*>(p + min(8 * s, a.d - 8));
+#pragma unroll
+        for (int s = 4 * NC - 4; s < STEPS; ++s)
+          if (8 * s >= a.d) v[s] = f64x2_t{0.0, 0.0};
+      };
+      f64x2_t qv[STEPS], kv[STEPS];
+      if (wave * 16 < nblk) means(qp, qv);
       for (int j0 = wave * 16; j0 < nblk; j0 += nw * 16) {
-        const double* kp = a.km + (pair * a.blocks + min(j0 + m, a.blocks - 1)) * a.d + 2 * g;
+        means(a.km + (pair * a.blocks + min(j0 + m, a.blocks - 1)) * a.d + 2 * g, kv);
         f64x4_t acc{0.0, 0.0, 0.0, 0.0};
-        for (int c = 0; c < a.d; c += 8 * STEPS) {
-          f64x2_t kv[STEPS], qv[STEPS];
 #pragma unroll
-          for (int s = 0; s < STEPS; ++s)
-            if (c + 8 * s < a.d) {
-              kv[s] = *reinterpret_cast<const f64x2_t*>(kp + c + 8 * s);
-              qv[s] = *reinterpret_cast<const f64x2_t*>(qp + c + 8 * s);
-            }
-#pragma unroll
-          for (int s = 0; s < STEPS; ++s)
-            if (c + 8 * s < a.d) {
-              acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][0], qv[s][0], acc, 0, 0, 0);
-              acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][1], qv[s][1], acc, 0, 0, 0);
-            }
+        for (int s = 0; s < STEPS; ++s) {
+          acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][0], qv[s][0], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f64_16x16x4f64(kv[s][1], qv[s][1], acc, 0, 0, 0);
         }
         if (m < a.rows) {
 #pragma unroll
@@ -197,24 +212,26 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
       }
       auto tally = [&](auto pred) {
         int n = 0;
-        if constexpr (KPL > 0) {
+        if constexpr (KPL > 0 && KPL <= 4) {
 #pragma unroll
           for (int i = 0; i < KPL; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(pred(held[i])));
+          return n;
+        } else if constexpr (KPL > 0) {
+#pragma unroll
+          for (int i = 0; i < KPL; ++i) n += pred(held[i]) ? 1 : 0;
         } else {
           for (int j = lane; j < nblk; j += kWave) n += pred(key[j]) ? 1 : 0;
-#pragma unroll
-          for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
-          n = __builtin_amdgcn_readfirstlane(n);
         }
-        return n;
+        return lanes_sum(n);
       };
       bool exact;
-      const unsigned hi = kth_word(a.keep, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); }, exact);
+      constexpr int BITS = KPL > 0 && KPL <= 4 ? 2 : 1;
+      const unsigned hi = kth_word<BITS>(a.keep, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); }, exact);
       unsigned long long least = (unsigned long long)hi << 32;  // everything >= least is kept, except some of the equal ones
       int need_equal = 0;  // of the values == least, when not exact
       if (!exact) {
         const int above = tally([&](unsigned long long k) { return (unsigned)(k >> 32) > hi; });
-        const unsigned lo = kth_word(
+        const unsigned lo = kth_word<BITS>(
             a.keep - above,
             [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) == hi && (unsigned)k >= c; }); }, exact);
         least |= lo;

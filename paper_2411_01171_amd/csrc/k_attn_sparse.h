@@ -28,7 +28,7 @@ struct SparseArgs {
   int Nq, Nk, heads_kv, group, d;
   int q_block, k_block, runs, words;
   int tiles_per_run;         // row tiles of a run
-  int64_t work;              // B * heads_kv * runs * tiles_per_run * nsplit
+  unsigned work;             // B * heads_kv * runs * tiles_per_run * nsplit
   int nsplit;
   float c;                   // softmax scale * log2(e)
   float* part;               // nsplit > 1: outputs [query row][nsplit][d], then (maximum, sum) [query row][nsplit]; query row = (b Nq + n) heads + h
@@ -178,21 +178,24 @@ __device__ __forceinline__ uint2 lds_read_tr(unsigned at) {
 // One row tile of a run, or a share of its blocks.
 struct SparseTile {
   int part, tile, run, hk, b, q_len, k_len;
-  __device__ __forceinline__ SparseTile(const SparseArgs& a, int64_t work) {
-    part = (int)(work % a.nsplit);
-    int64_t at = work / a.nsplit;
-    tile = (int)(at % a.tiles_per_run);
-    at /= a.tiles_per_run;
-    run = (int)(at % a.runs);
-    at /= a.runs;
-    hk = (int)(at % a.heads_kv);
-    b = (int)(at / a.heads_kv);
+  __device__ __forceinline__ SparseTile(const SparseArgs& a, unsigned work) {
+    auto pop = [&](int n) {  // the fastest index
+      const unsigned up = work / (unsigned)n;
+      const int i = (int)(work - up * n);
+      work = up;
+      return i;
+    };
+    part = a.nsplit > 1 ? pop(a.nsplit) : 0;
+    tile = a.tiles_per_run > 1 ? pop(a.tiles_per_run) : 0;
+    run = pop(a.runs);
+    hk = pop(a.heads_kv);
+    b = (int)work;
     q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq;
     k_len = a.k_len ? min(max(a.k_len[b], 0), a.Nk) : a.Nk;
   }
   // token of row `rho` of the run, or -1; sub: its head among those of the key head
   __device__ __forceinline__ int token(const SparseArgs& a, int rho, int& sub) const {
-    const int in_run = rho / a.group;
+    const int in_run = a.group > 1 ? rho / a.group : rho;
     const int64_t n = (int64_t)run * a.q_block + in_run;
     sub = rho - in_run * a.group;
     return in_run < a.q_block && n < q_len ? (int)n : -1;
@@ -331,9 +334,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
   const unsigned vat = lds0 + G::HALF + vr * ROW + ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ G::swizzle(vr)) * 16 + (lane % 2) * 8;
 
   // Work goes to the 8 XCDs in contiguous chunks, so that the keys and values of a head are fetched into one L2.
-  const int64_t chunk = (a.work + 7) / 8;
-  const int64_t chunk_end = min(a.work, ((int64_t)(blockIdx.x % 8) + 1) * chunk);
-  for (int64_t work = (int64_t)(blockIdx.x % 8) * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
+  const unsigned chunk = (a.work + 7) / 8;
+  const unsigned chunk_end = min(a.work, (blockIdx.x % 8 + 1) * chunk);
+  for (unsigned work = blockIdx.x % 8 * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
     const SparseTile t(a, work);
     int sub;
     const int token = t.token(a, (t.tile * NW + loads.wave) * 32 + r, sub);  // this lane's query row
@@ -479,9 +482,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || KS <= 4 ? 2 : 1) void sparse_at
   const unsigned kat = lds0 + c * ROW + ((g / 2) ^ G::swizzle(c)) * 16 + (g % 2) * 8;  // channels 8 s + 2 g ..: ^ 32 s
   const unsigned vat = lds0 + G::HALF + 4 * g * ROW + ((c / 4) ^ G::swizzle(4 * g)) * 16 + (c % 4) * 4;  // channel tile i: ^ 64 i
 
-  const int64_t chunk = (a.work + 7) / 8;  // contiguous per XCD, as above
-  const int64_t chunk_end = min(a.work, ((int64_t)(blockIdx.x % 8) + 1) * chunk);
-  for (int64_t work = (int64_t)(blockIdx.x % 8) * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
+  const unsigned chunk = (a.work + 7) / 8;  // contiguous per XCD, as above
+  const unsigned chunk_end = min(a.work, (blockIdx.x % 8 + 1) * chunk);
+  for (unsigned work = blockIdx.x % 8 * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
     const SparseTile t(a, work);
     int token[2], sub[2];
 #pragma unroll

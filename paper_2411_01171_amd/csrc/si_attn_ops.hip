@@ -175,6 +175,8 @@ si_status enqueue_rope(const si_heads* q, const si_heads* k, const si_rope* r, i
 
 // ----------------------------------------------------------------------------- runs and blocks
 
+constexpr int64_t kGridMost = 1 << 20;  // workgroups of a launch; kernels walk longer lists
+
 // Sizes that the selection and the attention share.
 si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block, BlocksPlan* p) {
   if (q->dtype != k->dtype) return SI_ERR_DTYPE;
@@ -186,12 +188,12 @@ si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int
   p->runs = (q->N + q_block - 1) / q_block;
   p->blocks = (k->N + k_block - 1) / k_block;
   p->words = (p->blocks + 31) / 32;
-  // bitmap and workgroup counts stay well inside 64 bits and a grid
-  if ((double)q->B * k->heads * p->runs * (double)(p->words + 1) >= 1e12) return SI_ERR_SHAPE;
+  // kernels count lists, blocks and pieces of rows in 32 bits
+  const double lists = (double)q->B * (double)k->heads, most = 2147483648.0 - kGridMost;
+  if (lists * (double)p->runs * 16 >= most || lists * (double)p->blocks * 16 >= most) return SI_ERR_SHAPE;
+  if (lists * (double)p->runs * (double)(p->words + 1) >= 1e12) return SI_ERR_SHAPE;
   return SI_OK;
 }
-
-constexpr int64_t kGridMost = 1 << 20;  // workgroups of a launch; kernels walk longer lists
 
 // ----------------------------------------------------------------------------- selection
 
@@ -201,7 +203,7 @@ size_t select_bytes(const si_heads* q, const si_heads* k, const BlocksPlan& p) {
 }
 
 static MeansOf means_of(const si_heads* x, int64_t heads_kv, int64_t block, int64_t runs, int64_t chunks, const int32_t* len, double* out) {
-  return MeansOf{view_of(x), len, out, (int)x->N, (int)(x->heads / heads_kv), (int)block, (int)runs, x->B * runs * chunks};
+  return MeansOf{view_of(x), len, out, (int)x->N, (int)(x->heads / heads_kv), (int)block, (int)runs, (unsigned)(x->B * runs * chunks)};
 }
 
 si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan& p, int64_t q_block, int64_t k_block, int64_t keep,
@@ -216,7 +218,7 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
   m.chunks = (int)((k->heads * q->dim_head * heads_esize(q) / 16 + kMeanPieces - 1) / kMeanPieces);
   m.of[0] = means_of(q, k->heads, q_block, p.runs, m.chunks, q_len, qm);
   m.of[1] = means_of(k, k->heads, k_block, p.blocks, m.chunks, k_len, km);
-  const unsigned grid = (unsigned)std::min<int64_t>(m.of[0].work + m.of[1].work, kGridMost);
+  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)m.of[0].work + m.of[1].work, kGridMost);
   if (q->dtype == SI_F32) block_means_kernel<float><<<grid, kMeanPieces * kMeanSlices, 0, st>>>(m);
   else block_means_kernel<bf16><<<grid, kMeanPieces * kMeanSlices, 0, st>>>(m);
   SI_CHECK_LAUNCH();
@@ -232,8 +234,14 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
   auto launch = [&](auto cap, auto kpl, auto threads) {
     a.rows = std::min(16, cap.value / a.pitch);
     a.tiles = (int)((p.runs + a.rows - 1) / a.rows);
-    a.work = q->B * k->heads * a.tiles;
-    block_select_kernel<cap.value, kpl.value, threads.value><<<(unsigned)((std::min<int64_t>(a.work, kGridMost) + 7) / 8 * 8), threads.value, 0, st>>>(a);
+    a.work = (unsigned)(q->B * k->heads * a.tiles);
+    const unsigned grid = (unsigned)((std::min<int64_t>((int64_t)a.work, kGridMost) + 7) / 8 * 8);
+    switch ((a.d + 31) / 32) {
+      case 1: block_select_kernel<cap.value, kpl.value, threads.value, 1><<<grid, threads.value, 0, st>>>(a); break;
+      case 2: block_select_kernel<cap.value, kpl.value, threads.value, 2><<<grid, threads.value, 0, st>>>(a); break;
+      case 3: block_select_kernel<cap.value, kpl.value, threads.value, 3><<<grid, threads.value, 0, st>>>(a); break;
+      default: block_select_kernel<cap.value, kpl.value, threads.value, 4><<<grid, threads.value, 0, st>>>(a); break;
+    }
   };
   // the smallest store of scores that holds 16 runs, for as many workgroups on a CU as possible
   using std::integral_constant;
@@ -241,8 +249,8 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
   else if (p.blocks <= 128) launch(integral_constant<int, 16 * 130>(), integral_constant<int, 2>(), integral_constant<int, 256>());
   else if (p.blocks <= 256) launch(integral_constant<int, 16 * 258>(), integral_constant<int, 4>(), integral_constant<int, 256>());
   else if (p.blocks <= 512) launch(integral_constant<int, 16 * 514>(), integral_constant<int, 8>(), integral_constant<int, 512>());
-  else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>(), integral_constant<int, 1024>());
-  else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>(), integral_constant<int, 1024>());
+  else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>(), integral_constant<int, 512>());
+  else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>(), integral_constant<int, 512>());
   static_assert(16 * 1028 >= kSelectMaxBlocks + 2, "one run of the longest list");
   SI_CHECK_LAUNCH();
   return SI_OK;
@@ -258,7 +266,7 @@ si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, con
   const int d = (int)q->dim_head;
   p->ks = d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 80 ? 5 : d <= 96 ? 6 : 8;
   p->tiles_per_run = (rows + 32 * p->nw - 1) / (32 * p->nw);
-  if ((double)q->B * k->heads * b.runs * (double)p->tiles_per_run >= 1e12) return SI_ERR_SHAPE;
+  if ((double)q->B * k->heads * b.runs * (double)p->tiles_per_run >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
   p->tiles = q->B * k->heads * b.runs * p->tiles_per_run;
   const int64_t want = p->nw == 1 ? 1024 : 512;
   p->nsplit = 1;
@@ -271,7 +279,7 @@ si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, con
 
 template <typename T, int KS, int NW>
 static void launch_sparse(const SparseArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)((std::min<int64_t>(a.work, kGridMost) + 7) / 8 * 8);
+  const unsigned grid = (unsigned)((std::min<int64_t>((int64_t)a.work, kGridMost) + 7) / 8 * 8);
   if constexpr (sizeof(T) == 2) sparse_attn_bf16_kernel<KS, NW><<<grid, 64 * NW, 0, st>>>(a);
   else sparse_attn_f32_kernel<KS, NW><<<grid, 64 * NW, 0, st>>>(a);
 }
@@ -314,7 +322,7 @@ si_status enqueue_sparse(const si_heads* q, const si_heads* k, const si_heads* v
   a.q_block = (int)q_block; a.k_block = (int)k_block;
   a.runs = (int)b.runs; a.words = (int)b.words;
   a.tiles_per_run = (int)p.tiles_per_run;
-  a.work = p.work; a.nsplit = p.nsplit;
+  a.work = (unsigned)p.work; a.nsplit = p.nsplit;
   a.c = scale * 1.4426950408889634f;
   a.part = reinterpret_cast<float*>(ws);
   a.part_ml = reinterpret_cast<float2*>(a.part + (p.nsplit > 1 ? p.rows * p.nsplit * q->dim_head : 0));
