@@ -470,13 +470,15 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
 // serves two products; a result lane (c, g), g = lane / 16, holds column c and rows 4 g + j.  Those four keys are, register by
 // register, the column operand of four steps of the second product.  16-channel tiles: heads of 40 contract 40 and produce
 // 48 channels (32 x 32 tiles: 48 and 64).  Bound by the float32 matrix rate, 256 flop per clock and CU.
-template <int KS, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 4 || KS <= 4 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {
-  using G = SparseGeo<float, KS>;
+// D8: head channels / 8, exactly: the products of a stage are one block of instructions with its reads ahead of it.
+template <int D8, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {
+  constexpr int KS = (D8 + 1) / 2, KL = KS < 2 ? 2 : KS;  // channels in steps of 16: of the output, and of a row in LDS
+  using G = SparseGeo<float, KL>;
   constexpr int SK = G::SK, ROW = G::ROW;
   __shared__ __align__(1024) u32x4_t ring[G::NS * 2 * G::HALF / 16];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
-  StageLoads<float, KS, NW> loads;
+  StageLoads<float, KL, NW> loads;
   loads.setup(a, lds0);
   const int lane = loads.lane, c = lane % 16, g = lane / 16;
   const unsigned kat = lds0 + c * ROW + ((g / 2) ^ G::swizzle(c)) * 16 + (g % 2) * 8;  // channels 8 s + 2 g ..: ^ 32 s
@@ -494,15 +496,15 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || KS <= 4 ? 2 : 1) void sparse_at
     loads.begin(a, t);
     for (int i = 0; i < G::NS - 1; ++i) loads.issue(a, walk);
 
-    float2 qop[2][2 * KS];
+    float2 qop[2][D8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float* qrow = static_cast<const float*>(a.q) + t.b * a.qb + (int64_t)max(token[h], 0) * a.qn +
                           (int64_t)(t.hk * a.group + (token[h] < 0 ? 0 : sub[h])) * a.qh + 2 * g;
 #pragma unroll
-      for (int s = 0; s < 2 * KS; ++s) {
+      for (int s = 0; s < D8; ++s) {
         qop[h][s] = make_float2(0.f, 0.f);
-        if (8 * s < a.d && t.q_len > 0) qop[h][s] = *reinterpret_cast<const float2*>(qrow + 8 * s);
+        if (t.q_len > 0) qop[h][s] = *reinterpret_cast<const float2*>(qrow + 8 * s);
       }
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // the queries: nothing that the compiler tracks stays pending in the loop
@@ -525,19 +527,18 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || KS <= 4 ? 2 : 1) void sparse_at
 #pragma unroll
         for (int h = 0; h < 2; ++h) sc[u][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < 2 * KS; ++s)
-        if (8 * s < a.d) {
-          f32x2_t kf[2];
+      for (int s = 0; s < D8; ++s) {
+        f32x2_t kf[2];
 #pragma unroll
-          for (int u = 0; u < 2; ++u) kf[u] = lds_read<f32x2_t>(((kat + cslot) ^ (32 * s)) + 16 * u * ROW);
+        for (int u = 0; u < 2; ++u) kf[u] = lds_read<f32x2_t>(((kat + cslot) ^ (32 * s)) + 16 * u * ROW);
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int h = 0; h < 2; ++h)
-                sc[u][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u][j], j ? qop[h][s].y : qop[h][s].x, sc[u][h], 0, 0, 0);
-        }
+            for (int h = 0; h < 2; ++h)
+              sc[u][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u][j], j ? qop[h][s].y : qop[h][s].x, sc[u][h], 0, 0, 0);
+      }
       if (nkeys < SK) {
         const int lim = nkeys - 4 * g;
 #pragma unroll
@@ -548,6 +549,17 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || KS <= 4 ? 2 : 1) void sparse_at
             for (int j = 0; j < 4; ++j)
               if (16 * u + j >= lim) sc[u][h][j] = -INFINITY;
       }
+
+      // the first key tile's values are on their way while the exponentials are taken, the second's during its products
+      float vf[2][4][KS];
+      auto values = [&](int u) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < KS; ++i) vf[u][j][i] = lds_read<float>(((vat + cslot) ^ (G::swizzle(j) * 16) ^ (64 * i)) + (16 * u + j) * ROW);
+      };
+      values(0);
+      __builtin_amdgcn_sched_barrier(0);
 
       // ---- probabilities against the lazy reference maximum, as above
       float p[2][2][4], rs[2];
@@ -589,16 +601,16 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || KS <= 4 ? 2 : 1) void sparse_at
       lsum[1] += rs[1];
 
       // ---- O^T += V^T P^T: step (u, j) takes keys 16 u + 4 g + j
+      values(1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int i = 0; i < KS; ++i) {
-            const float vf = lds_read<float>(((vat + cslot) ^ (G::swizzle(j) * 16) ^ (64 * i)) + (16 * u + j) * ROW);
+          for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) oacc[h][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, p[u][h][j], oacc[h][i], 0, 0, 0);
-          }
+            for (int h = 0; h < 2; ++h) oacc[h][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[u][j][i], p[u][h][j], oacc[h][i], 0, 0, 0);
       cslot = cslot == (G::NS - 1) * 2 * G::HALF ? 0 : cslot + 2 * G::HALF;
     }
 #pragma unroll

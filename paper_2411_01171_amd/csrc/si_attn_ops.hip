@@ -263,8 +263,6 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
 si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, bool may_split, SparsePlan* p) {
   const int64_t rows = b.group * std::min<int64_t>(q_block, std::max<int64_t>(q->N, 1));
   p->nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  const int d = (int)q->dim_head;
-  p->ks = d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 80 ? 5 : d <= 96 ? 6 : 8;
   p->tiles_per_run = (rows + 32 * p->nw - 1) / (32 * p->nw);
   if ((double)q->B * k->heads * b.runs * (double)p->tiles_per_run >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
   p->tiles = q->B * k->heads * b.runs * p->tiles_per_run;
@@ -277,23 +275,32 @@ si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, con
   return SI_OK;
 }
 
-template <typename T, int KS, int NW>
-static void launch_sparse(const SparseArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)((std::min<int64_t>((int64_t)a.work, kGridMost) + 7) / 8 * 8);
-  if constexpr (sizeof(T) == 2) sparse_attn_bf16_kernel<KS, NW><<<grid, 64 * NW, 0, st>>>(a);
-  else sparse_attn_f32_kernel<KS, NW><<<grid, 64 * NW, 0, st>>>(a);
+// Calls f(integral_constant<d / 8>) for a head of d channels.
+template <int D8 = 1, class Fn>
+static void by_head(int d, Fn f) {
+  if constexpr (D8 <= 16) {
+    if (d == 8 * D8) f(std::integral_constant<int, D8>());
+    else by_head<D8 + 1>(d, f);
+  }
 }
+
 template <typename T>
 static void dispatch_sparse(const SparseArgs& a, const SparsePlan& p, hipStream_t st) {
+  const unsigned grid = (unsigned)((std::min<int64_t>((int64_t)a.work, kGridMost) + 7) / 8 * 8);
   auto by_width = [&](auto nw) {
     constexpr int NW = nw.value;
-    switch (p.ks) {
-      case 2: launch_sparse<T, 2, NW>(a, st); break;
-      case 3: launch_sparse<T, 3, NW>(a, st); break;
-      case 4: launch_sparse<T, 4, NW>(a, st); break;
-      case 5: launch_sparse<T, 5, NW>(a, st); break;
-      case 6: launch_sparse<T, 6, NW>(a, st); break;
-      default: launch_sparse<T, 8, NW>(a, st); break;
+    if constexpr (sizeof(T) == 4) {
+      by_head(a.d, [&](auto d8) { sparse_attn_f32_kernel<d8.value, NW><<<grid, 64 * NW, 0, st>>>(a); });
+    } else {
+      // steps of 16 channels; one form for 8 to 32 channels and one for 104 to 128
+      auto launch = [&](auto ks) { sparse_attn_bf16_kernel<ks.value, NW><<<grid, 64 * NW, 0, st>>>(a); };
+      const int ks = (a.d + 15) / 16;
+      if (ks <= 2) launch(std::integral_constant<int, 2>());
+      else if (ks == 3) launch(std::integral_constant<int, 3>());
+      else if (ks == 4) launch(std::integral_constant<int, 4>());
+      else if (ks == 5) launch(std::integral_constant<int, 5>());
+      else if (ks == 6) launch(std::integral_constant<int, 6>());
+      else launch(std::integral_constant<int, 8>());
     }
   };
   if (p.nw == 1) by_width(std::integral_constant<int, 1>());
