@@ -42,7 +42,7 @@ constexpr int vmcnt_imm(int n) { return (n & 0xF) | 0x70 | 0xF00 | ((n >> 4) << 
 constexpr float kSparseLow = -1e30f;  // reference maximum before the first key: below every score, and finite
 constexpr float kSparseTrigger = 256.f;
 
-// zero rows for keys past the end and channels past the head
+// zero rows for keys past the end
 static __device__ __align__(16) const unsigned kSparseZero[4] = {0, 0, 0, 0};
 
 // The key blocks of one run, as the first keys of stages of SK keys in ascending order.  Every wavefront walks the list
@@ -218,8 +218,9 @@ struct StageLoads {
   static_assert(G::LOADS % NW == 0, "every wavefront issues the same number of loads, the waits count them");
   unsigned lds0, slot;
   int lane, wave;
-  bool whole_rows;
-  unsigned koff[PER], voff[PER];  // load i: rows (wave + NW i) (64 / PR) .., lane l takes slot l % PR of row l / PR of them
+  // Load i: rows (wave + NW i) (64 / PR) .., lane l takes slot l % PR of row l / PR of them; slots of channels past the head
+  // receive the row's first piece, and whoever reads them does not use it.
+  unsigned koff[PER], voff[PER];
   const char *kbase, *vbase;
   int issued, last_keys;
 
@@ -227,10 +228,9 @@ struct StageLoads {
     lds0 = at;
     lane = threadIdx.x % kWave;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    whole_rows = a.d == G::PR * G::VEC;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int row = (wave + NW * i) * (64 / G::PR) + lane / G::PR, piece = (lane % G::PR) ^ G::swizzle(row);
+      const int row = (wave + NW * i) * (64 / G::PR) + lane / G::PR, at = (lane % G::PR) ^ G::swizzle(row), piece = at * G::VEC < a.d ? at : 0;
       koff[i] = (unsigned)(row * (int)a.kn + piece * G::VEC) * (unsigned)sizeof(T);  // the host keeps this inside 31 bits
       voff[i] = (unsigned)(row * (int)a.vn + piece * G::VEC) * (unsigned)sizeof(T);
     }
@@ -250,19 +250,18 @@ struct StageLoads {
     const char* ksrc = kbase + (int64_t)key0 * a.kn * (int64_t)sizeof(T);
     const char* vsrc = vbase + (int64_t)key0 * a.vn * (int64_t)sizeof(T);
     const unsigned dst = lds0 + slot + wave * 1024;
-    if (nkeys == G::SK && whole_rows) {
+    if (nkeys == G::SK) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(koff[i]), "s"(ksrc), "s"(dst + NW * i * 1024) : "memory");
         asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff[i]), "s"(vsrc), "s"(dst + G::HALF + NW * i * 1024) : "memory");
       }
-    } else {  // keys past the end and channels past the head as zeros
+    } else {  // keys past the end as zeros
       int l = lane;
-      asm volatile("" : "+v"(l));  // rows and pieces are formed here again: kept through the loop they cost registers
+      asm volatile("" : "+v"(l));  // rows are formed here again: kept through the loop they cost registers
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int row = (wave + NW * i) * (64 / G::PR) + l / G::PR, piece = (l % G::PR) ^ G::swizzle(row);
-        const bool in = piece * G::VEC < a.d && row < nkeys;
+        const bool in = (wave + NW * i) * (64 / G::PR) + l / G::PR < nkeys;
         const char* ks = in ? ksrc + koff[i] : reinterpret_cast<const char*>(kSparseZero);
         const char* vs = in ? vsrc + voff[i] : reinterpret_cast<const char*>(kSparseZero);
         asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ks), "s"(dst + NW * i * 1024) : "memory");
@@ -316,7 +315,8 @@ __device__ __forceinline__ void sparse_put_ml(const SparseArgs& a, const SparseT
 // would save 4 % at 57600 tokens), 16 conversions and 16 sums of pairs; and by power: in long launches the clock falls to
 // 1.9 GHz.  72x128 frame over a quarter of its keys 70 us (780 TFLOP/s), 57600 tokens over a tenth 1906 us (890).  Three
 // workgroups on a CU (two for wide heads) hide each other's waits; s_setprio around either half changes nothing.
-template <int KS, int NW>
+// PAD: d < 16 KS; what the keys' fragments hold past the head is made zero, as the queries are there.
+template <int KS, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_attn_bf16_kernel(SparseArgs a) {
   using G = SparseGeo<bf16, KS>;
   constexpr int SK = G::SK, ROW = G::ROW;
@@ -375,6 +375,13 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
 #pragma unroll
         for (int u = 0; u < 2; ++u) kf[s][u] = lds_read<u32x4_t>(((kat + cslot) ^ (32 * s)) + 32 * u * ROW);
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (PAD) {
+#pragma unroll
+        for (int s = KS == 2 ? 0 : KS == 8 ? 6 : KS - 1; s < KS; ++s)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            if (16 * s + 8 * g >= a.d) kf[s][u] = u32x4_t{0, 0, 0, 0};
+      }
       f32x16_t sc[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -466,13 +473,14 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
   }
 }
 
-// float32 throughout, on v_mfma_f32_16x16x4_f32: a wavefront's 32 rows are two column tiles, so that a key or value operand
-// serves two products; a result lane (c, g), g = lane / 16, holds column c and rows 4 g + j.  Those four keys are, register by
+// float32 throughout, on v_mfma_f32_16x16x4_f32: a wavefront's rows are H column tiles of 16; with two of them a key or value
+// operand serves two products, with one there are twice the wavefronts to hide each other's waits (runs of 64 rows, 64x64, heads
+// of 40: 121 -> 118 us).  A result lane (c, g), g = lane / 16, holds column c and rows 4 g + j.  Those four keys are, register by
 // register, the column operand of four steps of the second product.  16-channel tiles: heads of 40 contract 40 and produce
 // 48 channels (32 x 32 tiles: 48 and 64).  Bound by the float32 matrix rate, 256 flop per clock and CU.
 // D8: head channels / 8, exactly: the products of a stage are one block of instructions with its reads ahead of it.
-template <int D8, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {
+template <int D8, int NW, int H>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {
   constexpr int KS = (D8 + 1) / 2, KL = KS < 2 ? 2 : KS;  // channels in steps of 16: of the output, and of a row in LDS
   using G = SparseGeo<float, KL>;
   constexpr int SK = G::SK, ROW = G::ROW;
@@ -488,17 +496,17 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
   const unsigned chunk_end = min(a.work, (blockIdx.x % 8 + 1) * chunk);
   for (unsigned work = blockIdx.x % 8 * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
     const SparseTile t(a, work);
-    int token[2], sub[2];
+    int token[H], sub[H];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) token[h] = t.token(a, (t.tile * NW + loads.wave) * 32 + 16 * h + c, sub[h]);
+    for (int h = 0; h < H; ++h) token[h] = t.token(a, ((t.tile * NW + loads.wave) * H + h) * 16 + c, sub[h]);
     BlockWalk<SK> walk;
-    t.begin(a, NW * 32, walk);
+    t.begin(a, NW * H * 16, walk);
     loads.begin(a, t);
     for (int i = 0; i < G::NS - 1; ++i) loads.issue(a, walk);
 
-    float2 qop[2][D8];
+    float2 qop[H][D8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < H; ++h) {
       const float* qrow = static_cast<const float*>(a.q) + t.b * a.qb + (int64_t)max(token[h], 0) * a.qn +
                           (int64_t)(t.hk * a.group + (token[h] < 0 ? 0 : sub[h])) * a.qh + 2 * g;
 #pragma unroll
@@ -509,10 +517,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // the queries: nothing that the compiler tracks stays pending in the loop
 
-    f32x4_t oacc[2][KS];
-    float mref[2], lsum[2];
+    f32x4_t oacc[H][KS];
+    float mref[H], lsum[H];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < H; ++h) {
       mref[h] = kSparseLow;
       lsum[h] = 0.f;
 #pragma unroll
@@ -521,11 +529,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
     unsigned cslot = 0;
     for (int st = 0; st < loads.issued; ++st) {
       const int nkeys = loads.open(a, walk, st);
-      f32x4_t sc[2][2];  // [key tile][column tile]
+      f32x4_t sc[2][H];  // [key tile][column tile]
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) sc[u][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < H; ++h) sc[u][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < D8; ++s) {
         f32x2_t kf[2];
@@ -536,7 +544,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < H; ++h)
               sc[u][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u][j], j ? qop[h][s].y : qop[h][s].x, sc[u][h], 0, 0, 0);
       }
       if (nkeys < SK) {
@@ -544,7 +552,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               if (16 * u + j >= lim) sc[u][h][j] = -INFINITY;
@@ -562,10 +570,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
       __builtin_amdgcn_sched_barrier(0);
 
       // ---- probabilities against the lazy reference maximum, as above
-      float p[2][2][4], rs[2];
+      float p[2][H][4], rs[H];
       auto exponentiate = [&]() {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < H; ++h) {
           rs[h] = 0.f;
 #pragma unroll
           for (int u = 0; u < 2; ++u)
@@ -577,9 +585,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
         }
       };
       exponentiate();
-      if (__builtin_amdgcn_ballot_w64(!(rs[0] <= kSparseTrigger) || !(rs[1] <= kSparseTrigger)) != 0) {
+      if (__builtin_amdgcn_ballot_w64(!(rs[0] <= kSparseTrigger) || !(rs[H - 1] <= kSparseTrigger)) != 0) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < H; ++h) {
           float mx = sc[0][h][0];
 #pragma unroll
           for (int u = 0; u < 2; ++u)
@@ -597,8 +605,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
         }
         exponentiate();
       }
-      lsum[0] += rs[0];
-      lsum[1] += rs[1];
+#pragma unroll
+      for (int h = 0; h < H; ++h) lsum[h] += rs[h];
 
       // ---- O^T += V^T P^T: step (u, j) takes keys 16 u + 4 g + j
       values(1);
@@ -610,11 +618,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 || D8 <= 8 ? 2 : 1) void sparse_at
 #pragma unroll
           for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) oacc[h][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[u][j][i], p[u][h][j], oacc[h][i], 0, 0, 0);
+            for (int h = 0; h < H; ++h) oacc[h][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[u][j][i], p[u][h][j], oacc[h][i], 0, 0, 0);
       cslot = cslot == (G::NS - 1) * 2 * G::HALF ? 0 : cslot + 2 * G::HALF;
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < H; ++h) {
       lsum[h] += __shfl_xor(lsum[h], 16, kWave);
       lsum[h] += __shfl_xor(lsum[h], 32, kWave);
       if (token[h] >= 0) {

@@ -14,7 +14,7 @@ struct BlocksPlan {
 };
 
 struct SparsePlan {
-  int nw, nsplit;
+  int tile_rows, nsplit;
   int64_t tiles_per_run, tiles, work;
   int64_t rows;  // of all queries and heads
   size_t part_bytes;

@@ -258,15 +258,16 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
 
 // ----------------------------------------------------------------------------- attention over blocks
 
-// Wavefronts of a workgroup and shares of a run's blocks.  A run with up to 32 (64) rows takes one (two) wavefronts.  Blocks
-// are dealt out to several workgroups while there are fewer than two for every CU.
+// Rows of a workgroup and shares of a run's blocks.  bf16: 32 rows per wavefront, up to 128 of a run together.  float32: 16
+// per wavefront, 32 in runs of more than 64 rows.  Blocks are dealt out to several workgroups while there are fewer than two
+// for every CU.
 si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, bool may_split, SparsePlan* p) {
   const int64_t rows = b.group * std::min<int64_t>(q_block, std::max<int64_t>(q->N, 1));
-  p->nw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  p->tiles_per_run = (rows + 32 * p->nw - 1) / (32 * p->nw);
+  p->tile_rows = q->dtype == SI_F32 && rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  p->tiles_per_run = (rows + p->tile_rows - 1) / p->tile_rows;
   if ((double)q->B * k->heads * b.runs * (double)p->tiles_per_run >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
   p->tiles = q->B * k->heads * b.runs * p->tiles_per_run;
-  const int64_t want = p->nw == 1 ? 1024 : 512;
+  const int64_t want = p->tile_rows <= 32 ? 1024 : 512;
   p->nsplit = 1;
   if (may_split && p->tiles > 0 && p->tiles * 2 <= want) p->nsplit = (int)std::min<int64_t>(std::min<int64_t>(want / p->tiles, 64), std::max<int64_t>(1, b.blocks / 2));
   p->work = p->tiles * p->nsplit;
@@ -287,25 +288,33 @@ static void by_head(int d, Fn f) {
 template <typename T>
 static void dispatch_sparse(const SparseArgs& a, const SparsePlan& p, hipStream_t st) {
   const unsigned grid = (unsigned)((std::min<int64_t>((int64_t)a.work, kGridMost) + 7) / 8 * 8);
-  auto by_width = [&](auto nw) {
-    constexpr int NW = nw.value;
-    if constexpr (sizeof(T) == 4) {
-      by_head(a.d, [&](auto d8) { sparse_attn_f32_kernel<d8.value, NW><<<grid, 64 * NW, 0, st>>>(a); });
-    } else {
-      // steps of 16 channels; one form for 8 to 32 channels and one for 104 to 128
-      auto launch = [&](auto ks) { sparse_attn_bf16_kernel<ks.value, NW><<<grid, 64 * NW, 0, st>>>(a); };
-      const int ks = (a.d + 15) / 16;
-      if (ks <= 2) launch(std::integral_constant<int, 2>());
-      else if (ks == 3) launch(std::integral_constant<int, 3>());
-      else if (ks == 4) launch(std::integral_constant<int, 4>());
-      else if (ks == 5) launch(std::integral_constant<int, 5>());
-      else if (ks == 6) launch(std::integral_constant<int, 6>());
-      else launch(std::integral_constant<int, 8>());
-    }
-  };
-  if (p.nw == 1) by_width(std::integral_constant<int, 1>());
-  else if (p.nw == 2) by_width(std::integral_constant<int, 2>());
-  else by_width(std::integral_constant<int, 4>());
+  using std::integral_constant;
+  if constexpr (sizeof(T) == 4) {
+    by_head(a.d, [&](auto d8) {
+      if (p.tile_rows == 16) sparse_attn_f32_kernel<d8.value, 1, 1><<<grid, 64, 0, st>>>(a);
+      else if (p.tile_rows == 32) sparse_attn_f32_kernel<d8.value, 2, 1><<<grid, 128, 0, st>>>(a);
+      else if (p.tile_rows == 64) sparse_attn_f32_kernel<d8.value, 4, 1><<<grid, 256, 0, st>>>(a);
+      else sparse_attn_f32_kernel<d8.value, 4, 2><<<grid, 256, 0, st>>>(a);
+    });
+  } else {
+    // steps of 16 channels; one form for 8 to 32 channels and one for 104 to 128
+    auto launch_pad = [&](auto ks, auto pad) {
+      if (p.tile_rows == 32) sparse_attn_bf16_kernel<ks.value, 1, pad.value><<<grid, 64, 0, st>>>(a);
+      else if (p.tile_rows == 64) sparse_attn_bf16_kernel<ks.value, 2, pad.value><<<grid, 128, 0, st>>>(a);
+      else sparse_attn_bf16_kernel<ks.value, 4, pad.value><<<grid, 256, 0, st>>>(a);
+    };
+    auto launch = [&](auto ks) {
+      if (a.d < 16 * ks.value) launch_pad(ks, std::true_type());
+      else launch_pad(ks, std::false_type());
+    };
+    const int ks = (a.d + 15) / 16;
+    if (ks <= 2) launch(integral_constant<int, 2>());
+    else if (ks == 3) launch(integral_constant<int, 3>());
+    else if (ks == 4) launch(integral_constant<int, 4>());
+    else if (ks == 5) launch(integral_constant<int, 5>());
+    else if (ks == 6) launch(integral_constant<int, 6>());
+    else launch(integral_constant<int, 8>());
+  }
   if (a.nsplit > 1) {
     const int64_t rows = p.rows;
     sparse_join_kernel<T><<<(unsigned)std::min<int64_t>((rows + 3) / 4, kGridMost), 256, 0, st>>>(a, rows);

@@ -159,18 +159,22 @@ def test_rising_scores():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_scores_of_minus_infinity_weigh_nothing(dtype):
-    """Keys whose score is -inf stand in the first block, a whole block of them even; the others share the weight."""
-    q = np.zeros((1, 3, 1, 64), np.float32)
+@pytest.mark.parametrize("d", [8, 24, 40, 64, 72, 80, 88, 104, 112, 128])
+def test_scores_of_minus_infinity_weigh_nothing(dtype, d):
+    """Keys whose score is -inf stand in the first block, a whole block of them even; the others share the weight.  The
+    infinity is in a channel that a kernel could read again where a head is padded, times zero."""
+    q = np.zeros((1, 3, 1, d), np.float32)
     q[..., 0] = 1.0
-    k = np.zeros((1, 192, 1, 64), np.float32)
+    k = np.zeros((1, 192, 1, d), np.float32)
     k[0, :64, 0, 0] = -np.inf
     k[0, 64:100, 0, 0] = -np.inf
-    v = np.ones((1, 192, 1, 64), np.float32)
+    v = np.ones((1, 192, 1, d), np.float32)
     v[0, 100:146] = 3.0
-    out = torch.zeros(1, 3, 1, 64, device="cuda", dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q[..., 1:8] = 1.0  # a zero there would give 0 * inf in the definition as well
+    k[0, :100, 0, 1:8] = -np.inf
+    out = torch.zeros(1, 3, 1, d, device="cuda", dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
     _forward(strided(q, dtype, "rows"), strided(k, dtype, "rows"), strided(v, dtype, "rows"), 4, 64, None, out)
-    assert np.array_equal(host(out), np.full((1, 3, 1, 64), 2.0))
+    assert np.array_equal(host(out), np.full((1, 3, 1, d), 2.0))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
