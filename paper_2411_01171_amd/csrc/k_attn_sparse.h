@@ -139,7 +139,7 @@ struct BlockWalk {
 };
 
 // What all kernels share: where a head's rows lie in LDS.
-template <typename T, int KS>
+template <typename T, int KS, int NW>
 struct SparseGeo {
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr int SK = F32 ? 32 : 64;                            // keys of a stage
@@ -148,7 +148,9 @@ struct SparseGeo {
   static constexpr int PR = NP <= 4 ? 4 : NP <= 8 ? 8 : NP <= 16 ? 16 : 32;  // pieces of a row in LDS
   static constexpr int ROW = PR * 16;                                 // bytes
   static constexpr int HALF = SK * ROW;                               // bytes of a stage's keys; its values follow
-  static constexpr int NS = !F32 && HALF <= 8192 ? 3 : 2;             // stages in LDS
+  // Stages in LDS.  A wavefront on its own has no other that waits with it: two, and more workgroups (runs of 32 rows, heads of
+  // 64, 164 -> 142 us; one token against 16384 keys of 8 heads of 64, 39 -> 33 us).
+  static constexpr int NS = !F32 && HALF <= 8192 && NW > 1 ? 3 : 2;
   static constexpr int LOADS = HALF / 1024;                           // wave-wide loads of a stage's keys
 
   // Piece p of row r lies in slot p ^ swizzle(r) of its row.  LDS reads 256 bytes per clock.  Keys: the lanes of a clock read
@@ -213,7 +215,7 @@ struct SparseTile {
 // explicitly, the compiler would wait for all of them before the next LDS read.
 template <typename T, int KS, int NW>
 struct StageLoads {
-  using G = SparseGeo<T, KS>;
+  using G = SparseGeo<T, KS, NW>;
   static constexpr int PER = G::LOADS / NW;  // loads of a stage's keys per wavefront, and of its values
   static_assert(G::LOADS % NW == 0, "every wavefront issues the same number of loads, the waits count them");
   unsigned lds0, slot;
@@ -316,9 +318,12 @@ __device__ __forceinline__ void sparse_put_ml(const SparseArgs& a, const SparseT
 // 1.9 GHz.  72x128 frame over a quarter of its keys 70 us (780 TFLOP/s), 57600 tokens over a tenth 1906 us (890).  Three
 // workgroups on a CU (two for wide heads) hide each other's waits; s_setprio around either half changes nothing.
 // PAD: d < 16 KS; what the keys' fragments hold past the head is made zero, as the queries are there.
-template <int KS, int NW, bool PAD>
+// SPLIT 2: two wavefronts share 32 rows and take half of a stage's keys each, joined at the end: a run of 64 rows then has four
+// wavefronts on a CU for every stage in its LDS, not two (72x128 frame, runs of 64: 112 -> 79 us).
+template <int KS, int NW, bool PAD, int SPLIT>
 __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_attn_bf16_kernel(SparseArgs a) {
-  using G = SparseGeo<bf16, KS>;
+  constexpr int UT = 2 / SPLIT;  // 32-key tiles of a stage per wavefront
+  using G = SparseGeo<bf16, KS, NW>;
   constexpr int SK = G::SK, ROW = G::ROW;
   constexpr int OB = (KS + 1) / 2;  // 32-channel blocks of the output
   __shared__ __align__(1024) u32x4_t ring[G::NS * 2 * G::HALF / 16];
@@ -326,12 +331,13 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
   StageLoads<bf16, KS, NW> loads;
   loads.setup(a, lds0);
   const int lane = loads.lane, r = lane % 32, g = lane / 32;
+  const int rows_of = loads.wave % (NW / SPLIT), share = loads.wave / (NW / SPLIT);  // this wavefront's rows, and its half of the keys
   // LDS addresses of the first fragments; pieces further on are exclusive-ors (rows are aligned to their length), and so is
   // what a row further on changes in the slot
-  const unsigned kat = lds0 + r * ROW + (g ^ G::swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
+  const unsigned kat = lds0 + (32 * share + r) * ROW + (g ^ G::swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
   // step t of 16 keys: slots e < 4 of group g are keys 16 t + 4 g + e, the others 16 t + 8 + 4 g + e - 4; channel block i: ^ 64 i
   const int vr = 4 * g + (lane % 16) / 4;
-  const unsigned vat = lds0 + G::HALF + vr * ROW + ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ G::swizzle(vr)) * 16 + (lane % 2) * 8;
+  const unsigned vat = lds0 + G::HALF + (32 * share + vr) * ROW + ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ G::swizzle(vr)) * 16 + (lane % 2) * 8;
 
   // Work goes to the 8 XCDs in contiguous chunks, so that the keys and values of a head are fetched into one L2.
   const unsigned chunk = (a.work + 7) / 8;
@@ -339,9 +345,9 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
   for (unsigned work = blockIdx.x % 8 * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
     const SparseTile t(a, work);
     int sub;
-    const int token = t.token(a, (t.tile * NW + loads.wave) * 32 + r, sub);  // this lane's query row
+    const int token = t.token(a, (t.tile * (NW / SPLIT) + rows_of) * 32 + r, sub);  // this lane's query row
     BlockWalk<SK> walk;
-    t.begin(a, NW * 32, walk);
+    t.begin(a, NW / SPLIT * 32, walk);
     loads.begin(a, t);
     for (int i = 0; i < G::NS - 1; ++i) loads.issue(a, walk);
 
@@ -369,41 +375,41 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
       const int nkeys = loads.open(a, walk, st);
 
       // ---- scores of two tiles of 32 keys; all fragments are on their way before the first product
-      u32x4_t kf[KS][2];
+      u32x4_t kf[KS][UT];
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) kf[s][u] = lds_read<u32x4_t>(((kat + cslot) ^ (32 * s)) + 32 * u * ROW);
+        for (int u = 0; u < UT; ++u) kf[s][u] = lds_read<u32x4_t>(((kat + cslot) ^ (32 * s)) + 32 * u * ROW);
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (PAD) {
 #pragma unroll
         for (int s = KS == 2 ? 0 : KS == 8 ? 6 : KS - 1; s < KS; ++s)
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < UT; ++u)
             if (16 * s + 8 * g >= a.d) kf[s][u] = u32x4_t{0, 0, 0, 0};
       }
-      f32x16_t sc[2];
+      f32x16_t sc[UT];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < UT; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < UT; ++u)
           sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s][u]), __builtin_bit_cast(bf16x8_t, qop[s]), sc[u], 0, 0, 0);
       if (nkeys < SK) {
-        const int lim = nkeys - 4 * g;  // register e of tile u is key 32 u + 8 (e / 4) + e % 4 + 4 g
+        const int lim = nkeys - 32 * share - 4 * g;  // register e of tile u is key 32 u + 8 (e / 4) + e % 4 + 4 g
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < UT; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (32 * u + 8 * (e / 4) + e % 4 >= lim) sc[u][e] = -INFINITY;
       }
       // the values are on their way while the exponentials are taken
-      uint2 vlo[4][OB], vhi[4][OB];
+      uint2 vlo[2 * UT][OB], vhi[2 * UT][OB];
 #pragma unroll
-      for (int k16 = 0; k16 < 4; ++k16)
+      for (int k16 = 0; k16 < 2 * UT; ++k16)
 #pragma unroll
         for (int i = 0; i < OB; ++i) {
           vlo[k16][i] = lds_read_tr(((vat + cslot) ^ (64 * i)) + 16 * k16 * ROW);
@@ -416,11 +422,11 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
       // harmless in float32 and, relative as bf16 rounds, in bf16.  They are rounded to bf16, the matrix cores' type for V:
       // half a step of 2^-8 of each weight, which the sums over the keys average out; the row sum is of the rounded
       // values, those that weigh V.
-      u32x4_t pk[4];
+      u32x4_t pk[2 * UT];
       auto exponentiate = [&]() {
         float rs = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < UT; ++u)
 #pragma unroll
           for (int e = 0; e < 16; e += 2) {
             const unsigned w = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[u][e], a.c, -mref)), __builtin_amdgcn_exp2f(fmaf(sc[u][e + 1], a.c, -mref)));
@@ -433,7 +439,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
       if (__builtin_amdgcn_ballot_w64(!(rs <= kSparseTrigger)) != 0) {
         float mx = sc[0][0];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < UT; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[u][e]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * a.c;  // both halves of the row agree on the new reference
@@ -450,7 +456,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
 
       // ---- O^T += V^T P^T
 #pragma unroll
-      for (int k16 = 0; k16 < 4; ++k16)
+      for (int k16 = 0; k16 < 2 * UT; ++k16)
 #pragma unroll
         for (int i = 0; i < OB; ++i) {
           const u32x4_t vf{vlo[k16][i].x, vlo[k16][i].y, vhi[k16][i].x, vhi[k16][i].y};
@@ -459,7 +465,33 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
       cslot = cslot == (G::NS - 1) * 2 * G::HALF ? 0 : cslot + 2 * G::HALF;
     }
     lsum += __shfl_xor(lsum, 32, kWave);
-    if (token >= 0) {
+    if constexpr (SPLIT == 2) {
+      // the second half's wavefront leaves its output, maximum and sum in LDS, the first adds them to its own
+      constexpr int IMG = (OB * 16 + 2) * kWave;
+      static_assert(NW / 2 * IMG * 4 <= G::NS * 2 * G::HALF, "the outputs fit the ring");
+      float* img = reinterpret_cast<float*>(&ring[0]) + rows_of * IMG + lane;
+      __syncthreads();
+      if (share == 1) {
+#pragma unroll
+        for (int i = 0; i < OB; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) img[(16 * i + e) * kWave] = oacc[i][e];
+        img[OB * 16 * kWave] = mref;
+        img[(OB * 16 + 1) * kWave] = lsum;
+      }
+      __syncthreads();
+      if (share == 0) {
+        const float m2 = img[OB * 16 * kWave], top = fmaxf(mref, m2);
+        const float w1 = __builtin_amdgcn_exp2f(mref - top), w2 = __builtin_amdgcn_exp2f(m2 - top);
+        lsum = lsum * w1 + img[(OB * 16 + 1) * kWave] * w2;
+        mref = top;
+#pragma unroll
+        for (int i = 0; i < OB; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) oacc[i][e] = oacc[i][e] * w1 + img[(16 * i + e) * kWave] * w2;
+      }
+    }
+    if (token >= 0 && share == 0) {
 #pragma unroll
       for (int i = 0; i < OB; ++i)
 #pragma unroll
@@ -482,7 +514,7 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
 template <int D8, int NW, int H>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {
   constexpr int KS = (D8 + 1) / 2, KL = KS < 2 ? 2 : KS;  // channels in steps of 16: of the output, and of a row in LDS
-  using G = SparseGeo<float, KL>;
+  using G = SparseGeo<float, KL, NW>;
   constexpr int SK = G::SK, ROW = G::ROW;
   __shared__ __align__(1024) u32x4_t ring[G::NS * 2 * G::HALF / 16];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);

@@ -299,9 +299,9 @@ static void dispatch_sparse(const SparseArgs& a, const SparsePlan& p, hipStream_
   } else {
     // steps of 16 channels; one form for 8 to 32 channels and one for 104 to 128
     auto launch_pad = [&](auto ks, auto pad) {
-      if (p.tile_rows == 32) sparse_attn_bf16_kernel<ks.value, 1, pad.value><<<grid, 64, 0, st>>>(a);
-      else if (p.tile_rows == 64) sparse_attn_bf16_kernel<ks.value, 2, pad.value><<<grid, 128, 0, st>>>(a);
-      else sparse_attn_bf16_kernel<ks.value, 4, pad.value><<<grid, 256, 0, st>>>(a);
+      if (p.tile_rows == 32) sparse_attn_bf16_kernel<ks.value, 1, pad.value, 1><<<grid, 64, 0, st>>>(a);
+      else if (p.tile_rows == 64) sparse_attn_bf16_kernel<ks.value, 4, pad.value, 2><<<grid, 256, 0, st>>>(a);
+      else sparse_attn_bf16_kernel<ks.value, 4, pad.value, 1><<<grid, 256, 0, st>>>(a);
     };
     auto launch = [&](auto ks) {
       if (a.d < 16 * ks.value) launch_pad(ks, std::true_type());
