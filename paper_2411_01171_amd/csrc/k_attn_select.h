@@ -238,7 +238,7 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
         if (!exact) need_equal = a.keep - tally([&](unsigned long long k) { return k > least; });
       }
       int equal = 0;
-      auto put = [&](int j0, unsigned long long k) {
+      auto taken = [&](unsigned long long k) {
         bool take = exact ? k >= least : k > least;
         if (!exact) {
           const unsigned long long eqs = __builtin_amdgcn_ballot_w64(k == least);
@@ -246,15 +246,21 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
           take = take || (k == least && rank < need_equal);
           equal += __popcll(eqs);
         }
-        const unsigned long long bits = __builtin_amdgcn_ballot_w64(take);
-        if (lane < 2 && j0 / 32 + lane < a.words) out[j0 / 32 + lane] = (unsigned)(bits >> (32 * lane));
+        return __builtin_amdgcn_ballot_w64(take);
       };
-      if constexpr (KPL > 0) {
+      if constexpr (KPL > 0) {  // lane w collects word w
+        unsigned word = 0;
 #pragma unroll
-        for (int i = 0; i < KPL; ++i)
-          if (2 * i < a.words) put(i * kWave, held[i]);
+        for (int i = 0; i < KPL; ++i) {
+          const unsigned long long bits = taken(held[i]);
+          if (lane / 2 == i) word = (unsigned)(lane % 2 ? bits >> 32 : bits);
+        }
+        if (lane < a.words) out[lane] = word;
       } else {
-        for (int j0 = 0; j0 < 32 * a.words; j0 += kWave) put(j0, j0 + lane < nblk ? key[j0 + lane] : 0ull);
+        for (int j0 = 0; j0 < 32 * a.words; j0 += kWave) {
+          const unsigned long long bits = taken(j0 + lane < nblk ? key[j0 + lane] : 0ull);
+          if (lane < 2 && j0 / 32 + lane < a.words) out[j0 / 32 + lane] = (unsigned)(bits >> (32 * lane));
+        }
       }
     }
     __syncthreads();
