@@ -356,28 +356,27 @@ def _heads(t) -> _Heads:
     return _Heads(t.data_ptr(), _dtype_code(t), B, N, h, d, sb, sn, sh)
 
 
-class _on_device:
-    """The operands' device as the current one, and the stream to enqueue on, for one call."""
-
-    def __init__(self, stream, first, *others):
-        import torch
-        index = first.get_device()  # -1: not on a GPU
-        for t in others:
-            if t is not None and t.get_device() != index:
-                index = -1
-        if index < 0:
-            raise ValueError("all tensors must be on one GPU")
-        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
-        self.stream = _stream_ptr(torch.cuda.current_stream(index) if stream is None else stream)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(name: str, stream, tensors, args) -> None:
+    """Calls the entry point with `args` and a stream of the tensors' device (its current one unless given), on that device."""
+    import torch
+    index = tensors[0].get_device()  # -1: not on a GPU
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            index = -1
+    if index < 0:
+        raise ValueError("all tensors must be on one GPU")
+    if stream is None:
+        st = torch._C._cuda_getCurrentRawStream(index) or None  # torch.cuda.current_stream(index).cuda_stream, without the object
+    else:
+        st = _stream_ptr(stream)
+    fn = getattr(lib(), name)
+    if index == torch.cuda.current_device():
+        status = fn(*args, st)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, st)
+    if status != 0:
+        raise SiError(status, name)
 
 
 def _lengths(t, B: int) -> Optional[int]:
@@ -406,12 +405,10 @@ def si_rope_forward(q, k, rope: Rope, q_out, k_out, first: int = 0, stream=None)
     for g in rope.gains:
         if g is not None and (g.shape[0] != q.shape[3] or g.dtype != q.dtype):
             raise ValueError("gains must be [dim_head] in the operands' dtype")
-    qd, qo = _heads(q), _heads(q_out)
-    kd, ko = (None if t is None else C.byref(_heads(t)) for t in (k, k_out))
-    with _on_device(stream, q, k, q_out, k_out, *rope.gains) as st:
-        status = lib().si_rope_forward(C.byref(qd), kd, C.byref(rope.struct), first, C.byref(qo), ko, st)
-    if status != 0:
-        raise SiError(status, "si_rope_forward")
+    kd = None if k is None else C.byref(_heads(k))
+    ko = None if k_out is None else C.byref(_heads(k_out))
+    _call("si_rope_forward", stream, (q, k, q_out, k_out, *rope.gains),
+          (C.byref(_heads(q)), kd, C.byref(rope.struct), first, C.byref(_heads(q_out)), ko))
 
 
 def si_attn_block_words(n_keys: int, k_block: int) -> int:
@@ -426,13 +423,9 @@ def si_attn_select_workspace_bytes(q, k, q_block: int, k_block: int) -> int:
 def si_attn_select(q, k, q_block: int, k_block: int, keep: int, blocks, workspace, q_len=None, k_len=None, stream=None) -> None:
     """Writes the `keep` best key blocks of every run of q_block queries as bitmaps: blocks int32
     [B, k heads, runs, si_attn_block_words(N of k, k_block)]."""
-    qd, kd = _heads(q), _heads(k)
     ql, kl, bits = _lengths(q_len, q.shape[0]), _lengths(k_len, q.shape[0]), _bitmap(blocks, q, k, q_block, k_block)
-    with _on_device(stream, q, k, blocks, workspace, q_len, k_len) as st:
-        status = lib().si_attn_select(C.byref(qd), C.byref(kd), q_block, k_block, keep, ql, kl, bits, workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), st)
-    if status != 0:
-        raise SiError(status, "si_attn_select")
+    _call("si_attn_select", stream, (q, k, blocks, workspace, q_len, k_len),
+          (C.byref(_heads(q)), C.byref(_heads(k)), q_block, k_block, keep, ql, kl, bits, workspace.data_ptr(), workspace.nbytes))
 
 
 def si_attn_sparse_workspace_bytes(q, k, q_block: int, k_block: int) -> int:
@@ -444,14 +437,10 @@ def si_attn_sparse_forward(q, k, v, q_block: int, k_block: int, blocks, out, wor
                            k_len=None, stream=None) -> None:
     """Attention of runs of q_block queries over the key blocks in their bitmaps (blocks None: over every key).
     scale: 1/sqrt(dim_head) unless given."""
-    qd, kd, vd, od = _heads(q), _heads(k), _heads(v), _heads(out)
     ql, kl, bits = _lengths(q_len, q.shape[0]), _lengths(k_len, q.shape[0]), _bitmap(blocks, q, k, q_block, k_block)
-    with _on_device(stream, q, k, v, blocks, out, workspace, q_len, k_len) as st:
-        status = lib().si_attn_sparse_forward(C.byref(qd), C.byref(kd), C.byref(vd), q_block, k_block,
-                                              q.shape[3] ** -0.5 if scale is None else scale, ql, kl, bits, C.byref(od),
-                                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), st)
-    if status != 0:
-        raise SiError(status, "si_attn_sparse_forward")
+    _call("si_attn_sparse_forward", stream, (q, k, v, blocks, out, workspace, q_len, k_len),
+          (C.byref(_heads(q)), C.byref(_heads(k)), C.byref(_heads(v)), q_block, k_block, q.shape[3] ** -0.5 if scale is None else scale,
+           ql, kl, bits, C.byref(_heads(out)), workspace.data_ptr(), workspace.nbytes))
 
 
 class AttnOptions:

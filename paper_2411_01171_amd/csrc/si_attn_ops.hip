@@ -157,7 +157,11 @@ si_status enqueue_rope(const si_heads* q, const si_heads* k, const si_rope* r, i
   for (int ax = 0; ax < 3; ++ax) {
     a.origin[ax] = r->origin[ax];
     a.step[ax] = r->step[ax];
-    for (int i = 0; i < r->pairs[ax]; ++i) a.freq[p++] = std::pow(r->theta, -(double)i / r->pairs[ax]) * 0.15915494309189533577;
+    if (r->pairs[ax] == 0) continue;
+    // powers by products of 64-bit significands: nearer than a power function in float64, and one of them instead of many
+    const long double ratio = std::pow((long double)r->theta, -1.0L / r->pairs[ax]);
+    long double f = 0.159154943091895335768883763372514362L;  // 1 / (2 pi)
+    for (int i = 0; i < r->pairs[ax]; ++i, f *= ratio) a.freq[p++] = (double)f;
   }
   for (; p < kRopeMaxPairs; ++p) a.freq[p] = 0.0;
   // A workgroup takes every head of its tokens, so that their sines are computed once, unless that leaves CUs idle.
@@ -249,7 +253,7 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
   else if (p.blocks <= 128) launch(integral_constant<int, 16 * 130>(), integral_constant<int, 2>(), integral_constant<int, 256>());
   else if (p.blocks <= 256) launch(integral_constant<int, 16 * 258>(), integral_constant<int, 4>(), integral_constant<int, 256>());
   else if (p.blocks <= 512) launch(integral_constant<int, 16 * 514>(), integral_constant<int, 8>(), integral_constant<int, 512>());
-  else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>(), integral_constant<int, 512>());
+  else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>(), integral_constant<int, 1024>());
   else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>(), integral_constant<int, 512>());
   static_assert(16 * 1028 >= kSelectMaxBlocks + 2, "one run of the longest list");
   SI_CHECK_LAUNCH();
