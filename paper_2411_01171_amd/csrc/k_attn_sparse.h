@@ -371,7 +371,10 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
 #pragma unroll
       for (int e = 0; e < 16; ++e) oacc[i][e] = 0.f;
     unsigned cslot = 0;
-    for (int st = 0; st < loads.issued; ++st) {
+    // a wavefront whose rows all lie past the run's end loads its share of the stages, no more
+    if (__builtin_amdgcn_ballot_w64(token >= 0) == 0)
+      for (int st = 0; st < loads.issued; ++st) loads.open(a, walk, st);
+    else for (int st = 0; st < loads.issued; ++st) {
       const int nkeys = loads.open(a, walk, st);
 
       // ---- scores of two tiles of 32 keys; all fragments are on their way before the first product
@@ -559,7 +562,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_attn_f32_kern
       for (int i = 0; i < KS; ++i) oacc[h][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     unsigned cslot = 0;
-    for (int st = 0; st < loads.issued; ++st) {
+    // a wavefront whose rows all lie past the run's end loads its share of the stages, no more
+    if (__builtin_amdgcn_ballot_w64(max(token[0], token[H - 1]) >= 0) == 0)
+      for (int st = 0; st < loads.issued; ++st) loads.open(a, walk, st);
+    else for (int st = 0; st < loads.issued; ++st) {
       const int nkeys = loads.open(a, walk, st);
       f32x4_t sc[2][H];  // [key tile][column tile]
 #pragma unroll
