@@ -375,7 +375,10 @@ si_status si_rope_forward(const si_heads* q, const si_heads* k, const si_rope* r
  *
  * q_len, k_len (device int32 [B], may be NULL = N): tokens of every batch entry
  * that count, clamped to [0, N].  What lies behind them is never read as a value,
- * so it may hold anything. */
+ * so it may hold anything.
+ *
+ * stride_n of keys and values is below 2^23 elements; lists, row tiles and blocks
+ * of a call are counted in 31 bits (SI_ERR_SHAPE). */
 
 /* Words of one list; 0 if the arguments are invalid or there are no keys.  Host-only. */
 int64_t si_attn_block_words(int64_t n_keys, int64_t k_block);

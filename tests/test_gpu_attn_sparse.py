@@ -237,6 +237,55 @@ def test_offsets_beyond_32_bits():
     assert (np.abs(host(out) - ref) <= tol).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_no_keys_give_zeros_and_no_queries_give_nothing(dtype):
+    q, k = torch.randn(2, 5, 4, 64, device="cuda").to(dtype), torch.randn(2, 100, 2, 64, device="cuda").to(dtype)
+    for words in (None, torch.empty(2, 2, 1, 0, dtype=torch.int32, device="cuda")):
+        out = torch.full_like(q, 7.0)
+        _forward(q, k[:, :0], k[:, :0], 8, 64, words, out)
+        assert (out == 0).all()
+        none = q[:, :0]
+        _forward(none, k, k, 8, 64, None, none.clone())
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    """Calls that overlap in time: one token over a long cache (dealt out and joined) on two streams."""
+    k, v = (torch.randn(1, 20000, 2, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    qs = [torch.randn(1, 1, 8, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    refs, outs = [torch.empty_like(q) for q in qs], [torch.empty_like(q) for q in qs]
+    for q, ref in zip(qs, refs):
+        _forward(q, k, v, 1, 64, None, ref)
+    ws = [torch.empty(si.si_attn_sparse_workspace_bytes(qs[0], k, 1, 64), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i in range(2):
+            si.si_attn_sparse_forward(qs[i], k, v, 1, 64, None, outs[i], ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, r) for o, r in zip(outs, refs))
+
+
+def test_rotation_and_selection_beyond_32_bits():
+    """Rows that lie more than 2^31 elements behind the first one, rotated in place and pooled."""
+    wide = torch.zeros(1, 70000, 480, 64, device="cuda", dtype=torch.bfloat16)
+    x = wide[:, :, 479:]
+    x[0, -64:] = torch.randn(64, 1, 64, device="cuda")
+    near = x[:, -64:].clone()
+    rope = si.Rope((70000, 1, 1), (32, 0, 0))
+    si.si_rope_forward(near, None, rope, near, None, first=70000 - 64)
+    si.si_rope_forward(x, None, rope, x, None)
+    assert torch.equal(x[:, -64:], near) and not x[:, :-64].any()
+    x[0, 64 * 1092:64 * 1092 + 16] = 5.0  # the one block with a mean towards the query: (16 * 5 - 16 * 1) / 64
+    words = torch.zeros(1, 1, 1, si.si_attn_block_words(70000, 64), dtype=torch.int32, device="cuda")
+    x[0, -64:] = -1.0
+    q = torch.ones(1, 1, 1, 64, device="cuda", dtype=torch.bfloat16)
+    ws = torch.empty(si.si_attn_select_workspace_bytes(q, x, 1, 64), dtype=torch.uint8, device="cuda")
+    si.si_attn_select(q, x, 1, 64, 1, words, ws)
+    want = torch.zeros(1, 1, 1, 1094, dtype=torch.bool)
+    want[..., 1092] = True
+    assert np.array_equal(words.cpu().numpy(), oracle.pack_blocks_ref(want.numpy()))
+
+
 def test_rotate_select_attend_together():
     """The three operators one after the other on the rows of one projection, as an attention layer over video tokens calls
     them.  The features are clusters, so that the selection has margins that a rounding of q and k cannot bridge."""
