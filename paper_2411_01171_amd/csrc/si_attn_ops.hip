@@ -247,14 +247,17 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
       default: block_select_kernel<cap.value, kpl.value, threads.value, 4><<<grid, threads.value, 0, st>>>(a); break;
     }
   };
-  // the smallest store of scores that holds 16 runs, for as many workgroups on a CU as possible
+  // The smallest store of scores that holds 16 runs, for as many workgroups on a CU as possible, and a wavefront for every run;
+  // lists of up to 32 blocks have too little work for that many (32x32 frames, 16 blocks: 22.3 us with 512 threads, 25.0 with
+  // 1024; 64 blocks 13.0 and 12.4, 144 blocks 20.8 and 19.1, 900 blocks 139 and 134).
   using std::integral_constant;
-  if (p.blocks <= 64) launch(integral_constant<int, 16 * 66>(), integral_constant<int, 1>(), integral_constant<int, 256>());
-  else if (p.blocks <= 128) launch(integral_constant<int, 16 * 130>(), integral_constant<int, 2>(), integral_constant<int, 256>());
-  else if (p.blocks <= 256) launch(integral_constant<int, 16 * 258>(), integral_constant<int, 4>(), integral_constant<int, 256>());
-  else if (p.blocks <= 512) launch(integral_constant<int, 16 * 514>(), integral_constant<int, 8>(), integral_constant<int, 512>());
+  if (p.blocks <= 32) launch(integral_constant<int, 16 * 34>(), integral_constant<int, 1>(), integral_constant<int, 512>());
+  else if (p.blocks <= 64) launch(integral_constant<int, 16 * 66>(), integral_constant<int, 1>(), integral_constant<int, 1024>());
+  else if (p.blocks <= 128) launch(integral_constant<int, 16 * 130>(), integral_constant<int, 2>(), integral_constant<int, 1024>());
+  else if (p.blocks <= 256) launch(integral_constant<int, 16 * 258>(), integral_constant<int, 4>(), integral_constant<int, 1024>());
+  else if (p.blocks <= 512) launch(integral_constant<int, 16 * 514>(), integral_constant<int, 8>(), integral_constant<int, 1024>());
   else if (p.blocks <= 1024) launch(integral_constant<int, 16 * 1026>(), integral_constant<int, 16>(), integral_constant<int, 1024>());
-  else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>(), integral_constant<int, 512>());
+  else launch(integral_constant<int, 16 * 1028>(), integral_constant<int, 0>(), integral_constant<int, 1024>());
   static_assert(16 * 1028 >= kSelectMaxBlocks + 2, "one run of the longest list");
   SI_CHECK_LAUNCH();
   return SI_OK;
