@@ -31,7 +31,7 @@ struct RopeArgs {
   int heads_per_wg;          // a workgroup's share of the heads (blockIdx.y)
   int pairs, end_f, end_y;   // all pairs; pairs [0, end_f) turn with the frame, [end_f, end_y) with the row
   int tokens_per_wg;         // kRopeThreads / (d / 8)
-  float eps;
+  float eps, inv_d;          // inv_d: 1 / d
   double origin[3], step[3];
   double freq[kRopeMaxPairs];  // revolutions per position
 };
@@ -63,6 +63,8 @@ __device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = r.v[i / 4][i % 4];
 }
+__device__ __forceinline__ void ones8(Raw8<bf16>& r) { r.v = u32x4_t{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}; }
+__device__ __forceinline__ void ones8(Raw8<float>& r) { r.v[0] = r.v[1] = f32x4_t{1.f, 1.f, 1.f, 1.f}; }
 template <bool ONE> __device__ __forceinline__ void store8(bf16* p, int c0, int c1, const float (&y)[8]) {
   unsigned w[4];
 #pragma unroll
@@ -76,6 +78,11 @@ template <bool ONE> __device__ __forceinline__ void store8(bf16* p, int c0, int 
 template <bool ONE> __device__ __forceinline__ void store8(float* p, int c0, int c1, const float (&y)[8]) {
   *reinterpret_cast<f32x4_t*>(p + c0) = f32x4_t{y[0], y[1], y[2], y[3]};
   *reinterpret_cast<f32x4_t*>(p + c1) = f32x4_t{y[4], y[5], y[6], y[7]};
+}
+
+// v of the lane that a data-parallel primitive names, added to v
+template <int CTRL> __device__ __forceinline__ float add_dpp(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 
 // HALVES: pair p is channels (p, pairs + p), else (2p, 2p + 1).  The channels behind the pairs pass through.
@@ -106,14 +113,15 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
       sincospif(2.f * (float)(rev - rint(rev)), &sn[i], &cs[i]);
     }
   }
-  float gq[8], gk[8];
+  Raw8<T> gq, gk;  // as they lie in memory: half the registers for bf16
   if constexpr (NORM) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int ch = i < 4 ? c0 + i : c1 + i - 4;
-      gq[i] = param_or(static_cast<const T*>(a.q_gain), ch, 1.f);
-      gk[i] = param_or(static_cast<const T*>(a.k_gain), ch, 1.f);
-    }
+    auto gain = [&](const void* p, Raw8<T>& g) {
+      if (!p) ones8(g);
+      else if (HALVES && turned) load8<false>(static_cast<const T*>(p), c0, c1, g);
+      else load8<true>(static_cast<const T*>(p), c0, c1, g);
+    };
+    gain(a.q_gain, gq);
+    gain(a.k_gain, gk);
   }
   const int h_end = min(a.heads, (int)(blockIdx.y + 1) * a.heads_per_wg);
   int flip = 0;
@@ -141,13 +149,24 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
         for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
         part[u] = s;
       }
-      sums[flip][threadIdx.x] = part;
-      __syncthreads();
-      f32x4_t all{0.f, 0.f, 0.f, 0.f};
-      if (live)
-        for (int i = 0; i < nchunk; ++i) all += sums[flip][slot * nchunk + i];
+      f32x4_t all = part;
+      if ((nchunk & (nchunk - 1)) == 0) {  // a head's threads are neighbouring lanes, 1 to 16 of a row
 #pragma unroll
-      for (int u = 0; u < kRopeHeads; ++u) inv[u] = 1.f / sqrtf(all[u] / (float)a.d + a.eps);
+        for (int u = 0; u < kRopeHeads; ++u) {
+          if (nchunk > 1) all[u] = add_dpp<0xB1>(all[u]);   // lane ^ 1
+          if (nchunk > 2) all[u] = add_dpp<0x4E>(all[u]);   // lane ^ 2
+          if (nchunk > 4) all[u] = add_dpp<0x141>(all[u]);  // the other half of 8
+          if (nchunk > 8) all[u] = add_dpp<0x140>(all[u]);  // the other half of 16
+        }
+      } else {
+        sums[flip][threadIdx.x] = part;
+        __syncthreads();
+        all = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (live)
+          for (int i = 0; i < nchunk; ++i) all += sums[flip][slot * nchunk + i];
+      }
+#pragma unroll
+      for (int u = 0; u < kRopeHeads; ++u) inv[u] = rsqrtf(fmaf(all[u], a.inv_d, a.eps));
     }
     if (!live) continue;
 #pragma unroll
@@ -158,8 +177,10 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
       float x[8], y[8];
       unpack8(raw[u], x);
       if constexpr (NORM) {
+        float gain[8];
+        unpack8(is_q ? gq : gk, gain);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= inv[u] * (is_q ? gq[i] : gk[i]);
+        for (int i = 0; i < 8; ++i) x[i] *= inv[u] * gain[i];
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {

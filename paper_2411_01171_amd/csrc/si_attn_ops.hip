@@ -152,6 +152,7 @@ si_status enqueue_rope(const si_heads* q, const si_heads* k, const si_rope* r, i
   a.end_f = r->pairs[0];
   a.end_y = r->pairs[0] + r->pairs[1];
   a.eps = r->norm_eps;
+  a.inv_d = 1.f / (float)a.d;
   a.tokens_per_wg = kRopeThreads / (a.d / 8);
   int p = 0;
   for (int ax = 0; ax < 3; ++ax) {
