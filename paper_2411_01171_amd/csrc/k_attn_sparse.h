@@ -314,9 +314,11 @@ __device__ __forceinline__ void sparse_put_ml(const SparseArgs& a, const SparseT
 //
 // Bound by the vector ALUs and the matrix cores together: per 32 rows x 64 keys and head of 64, 512 clocks of MFMA and, beside
 // them, 32 exponentials (8 clocks each), 32 fma (the scale stays in float32: folded into q before a second rounding of q it
-// would save 4 % at 57600 tokens), 16 conversions and 16 sums of pairs; and by power: in long launches the clock falls to
-// 1.9 GHz.  72x128 frame over a quarter of its keys 70 us (780 TFLOP/s), 57600 tokens over a tenth 1906 us (890).  Three
-// workgroups on a CU (two for wide heads) hide each other's waits; s_setprio around either half changes nothing.
+// would save 4 % at 57600 tokens), 16 conversions and 16 sums of pairs; the two hardly overlap, whatever the number of
+// wavefronts (four per SIMD, sharing rows in pairs, 1958 us at 57600 tokens against 1858 with three); and by power: in long
+// launches the clock falls to 1.8 GHz.  72x128 frame over a quarter of its keys 67 us (809 TFLOP/s, 10 of them before the first
+// product and behind the last), 57600 tokens over a tenth 1858 us (914); a library product of 8192^3 reaches 1136.  Heads of
+// 128: 870 to 1030.  s_setprio around either half changes nothing.
 // PAD: d < 16 KS; what the keys' fragments hold past the head is made zero, as the queries are there.
 // SPLIT 2: two wavefronts share 32 rows and take half of a stage's keys each, joined at the end: a run of 64 rows then has four
 // wavefronts on a CU for every stage in its LDS, not two (72x128 frame, runs of 64: 112 -> 79 us).
@@ -512,7 +514,8 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
 // operand serves two products, with one there are twice the wavefronts to hide each other's waits (runs of 64 rows, 64x64, heads
 // of 40: 121 -> 118 us).  A result lane (c, g), g = lane / 16, holds column c and rows 4 g + j.  Those four keys are, register by
 // register, the column operand of four steps of the second product.  16-channel tiles: heads of 40 contract 40 and produce
-// 48 channels (32 x 32 tiles: 48 and 64).  Bound by the float32 matrix rate, 256 flop per clock and CU.
+// 48 channels (32 x 32 tiles: 48 and 64).  Bound by the float32 matrix rate, 256 flop per clock and CU: heads of 64 and 128
+// run at 120 TFLOP/s (a library product of 8192^3 at 153), heads of 40 at 104 of their own and 113 with the padded channels.
 // D8: head channels / 8, exactly: the products of a stage are one block of instructions with its reads ahead of it.
 template <int D8, int NW, int H>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {

@@ -9,7 +9,11 @@
 //
 // Bound by HBM: every head is read and written once.  A thread owns eight channels (four pairs) of one token and walks the
 // heads of q and k: the sines of a token are computed once for all of them, and the loads of kRopeHeads heads are in
-// flight together.
+// flight together.  25 frames of 72x128, two batch entries, 5 heads of 64 (1180 MB in and out): 219 us (5.4 TB/s; a copy of
+// 2 GiB reaches 4.9), channel halves 238, with the norm 216 and 237; float32, 14 frames of 45x50, 8 heads of 80 (323 MB) 72 us.
+// The norm's sums over a head's threads go by lane primitives where those are 1, 2, 4, 8 or 16 lanes of a row, else by LDS;
+// 1 / sqrt is the hardware's (one step of float32), and the gains stay as they lie in memory: both took the vector ALUs from
+// 79 % of the cycles (halves: 267 us).  One 16x16 frame takes the kernel 4.4 us and its call 9, on the host.
 #pragma once
 #include "si_common.h"
 
