@@ -402,7 +402,9 @@ si_status si_attn_select(const si_heads* q, const si_heads* k, int64_t q_block, 
 /* out[b, n, h] = sum_j softmax_j(scale * <q[b, n, h], k[b, j, hk]>) v[b, j, hk], j over the counted tokens of
  * the blocks in the list of n's run (blocks NULL: of every block), hk = h / (q->heads / k->heads).
  * A listed block without a counted token adds nothing; a row whose list leaves no
- * key gives zeros; rows at and behind q_len are left as they were.
+ * key, or only scores of -infinity, gives zeros; NaN or +infinity among the scores
+ * of a row makes it NaN; rows at and behind q_len are left as they were.  Finite
+ * scores times scale are at most 1e9 in magnitude.
  * scale > 0.  q, k, v and out have one dtype; v is shaped like k, out like q.  No
  * element of out may lie on one of q, k or v.  bf16 operands: scores, maxima, sums
  * and outputs in float32, probabilities rounded to bf16 for the second product;

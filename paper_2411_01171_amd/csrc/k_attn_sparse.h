@@ -293,9 +293,9 @@ __device__ __forceinline__ void sparse_put(const SparseArgs& a, const SparseTile
     *reinterpret_cast<f32x4_t*>(a.part + share * a.d + ch) = o;
     return;
   }
-  const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+  const float inv = 1.f / lsum;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) o[j] = lsum > 0.f ? o[j] * inv : 0.f;  // a row without keys gives zero
+  for (int j = 0; j < 4; ++j) o[j] = lsum == 0.f ? 0.f : o[j] * inv;  // a row without keys gives zero; a sum that is NaN stays one
   T* dst = static_cast<T*>(a.o) + t.b * a.ob + (int64_t)token * a.on + (int64_t)h * a.oh + ch;
   if constexpr (sizeof(T) == 2) {
     if (a.o_frag) dst = static_cast<T*>(a.o) + act_offset((int64_t)t.b * a.Nq + token, h * a.d + ch, a.o_frag);
@@ -714,9 +714,9 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(SparseArgs a, int64_t 
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], step, kWave);
     if (which != 0 || quad >= quads) continue;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = 1.f / l;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = l > 0.f ? o[j] * inv : 0.f;
+    for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : o[j] * inv;
     T* dst = static_cast<T*>(a.o) + b * a.ob + token * a.on + (int64_t)h * a.oh + 4 * quad;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
     else *reinterpret_cast<f32x4_t*>(dst) = o;

@@ -178,6 +178,35 @@ def test_scores_of_minus_infinity_weigh_nothing(dtype, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_block", [1, 20, 64, 128])
+@pytest.mark.parametrize("keys", [128, 640])  # one workgroup per tile; a tile's blocks dealt out to several
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_counted_values_that_are_not_finite_show_in_their_rows(dtype, q_block, keys, value):
+    """NaN, or infinity that makes a score +infinity: NaN in every row that counts it and in no other."""
+    rng = np.random.default_rng(17)
+    q, k, v = (draw(rng, (1, n, 2, 64), dtype) for n in (200, keys, keys))
+    q[0, :, 1, 3] = np.abs(q[0, :, 1, 3]) + 1
+    kept = rng.random((1, 2, -(-200 // q_block), keys // 64)) < 0.5
+    kept[:, :, :, 0] = True
+    bad_q, bad_k = q.copy(), k.copy()
+    bad_q[0, 77, 0, 5] = value    # one query of head 0
+    bad_k[0, 100, 1, 3] = value   # one key of head 1, in block 1
+    with np.errstate(invalid="ignore"):
+        ref, spread, mass = oracle.sparse_attention_ref(bad_q, bad_k, v, kept, q_block, 64)
+    nan = np.isnan(ref)
+    rows = nan[0].all(axis=-1)
+    assert (nan.any(axis=-1)[0] == rows).all() and rows[:, 0].nonzero()[0].tolist() == [77]
+    assert (rows[:, 1] == np.repeat(kept[0, 1, :, 1], q_block)[:200]).all()
+    words = torch.from_numpy(oracle.pack_blocks_ref(kept)).to("cuda")
+    out = strided(np.zeros(q.shape, np.float32), dtype, "rows")
+    _forward(*(strided(t, dtype, "rows") for t in (bad_q, bad_k, v)), q_block, 64, words, out)
+    got = host(out)
+    assert (np.isnan(got) == nan).all()
+    tol = attention_bound(q, k, spread, mass, ref, dtype, 0.125, keys)
+    assert (np.abs(got - ref)[~nan] <= tol[~nan]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_not_finite_where_no_list_looks(dtype):
     rng = np.random.default_rng(4)
     q, k, v = (torch.from_numpy(draw(rng, (1, 256, 1, 64), dtype)).to("cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32) for _ in range(3))
