@@ -345,7 +345,7 @@ typedef struct {
  * sqrt(mean of its squares + norm_eps) and multiplied by q_gain / k_gain (device,
  * [dim_head] in the operands' type, NULL = one); norm_eps < 0: it is not.
  * Angles are formed in float64, everything else in float32 with one rounding.
- * |origin| and |step| * extent are at most 1e12. */
+ * |origin| and |step| * extent are at most 1e12 (theta < 1: 1e12 theta). */
 typedef enum { SI_ROPE_INTERLEAVED = 0, SI_ROPE_HALVES = 1 } si_rope_layout;
 typedef struct {
   int64_t extent[3];
@@ -360,7 +360,8 @@ typedef struct {
  * of every batch entry is grid point first + n; first + N must lie inside the
  * grid.  k may have another number of heads than q; B, N, dim_head and dtype are
  * common.  An output may be its own input (in place); otherwise no element of an
- * output may lie on one of an input or of the other output. */
+ * output may lie on one of an input, of the other output or of a gain.
+ * B * N * dim_head is at most 2^33. */
 si_status si_rope_forward(const si_heads* q, const si_heads* k, const si_rope* rope, int64_t first, si_heads* q_out,
                           si_heads* k_out, void* stream);
 

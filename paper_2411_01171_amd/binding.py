@@ -463,8 +463,8 @@ def si_block_forward_attn(x, weights: BlockWeights, ctx, attn: AttnOptions, out,
     """si_block_forward_ex of a spatial block whose self-attention is the one that `attn` describes."""
     if attn.rope is not None:
         for g in attn.rope.gains:
-            if g is not None and (g.shape[0] != weights.struct.dim_head or g.dtype != x.dtype):
-                raise ValueError("gains must be [dim_head] in the feature's dtype")
+            if g is not None and (g.shape[0] != weights.struct.dim_head or g.dtype != x.dtype or g.device != x.device):
+                raise ValueError("gains must be [dim_head] in the feature's dtype, on its device")
     xd, od = _tensor5(x), _tensor5(out)
     pc, _keep = _pctx(ctx)
     st = lib().si_block_forward_attn(C.byref(xd), C.byref(weights.struct), pc, C.byref(attn.struct), C.byref(od), axis, slice_len,

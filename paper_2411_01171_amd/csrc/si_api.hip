@@ -1257,6 +1257,9 @@ static si_status check_forward(const si_tensor5* x, const si_block_weights* w, c
   if (si::ranges_overlap(workspace, p.total_bytes, out->ptr, xbytes) ||
       si::ranges_overlap(workspace, p.total_bytes, x->ptr, xbytes))
     return SI_ERR_ARG;
+  if (attn && attn->rope &&
+      (si::rope_gain_in(attn->rope, p.d, p.esize, workspace, p.total_bytes) || si::rope_gain_in(attn->rope, p.d, p.esize, out->ptr, xbytes)))
+    return SI_ERR_ARG;
   return SI_OK;
 }
 

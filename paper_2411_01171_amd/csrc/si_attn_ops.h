@@ -21,6 +21,7 @@ struct SparsePlan {
 };
 
 si_status check_rope(const si_rope* r, int d);
+bool rope_gain_in(const si_rope* r, int d, int esize, const void* p, size_t bytes);
 si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block, BlocksPlan* p);
 si_status plan_sparse(const si_heads* q, const si_heads* k, int64_t q_block, const BlocksPlan& b, bool may_split, SparsePlan* p);
 size_t select_bytes(const si_heads* q, const si_heads* k, const BlocksPlan& p);

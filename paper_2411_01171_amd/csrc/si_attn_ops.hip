@@ -100,16 +100,17 @@ si_status check_rope(const si_rope* r, int d) {
   if (!r) return SI_ERR_NULL;
   int64_t pairs = 0;
   double tokens = 1.0;
+  if (!(r->theta > 0.0) || !std::isfinite(r->theta)) return SI_ERR_ARG;
+  const double most = 1e12 * std::min(1.0, r->theta);  // frequencies are at most max(1, 1 / theta)
   for (int i = 0; i < 3; ++i) {
     if (r->extent[i] < 1 || r->extent[i] > INT32_MAX || r->pairs[i] < 0 || r->pairs[i] > d / 2) return SI_ERR_SHAPE;
     tokens *= (double)r->extent[i];
     pairs += r->pairs[i];
     // further out, a position times a frequency has no digits left behind the point
-    if (!(std::fabs(r->origin[i]) <= 1e12) || !(std::fabs(r->step[i]) * (double)r->extent[i] <= 1e12)) return SI_ERR_ARG;
+    if (!(std::fabs(r->origin[i]) <= most) || !(std::fabs(r->step[i]) * (double)r->extent[i] <= most)) return SI_ERR_ARG;
   }
   if (tokens > (double)(INT32_MAX - (1 << 22))) return SI_ERR_SHAPE;
   if (pairs < 1 || pairs % 4 || 2 * pairs > d) return SI_ERR_SHAPE;
-  if (!(r->theta > 0.0) || !std::isfinite(r->theta)) return SI_ERR_ARG;
   if (r->layout != SI_ROPE_INTERLEAVED && r->layout != SI_ROPE_HALVES) return SI_ERR_ARG;
   if (!std::isfinite(r->norm_eps)) return SI_ERR_ARG;
   if (r->norm_eps >= 0.f) {
@@ -127,6 +128,14 @@ static void launch_rope(const RopeArgs& a, bool halves, bool norm, dim3 grid, hi
     if (norm) rope_kernel<T, false, true><<<grid, kRopeThreads, 0, st>>>(a);
     else rope_kernel<T, false, false><<<grid, kRopeThreads, 0, st>>>(a);
   }
+}
+
+// Whether a gain that the norm reads (d elements of esize bytes) has a byte in [p, p + bytes).
+bool rope_gain_in(const si_rope* r, int d, int esize, const void* p, size_t bytes) {
+  if (r->norm_eps < 0.f) return false;
+  for (const void* g : {r->q_gain, r->k_gain})
+    if (g && ranges_overlap(g, (size_t)d * (size_t)esize, p, bytes)) return true;
+  return false;
 }
 
 // Operands and descriptor have been checked; k and ko may be NULL.
@@ -385,6 +394,8 @@ si_status si_rope_forward(const si_heads* q, const si_heads* k, const si_rope* r
       if (!(i == j && si::same_heads(in[j], out[i])) && !si::heads_apart(in[j], out[i])) return SI_ERR_ARG;
       if (i != j && !si::heads_apart(out[i], out[j])) return SI_ERR_ARG;
     }
+    const int es = si::heads_esize(q);
+    if (!si::heads_empty(out[i]) && si::rope_gain_in(rope, (int)q->dim_head, es, out[i]->ptr, (size_t)si::heads_extent(out[i]) * es)) return SI_ERR_ARG;
   }
   return si::enqueue_rope(q, k, rope, first, q_out, k_out, static_cast<hipStream_t>(stream));
 }
@@ -457,7 +468,7 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
   if (v->B != k->B || v->N != k->N || v->heads != k->heads || v->dim_head != k->dim_head) return SI_ERR_SHAPE;
   if (v->N > 1 && v->stride_n >= (1 << 23)) return SI_ERR_SHAPE;
   if (out->B != q->B || out->N != q->N || out->heads != q->heads || out->dim_head != q->dim_head) return SI_ERR_SHAPE;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return SI_ERR_ARG;
+  if (!(scale > 0.f) || !(scale <= 1e38f)) return SI_ERR_ARG;  // times log2(e) it is a float32
   const size_t need = p.part_bytes + 256, bits = blocks ? (size_t)(q->B * k->heads * b.runs * b.words) * 4 : 0;
   if (!workspace) return SI_ERR_NULL;
   if ((reinterpret_cast<uintptr_t>(q_len) & 3u) || (reinterpret_cast<uintptr_t>(k_len) & 3u) || (reinterpret_cast<uintptr_t>(blocks) & 3u) ||

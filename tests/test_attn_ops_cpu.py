@@ -202,6 +202,31 @@ def test_binding_refuses_what_it_cannot_describe():
         si.si_attn_select(x, x, 0, 64, 1, words, ws)
 
 
+def test_gains_under_an_output():
+    """A gain that the call would overwrite while other workgroups read it."""
+    size = 2 * 300 * 4 * 64 * 2
+    for at in (2 * FAR, 2 * FAR + size - 128, 3 * FAR + 4096):
+        for name in ("q_gain", "k_gain"):
+            assert rope_call(r=rope(norm_eps=1e-6, **{name: BASE + at})) == ARG, (at, name)
+    x, out = B._Tensor5(BASE, B.SI_BF16, 2, 64, 4, 8, 8), B._Tensor5(BASE + FAR, B.SI_BF16, 2, 64, 4, 8, 8)
+    ctx = B._Context(BASE + 2 * FAR, B.SI_BF16, 2, 5, 16)
+    w = B._Weights()
+    w.kind, w.heads, w.dim_head, w.gn_groups, w.gn_eps, w.ln_eps, w.add_sin_pe = B.SI_BLOCK_SPATIAL, 2, 32, 8, 1e-6, 1e-5, 0
+    for name in B.WEIGHT_FIELDS:
+        setattr(w, name, BASE + 3 * FAR)
+    for gain in (WS + 1024, BASE + FAR + 64):
+        r = rope(pairs=(4, 4, 8), extent=(4, 8, 8), norm_eps=1e-6, k_gain=gain)
+        attn = B._AttnOptions(C.pointer(r), 32, 64, 1)
+        assert si.lib().si_block_forward_attn(C.byref(x), C.byref(w), C.byref(ctx), C.byref(attn), C.byref(out), B.SI_AXIS_F, 1, WS, 1 << 40,
+                                              0, None) == ARG
+
+
+def test_angles_and_scales_that_float_cannot_hold():
+    assert rope_call(r=rope(theta=1e-3, origin=(2e9, 0, 0))) == ARG and rope_call(r=rope(theta=1e-3, step=(1, 2e8, 1))) == ARG
+    assert rope_call(r=rope(theta=5e-324)) == ARG
+    assert sparse(scale=3e38) == ARG
+
+
 # ------------------------------------------------------------------------------------------------ the oracle
 
 def test_oracle_rotation_is_relative_and_keeps_lengths():
