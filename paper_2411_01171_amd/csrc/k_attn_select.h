@@ -7,11 +7,14 @@
 // Everything behind the loads is float64: which block is the last one kept can hang on any digit of its score, and the
 // result is discrete.  The means are bound by HBM: every query and key is read once, 57600 tokens of 10 heads of 64, two batch
 // entries (295 MB), in 50 us (5.9 TB/s).  The scores take 2 d flop per (run, block) at some 60 TFLOP/s (450 runs x 900 blocks x
-// 20 heads: 16 us of matrix cores); the second kernel's 85 us there are latency: one workgroup fills a CU's LDS with the scores
-// of 16 runs, about 40 us go to fetching means from the L2 and 40 to the search for the threshold.  Means laid out as the
-// matrix cores' fragments made that kernel 15 us shorter and the first one 7 longer, and calls of one frame 6 % slower.
+// 20 heads: 16 us of matrix cores); the second kernel's 75 us there are latency: one workgroup fills a CU's LDS with the scores
+// of 16 runs, about 40 us go to fetching means from the L2 and 30 to the search for the threshold.  Means laid out as the
+// matrix cores' fragments made that kernel 15 us shorter and the first one 7 longer, and calls of one frame 6 % slower; means of
+// the next blocks fetched ahead of the products made it 10 us longer.
 #pragma once
 #include "k_rope.h"
+
+#include <type_traits>
 
 namespace si {
 
@@ -108,39 +111,39 @@ __device__ __forceinline__ unsigned long long order_key(double x) {
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
-// The largest T of 32-bit words with at least `need` values >= T, found from the top bits on; count(c) = number of values >= c.
-// Stops early, with `exact`, when exactly `need` values are >= the prefix.  BITS at a time: 2 where a count is nearly all
-// latency (a few ballots), 1 where it is work.  (Candidates interpolated from the counts, half as many, cost more than they save.)
-template <int BITS, class Count>
-__device__ __forceinline__ unsigned kth_word(int need, Count count, bool& exact) {
-  unsigned t = 0;
-  exact = false;
-  for (int bit = 32 - BITS; bit >= 0; bit -= BITS) {
-    int n[1 << BITS];
+// Narrows [lo, hi) to the largest T with count(T) = (number of values >= T) >= need, where count(lo) = n_lo >= need > n_hi =
+// count(hi).  Ends with hi = lo + 1, or as soon as count(lo) is `need`, or when no more than `few` values lie in [lo, hi).
+// WAYS parts per step: 4 where a count is nearly all latency (a few ballots), 2 where it is work.
+template <int WAYS, class U, class Count>
+__device__ __forceinline__ void narrow(U& lo, U& hi, int& n_lo, int& n_hi, int need, int few, Count count) {
+  while (hi - lo > 1 && n_lo != need && n_lo - n_hi > few) {
+    const U part = hi - lo > WAYS ? (hi - lo) / WAYS : 1;
+    int n[WAYS];
 #pragma unroll
-    for (int i = 1; i < 1 << BITS; ++i) n[i] = count(t | ((unsigned)i << bit));
-    unsigned up = 0;
+    for (int i = 1; i < WAYS; ++i) n[i] = count(lo + part * i);  // past the end: too few
+    const U base = lo;
 #pragma unroll
-    for (int i = 1; i < 1 << BITS; ++i)  // counts fall with i
-      if (n[i] >= need) {
-        up = (unsigned)i << bit;
-        exact = n[i] == need;
-      }
-    t |= up;
-    if (exact) break;
+    for (int i = 1; i < WAYS; ++i)  // counts fall with i
+      if (n[i] >= need) { lo = base + part * i; n_lo = n[i]; }
+#pragma unroll
+    for (int i = WAYS - 1; i > 0; --i)
+      if (n[i] < need) { hi = base + part * i; n_hi = n[i]; }
   }
-  return t;
 }
 
-// Sum over the wavefront's lanes by data-parallel primitives, in a scalar register.
-__device__ __forceinline__ int lanes_sum(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // from lane - 1, - 2, - 4, - 8 of a row of 16
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last lane of row 0 to row 1, of row 2 to row 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
-  return __builtin_amdgcn_readlane(v, 63);
+// v of all lanes of the wavefront joined (identity 0) by data-parallel primitives, in a scalar register.
+template <class Join>
+__device__ __forceinline__ unsigned lanes_join(unsigned v, Join join) {
+  auto step = [&](auto ctrl, auto rows) { v = join(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl.value, rows.value, 0xf, rows.value == 0xf)); };
+  using std::integral_constant;
+  using All = integral_constant<int, 0xf>;
+  step(integral_constant<int, 0x111>(), All());  // from lane - 1, - 2, - 4, - 8 of a row of 16
+  step(integral_constant<int, 0x112>(), All());
+  step(integral_constant<int, 0x114>(), All());
+  step(integral_constant<int, 0x118>(), All());
+  step(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());  // the last lane of row 0 to row 1, of row 2 to row 3
+  step(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());  // lane 31 to rows 2 and 3
+  return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // CAP: scores (float64) of a workgroup in LDS.  KPL: keys of a run per lane in registers (64 KPL >= blocks), or 0: read from
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
       const int run = run0 + row;
       if (run >= a.runs) break;
       unsigned* out = a.out + (pair * a.runs + run) * a.words;
-      const unsigned long long* key = keys + row * a.pitch;
+      unsigned long long* key = keys + row * a.pitch;
       const bool none = (int64_t)run * a.q_block >= q_len;
       if (none || nblk <= a.keep) {  // nothing, or all
         for (int w = lane; w < a.words; w += kWave) {
@@ -225,20 +228,56 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
         } else {
           for (int j = lane; j < nblk; j += kWave) n += pred(key[j]) ? 1 : 0;
         }
-        return lanes_sum(n);
+        return (int)lanes_join((unsigned)n, [](unsigned x, unsigned y) { return x + y; });
       };
-      bool exact;
-      constexpr int BITS = KPL > 0 && KPL <= 4 ? 2 : 1;
-      const unsigned hi = kth_word<BITS>(a.keep, [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); }, exact);
-      unsigned long long least = (unsigned long long)hi << 32;  // everything >= least is kept, except some of the equal ones
+      // The upper words first, from eight binades below the largest on: most lists have their threshold there.  (From zero on,
+      // by the bits of a threshold, all candidates counted to the end: 134 us against 124 for 450 runs x 900 blocks x 20 heads.)
+      unsigned top = 0;
+      if constexpr (KPL > 0) {
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) top = max(top, (unsigned)(held[i] >> 32));
+      } else {
+        for (int j = lane; j < nblk; j += kWave) top = max(top, (unsigned)(key[j] >> 32));
+      }
+      top = lanes_join(top, [](unsigned x, unsigned y) { return max(x, y); });
+      constexpr unsigned kBinades = 8u << 20;
+      unsigned lo = 0, hi = top + 1;  // top is at most the infinity's
+      int n_lo = nblk, n_hi = 0;
+      auto upper = [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); };
+      const unsigned first = top > kBinades ? top - kBinades : top / 2 + 1;
+      const int n = upper(first);
+      if (n >= a.keep) { lo = first; n_lo = n; }
+      else { hi = first; n_hi = n; }
+      constexpr int WAYS = KPL > 0 && KPL <= 4 ? 4 : 2;
+      narrow<WAYS>(lo, hi, n_lo, n_hi, a.keep, KPL > 1 ? kWave : 0, upper);
+      unsigned long long least = (unsigned long long)lo << 32;  // everything >= least is kept, except some of the equal ones
+      bool exact = n_lo == a.keep;
       int need_equal = 0;  // of the values == least, when not exact
       if (!exact) {
-        const int above = tally([&](unsigned long long k) { return (unsigned)(k >> 32) > hi; });
-        const unsigned lo = kth_word<BITS>(
-            a.keep - above,
-            [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) == hi && (unsigned)k >= c; }); }, exact);
-        least |= lo;
-        if (!exact) need_equal = a.keep - tally([&](unsigned long long k) { return k > least; });
+        unsigned long long end = (unsigned long long)hi << 32;
+        if (KPL > 0 && n_lo - n_hi <= kWave) {  // one candidate per lane: a count is a ballot
+          unsigned long long mine = 0;
+          if constexpr (KPL == 1) {
+            mine = held[0] >= least && held[0] < end ? held[0] : 0ull;
+          } else if constexpr (KPL > 0) {
+            int at = 0;
+#pragma unroll
+            for (int i = 0; i < KPL; ++i) {  // the run's scores in LDS are in registers: their place is free
+              const bool in = held[i] >= least && held[i] < end;
+              const unsigned long long ins = __builtin_amdgcn_ballot_w64(in);
+              if (in) key[at + __popcll(ins & ((1ull << lane) - 1ull))] = held[i];
+              at += __popcll(ins);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (lane < at) mine = key[lane];
+          }
+          const int above = n_hi;
+          narrow<4>(least, end, n_lo, n_hi, a.keep, 0, [&](unsigned long long c) { return above + __popcll(__builtin_amdgcn_ballot_w64(mine >= c)); });
+        } else {  // many of one upper word
+          narrow<WAYS>(least, end, n_lo, n_hi, a.keep, 0, [&](unsigned long long c) { return tally([&](unsigned long long k) { return k >= c; }); });
+        }
+        exact = n_lo == a.keep;
+        need_equal = a.keep - n_hi;
       }
       int equal = 0;
       auto taken = [&](unsigned long long k) {

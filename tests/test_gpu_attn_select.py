@@ -106,6 +106,29 @@ def test_scores_that_differ_in_the_last_digits_only():
         assert np.array_equal(got, oracle.pack_blocks_ref((order >= 20 - keep)[None, None, None]))
 
 
+@pytest.mark.parametrize("kind", ["wide", "negative", "one_far_above", "one_upper_word", "equal", "two_values"])
+@pytest.mark.parametrize("blocks", [20, 50, 100, 200, 400, 1000, 1500])
+def test_distributions_of_scores(kind, blocks):
+    """Blocks of equal keys (value, 0, ...) against queries (1, 0, ...), (-1, 0, ...) and (2, 0, ...): scores known exactly."""
+    rng = np.random.default_rng(blocks)
+    value = {"wide": rng.standard_normal(blocks) * 2.0 ** rng.integers(-60, 60, blocks),
+             "negative": -1 - rng.random(blocks),
+             "one_far_above": np.where(np.arange(blocks) == blocks // 2, 1e30, rng.standard_normal(blocks)),
+             "one_upper_word": 1 + rng.integers(0, 8, blocks) * 2.0 ** -23,  # float64's upper 32 bits agree
+             "equal": np.full(blocks, 0.75),
+             "two_values": rng.integers(0, 2, blocks) * 1.0}[kind].astype(np.float32)
+    k = np.zeros((1, blocks * 64, 1, 8), np.float32)
+    k[0, :, 0, 0] = np.repeat(value, 64)
+    q = np.zeros((1, 3, 1, 8), np.float32)
+    q[0, :, 0, 0] = 1, -1, 2
+    dq, dk = strided(q, "f32", "rows"), strided(k, "f32", "rows")
+    for keep in (1, blocks // 3, blocks - 1):
+        kept = np.zeros((1, 1, 3, blocks), bool)
+        for i in range(3):
+            kept[0, 0, i, np.lexsort((np.arange(blocks), -(value.astype(np.float64) * q[0, i, 0, 0])))[:keep]] = True
+        assert np.array_equal(_select(dq, dk, 1, 64, keep), oracle.pack_blocks_ref(kept)), keep
+
+
 def test_scores_that_are_not_finite():
     q = np.ones((1, 1, 1, 8), np.float32)
     k = np.zeros((1, 64 * 6, 1, 8), np.float32)
