@@ -208,13 +208,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_mfma_kernel(Att
   auto issue_full = [&]() {
 #pragma unroll
     for (int i = 0; i < PER / 2; ++i) {
-      // assembly for the same reason as in WeightPipe::issue: completion is awaited explicitly
-      asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(kvoff), "s"(kcur[i]), "s"(islot + loff[i]) : "memory");
+      load_to_lds(kvoff, kcur[i], islot + loff[i]);
       kcur[i] += kstride;
     }
 #pragma unroll
     for (int i = 0; i < PER / 2; ++i) {
-      asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vvoff), "s"(vcur[i]), "s"(islot + loff[PER / 2 + i]) : "memory");
+      load_to_lds(vvoff, vcur[i], islot + loff[PER / 2 + i]);
       vcur[i] += vstride;
     }
     next_slot();
@@ -234,7 +233,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_mfma_kernel(Att
         k0 = k0 < a.Nkp - 8 ? k0 : a.Nkp - 8;
         src = reinterpret_cast<const bf16*>(vb) + (int64_t)(32 * (((id - 8) / 2) % 2) + r) * a.Nkp + k0;
       }
-      asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(islot + loff[i]) : "memory");
+      load_to_lds(src, islot + loff[i]);
     }
     next_slot();
   };

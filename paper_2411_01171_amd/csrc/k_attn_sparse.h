@@ -211,8 +211,7 @@ struct SparseTile {
   }
 };
 
-// The stages of a workgroup's list on their way to LDS, by direct global->LDS loads in assembly: their completion is awaited
-// explicitly, the compiler would wait for all of them before the next LDS read.
+// The stages of a workgroup's list on their way to LDS, by direct global->LDS loads whose completion is awaited explicitly.
 template <typename T, int KS, int NW>
 struct StageLoads {
   using G = SparseGeo<T, KS, NW>;
@@ -255,8 +254,8 @@ struct StageLoads {
     if (nkeys == G::SK) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(koff[i]), "s"(ksrc), "s"(dst + NW * i * 1024) : "memory");
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff[i]), "s"(vsrc), "s"(dst + G::HALF + NW * i * 1024) : "memory");
+        load_to_lds(koff[i], ksrc, dst + NW * i * 1024);
+        load_to_lds(voff[i], vsrc, dst + G::HALF + NW * i * 1024);
       }
     } else {  // keys past the end as zeros
       int l = lane;
@@ -266,8 +265,8 @@ struct StageLoads {
         const bool in = (wave + NW * i) * (64 / G::PR) + l / G::PR < nkeys;
         const char* ks = in ? ksrc + koff[i] : reinterpret_cast<const char*>(kSparseZero);
         const char* vs = in ? vsrc + voff[i] : reinterpret_cast<const char*>(kSparseZero);
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ks), "s"(dst + NW * i * 1024) : "memory");
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(vs), "s"(dst + G::HALF + NW * i * 1024) : "memory");
+        load_to_lds(ks, dst + NW * i * 1024);
+        load_to_lds(vs, dst + G::HALF + NW * i * 1024);
       }
     }
     slot = slot == (G::NS - 1) * 2 * G::HALF ? 0 : slot + 2 * G::HALF;

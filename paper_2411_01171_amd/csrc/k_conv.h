@@ -316,7 +316,7 @@ __global__ __launch_bounds__(WS ? 512 : 256, (WS && TM * TN > 2) ? 1 : 2) void r
         if constexpr (CHUNKS) voff = aim_act[j][ks];
         else voff = (real && tapv[j]) ? tapv[j] + (unsigned)((ld_c * 2 + ks) * 1024) : (unsigned)(lane * 16 % kActZeroBytes);
         const unsigned dst = slot + (unsigned)((((wave * TM + j) * 2 + ks)) * 1024);
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(a.act), "s"(dst) : "memory");
+        load_to_lds(voff, a.act, dst);
       }
     const char* wk = wtile + (int64_t)(real ? ld_kt : 0) * (WFR * 1024);
 #pragma unroll
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(WS ? 512 : 256, (WS && TM * TN > 2) ? 1 : 2) void r
       const char* sb = real ? wk + fi * 1024 : a.act;
       const unsigned voff = real ? (unsigned)(lane * 16) : (unsigned)(lane * 16 % kActZeroBytes);
       const unsigned dst = slot + (unsigned)((AF + fi) * 1024);
-      asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sb), "s"(dst) : "memory");
+      load_to_lds(voff, sb, dst);
     }
     ++ld_kt;
     if constexpr (CHUNKS) return;

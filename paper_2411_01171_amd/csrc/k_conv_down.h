@@ -81,10 +81,7 @@ __global__ __launch_bounds__(512, 2) void conv_down_kernel(ConvDownArgs a) {
 #pragma unroll
   for (int i = 0; i < NLW; ++i) wsrc[i] = (unsigned)(wave + 8 * i < 3 * WFR ? wave + 8 * i : 3 * WFR - 1) * 1024;
   auto load_w = [&](const char* row, int i, int buf) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"((unsigned)(lane * 16)), "s"(row + wsrc[i]), "s"(lds0 + wsrc[i] + (unsigned)(buf * WST))
-                 : "memory");
+    load_to_lds((unsigned)(lane * 16), row + wsrc[i], lds0 + wsrc[i] + (unsigned)(buf * WST));
   };
   // i-th load of what takes the place of stage (cc, r) when everybody has left it: the stage after the next.  Past the
   // last chunk the last one is fetched once more, into slots nobody reads.  wchunk is chunk wc's.

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(512, 2) void conv_halo_kernel(ConvArgs a, int nblk,
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds;
   const char* wtile = a.wf + (int64_t)col * (9 * nch) * (WFR * 1024);
   auto load = [&](unsigned voff, const char* sbase, unsigned dst) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase), "s"(lds0 + dst) : "memory");
+    load_to_lds(voff, sbase, lds0 + dst);
   };
   // A stage's loads, numbered per wavefront: first the weights of kernel row r, chunk cc (fragments past the stage repeat
   // the last one: same source, same destination), then part p (of three) of plane wave % 4 of a patch: its

@@ -258,10 +258,7 @@ struct WeightPipe {
     for (int i = 0; i < PER_THREAD; ++i) {
       const char* sb = sbase + (int64_t)(4 * i) * pitch * 16;
       const unsigned l = dst + (unsigned)(4 * i * kWave * 16);
-      // Issued as assembly so that the compiler's wait-count pass does not place a full vector-memory
-      // wait in front of every later LDS read; completion is awaited explicitly when a step closes.
-      // M0 is reserved by the compiler and used by nothing else in these kernels.
-      asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sb), "s"(l) : "memory");
+      load_to_lds(voff, sb, l);  // completion is awaited explicitly when a step closes
     }
   }
 };

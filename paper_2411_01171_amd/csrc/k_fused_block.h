@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   _Pragma("unroll") for (int q = 0; q < 4; ++q) {                                                    \
     const char* sb = park_s + ((nb) * 4 + q) * (kWave * 16);                                         \
     const unsigned l = park_lds + (unsigned)((((nb) % 2) * 16 + q) * (kWave * 16));                  \
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"((unsigned)(lane * 16)), "s"(sb), "s"(l) : "memory"); \
+    load_to_lds((unsigned)(lane * 16), sb, l);                                                       \
   }
   float4* const hdump = reinterpret_cast<float4*>(a.hpark + ((int64_t)w.B * F * w.Pw + 127) / 128 * 128 * D) + tid;
 #define SI_PROJ_IN_BLOCK(nb)                                                                         \

@@ -59,10 +59,7 @@ __global__ __launch_bounds__(256 * WC, WC == 2 ? 2 : 1) void gemm_160_kernel(Con
   }
   auto load = [&](int l, int slot) {
     const char* src = (l < AFR / NW ? actp : wfp) + off[l];
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"((unsigned)(lane * 16)), "s"(src), "s"(lds0 + (unsigned)(slot * SLOT + (wave + NW * l) * 1024))
-                 : "memory");
+    load_to_lds((unsigned)(lane * 16), src, lds0 + (unsigned)(slot * SLOT + (wave + NW * l) * 1024));
   };
   auto advance = [&](int st) {  // to stage st; past the end the last one is fetched once more, into a slot nobody reads
     if (st < nst) {
@@ -196,10 +193,7 @@ __global__ __launch_bounds__(256 * WC, WC == 2 ? 2 : 1) void gemm_160_kernel(Con
       for (int k = 0; k < ITER; ++k) {
         const int u = k * 256 + tid;
         const unsigned at = u / G < rows ? 4 * offset(u) : 0u;
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-                     :
-                     : "v"(at), "s"(base), "s"(lds0 + (unsigned)(k * 256 + wave * kWave) * 16)
-                     : "memory");
+        load_to_lds(at, base, lds0 + (unsigned)(k * 256 + wave * kWave) * 16);
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0070 | 0xF00);

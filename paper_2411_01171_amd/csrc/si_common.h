@@ -59,6 +59,18 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+// Direct global->LDS loads: every lane brings 16 bytes from base + off (from an address of its own) to LDS at lds + 16 lane.
+// As assembly, so that the compiler's wait-count pass does not place a full vector-memory wait in front of every later LDS
+// read: whoever calls them awaits their completion.  The LDS address goes through M0, and one wait state has to lie between a
+// scalar write of M0 and the load that reads it; nothing inside a string of assembly adds it, hence the s_nop.  The
+// compiler reserves M0 and takes no clobber of it; nothing else in the library uses it.
+__device__ __forceinline__ void load_to_lds(unsigned off, const void* base, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const void* p, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
+}
+
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
