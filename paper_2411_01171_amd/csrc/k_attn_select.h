@@ -13,6 +13,7 @@
 // the next blocks fetched ahead of the products made it 10 us longer.
 #pragma once
 #include "k_rope.h"
+#include "k_select_search.h"
 
 #include <type_traits>
 
@@ -103,33 +104,6 @@ struct SelectArgs {
   int tiles;              // of `rows` runs; a workgroup takes one tile of one (b, kv head)
   unsigned work;          // B * heads_kv * tiles
 };
-
-// Order of float64 as unsigned integers: NaN as -infinity, -0 as +0; 0 is below every value.
-__device__ __forceinline__ unsigned long long order_key(double x) {
-  if (!(x == x)) x = -INFINITY;
-  const unsigned long long b = __builtin_bit_cast(unsigned long long, x + 0.0);
-  return b >> 63 ? ~b : b | 0x8000000000000000ull;
-}
-
-// Narrows [lo, hi) to the largest T with count(T) = (number of values >= T) >= need, where count(lo) = n_lo >= need > n_hi =
-// count(hi).  Ends with hi = lo + 1, or as soon as count(lo) is `need`, or when no more than `few` values lie in [lo, hi).
-// WAYS parts per step: 4 where a count is nearly all latency (a few ballots), 2 where it is work.
-template <int WAYS, class U, class Count>
-__device__ __forceinline__ void narrow(U& lo, U& hi, int& n_lo, int& n_hi, int need, int few, Count count) {
-  while (hi - lo > 1 && n_lo != need && n_lo - n_hi > few) {
-    const U part = hi - lo > WAYS ? (hi - lo) / WAYS : 1;
-    int n[WAYS];
-#pragma unroll
-    for (int i = 1; i < WAYS; ++i) n[i] = count(lo + part * i);  // past the end: too few
-    const U base = lo;
-#pragma unroll
-    for (int i = 1; i < WAYS; ++i)  // counts fall with i
-      if (n[i] >= need) { lo = base + part * i; n_lo = n[i]; }
-#pragma unroll
-    for (int i = WAYS - 1; i > 0; --i)
-      if (n[i] < need) { hi = base + part * i; n_hi = n[i]; }
-  }
-}
 
 // v of all lanes of the wavefront joined (identity 0) by data-parallel primitives, in a scalar register.
 template <class Join>
@@ -230,8 +204,8 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
         }
         return (int)lanes_join((unsigned)n, [](unsigned x, unsigned y) { return x + y; });
       };
-      // The upper words first, from eight binades below the largest on: most lists have their threshold there.  (From zero on,
-      // by the bits of a threshold, all candidates counted to the end: 134 us against 124 for 450 runs x 900 blocks x 20 heads.)
+      // The upper words first.  (From zero on, by the bits of a threshold, all candidates counted to the end: 134 us against 124
+      // for 450 runs x 900 blocks x 20 heads.)
       unsigned top = 0;
       if constexpr (KPL > 0) {
 #pragma unroll
@@ -240,30 +214,25 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
         for (int j = lane; j < nblk; j += kWave) top = max(top, (unsigned)(key[j] >> 32));
       }
       top = lanes_join(top, [](unsigned x, unsigned y) { return max(x, y); });
-      constexpr unsigned kBinades = 8u << 20;
-      unsigned lo = 0, hi = top + 1;  // top is at most the infinity's
-      int n_lo = nblk, n_hi = 0;
-      auto upper = [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); };
-      const unsigned first = top > kBinades ? top - kBinades : top / 2 + 1;
-      const int n = upper(first);
-      if (n >= a.keep) { lo = first; n_lo = n; }
-      else { hi = first; n_hi = n; }
       constexpr int WAYS = KPL > 0 && KPL <= 4 ? 4 : 2;
-      narrow<WAYS>(lo, hi, n_lo, n_hi, a.keep, KPL > 1 ? kWave : 0, upper);
-      unsigned long long least = (unsigned long long)lo << 32;  // everything >= least is kept, except some of the equal ones
+      UpperBounds bounds = upper_bounds<WAYS>(top, nblk, a.keep, KPL > 1 ? kWave : 0,
+                                              [&](unsigned c) { return tally([&](unsigned long long k) { return (unsigned)(k >> 32) >= c; }); });
+      int &n_lo = bounds.n_lo, &n_hi = bounds.n_hi;
+      unsigned long long least = (unsigned long long)bounds.lo << 32;  // everything >= least is kept, except some of the equal ones
       bool exact = n_lo == a.keep;
       int need_equal = 0;  // of the values == least, when not exact
       if (!exact) {
-        unsigned long long end = (unsigned long long)hi << 32;
+        unsigned long long end = (unsigned long long)bounds.hi << 32;
         if (KPL > 0 && n_lo - n_hi <= kWave) {  // one candidate per lane: a count is a ballot
           unsigned long long mine = 0;
           if constexpr (KPL == 1) {
-            mine = held[0] >= least && held[0] < end ? held[0] : 0ull;
+            mine = is_candidate(held[0], least, end) ? held[0] : 0ull;
           } else if constexpr (KPL > 0) {
             int at = 0;
 #pragma unroll
-            for (int i = 0; i < KPL; ++i) {  // the run's scores in LDS are in registers: their place is free
-              const bool in = held[i] >= least && held[i] < end;
+            for (int i = 0; i < KPL; ++i) {  // the run's scores in LDS are in registers: their place is free, and holds more than the
+                                             // kWave candidates at most (KPL > 1: more than kWave blocks)
+              const bool in = is_candidate(held[i], least, end);
               const unsigned long long ins = __builtin_amdgcn_ballot_w64(in);
               if (in) key[at + __popcll(ins & ((1ull << lane) - 1ull))] = held[i];
               at += __popcll(ins);

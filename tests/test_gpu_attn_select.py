@@ -160,3 +160,15 @@ def test_captured_call_replays_like_the_eager_one():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, ref), i
+
+
+@pytest.mark.parametrize("blocks,keep", [(70, 35), (72, 36), (80, 60), (129, 65), (144, 72), (300, 200), (900, 450)])
+def test_many_of_the_blocks_kept_in_full_tiles_of_runs(blocks, keep):
+    """Thresholds far below the largest score, sixteen runs to a workgroup whose scores lie next to each other."""
+    _check("bf16", 1, 48, 64 * blocks - 5, 2, 2, 8, 1, 64, keep, seed=blocks)
+
+
+@pytest.mark.parametrize("blocks,counted,keep", [(100, 70, 40), (300, 60, 30), (500, 70, 66), (900, 100, 80)])
+def test_padded_batches_of_long_lists(blocks, counted, keep):
+    """Most of the places of a list stand for blocks without a counted key."""
+    _check("f32", 2, 40, 64 * blocks, 1, 1, 8, 1, 64, keep, q_len=[40, 33], k_len=[64 * counted - 3, 64 * blocks], seed=blocks)
