@@ -422,9 +422,10 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
  *            as si_rope_forward does; extent[1], extent[2] are the block's H, W
  *            (SI_ERR_SHAPE).  The frame axis turns the queries and keys of a frame
  *            alike and so drops out of a spatial block.
- *   keep     0: every key.  Else the `keep` best key blocks of every run of q_block
- *            queries, per frame and head, as si_attn_select and
- *            si_attn_sparse_forward define them (scale 1/sqrt(dim_head)).
+ *   keep     0: every key; q_block and k_block are not read.  Else the `keep`
+ *            best key blocks of every run of q_block queries, per frame and head,
+ *            as si_attn_select and si_attn_sparse_forward define them (scale
+ *            1/sqrt(dim_head)).
  * Every slicing of a call gives the same bits.  Temporal blocks -> SI_ERR_ARG. */
 typedef struct {
   const si_rope* rope;

@@ -132,6 +132,7 @@ struct Plan {
   size_t lane_stride;  // bytes between two lanes' slice intermediates
   int Mcp;          // context tokens rounded up to a multiple of 8 (transposed value copy)
   const si_attn_options* attn;  // self-attention of a spatial block with rotary positions / over selected key blocks, or NULL
+  int64_t q_block, k_block;     // attn: of its lists, or (no lists) tokens of a run and keys of a block as fits the kernels
   BlocksPlan blocks;            // attn: runs and key blocks of a frame
   // workspace offsets (bytes)
   size_t off_stats, off_rehash, off_pe, off_ctxkv, off_ctxvt, off_ml;
@@ -155,8 +156,10 @@ static si_status plan_attn(const si_attn_options* o, Plan* p) {
   p->attn = o;
   if (!o) return SI_OK;
   if (p->kind != SI_BLOCK_SPATIAL || o->keep < 0) return SI_ERR_ARG;
+  p->q_block = o->keep ? o->q_block : 128;  // whole row tiles; the bits do not depend on what the options hold then
+  p->k_block = o->keep ? o->k_block : 64;
   const si_heads q = window_heads(*p, nullptr, p->slice_len, 0), k = window_heads(*p, nullptr, p->slice_len, 1);
-  const si_status s = plan_blocks(&q, &k, o->q_block, o->k_block, &p->blocks);
+  const si_status s = plan_blocks(&q, &k, p->q_block, p->k_block, &p->blocks);
   if (s != SI_OK) return s;
   if (o->keep && p->blocks.blocks > kSelectMaxBlocks) return SI_ERR_SHAPE;
   if (o->rope) {
@@ -781,10 +784,10 @@ static si_status run_window_attention(const Plan& p, void* rows, void* out, int6
   const si_heads q = window_heads(p, rows, frames, 0), k = window_heads(p, rows, frames, 1), v = window_heads(p, rows, frames, 2);
   const si_heads y{out, p.dtype, q.B, q.N, q.heads, q.dim_head, p.P * p.D, p.D, p.d};
   if (o.rope) SI_TRY(enqueue_rope(&q, &k, o.rope, 0, &q, &k, st));
-  if (o.keep) SI_TRY(enqueue_select(&q, &k, p.blocks, o.q_block, o.k_block, o.keep, nullptr, nullptr, lists, attn_ws, st));
+  if (o.keep) SI_TRY(enqueue_select(&q, &k, p.blocks, p.q_block, p.k_block, o.keep, nullptr, nullptr, lists, attn_ws, st));
   SparsePlan sp;
-  SI_TRY(plan_sparse(&q, &k, o.q_block, p.blocks, false, &sp));
-  return enqueue_sparse(&q, &k, &v, p.blocks, sp, o.q_block, o.k_block, scale, nullptr, nullptr, o.keep ? lists : nullptr, &y, nullptr, st,
+  SI_TRY(plan_sparse(&q, &k, p.q_block, p.blocks, false, &sp));
+  return enqueue_sparse(&q, &k, &v, p.blocks, sp, p.q_block, p.k_block, scale, nullptr, nullptr, o.keep ? lists : nullptr, &y, nullptr, st,
                         o_frag);
 }
 

@@ -273,3 +273,15 @@ def test_oracle_block_without_options_is_the_plain_block():
     assert np.allclose(oracle.block_forward_attn_ref(x, w, spec, ctx), plain, rtol=0, atol=1e-12)
     assert np.allclose(oracle.block_forward_attn_ref(x, w, spec, ctx, keep=2), plain, rtol=0, atol=1e-12)
     assert not np.allclose(oracle.block_forward_attn_ref(x, w, spec, ctx, keep=1), plain, atol=1e-4)
+
+
+def test_block_without_lists_takes_any_sizes_of_runs_and_blocks():
+    x = B._Tensor5(BASE, B.SI_BF16, 2, 64, 4, 8, 8)
+    ctx = B._Context(BASE + 2 * FAR, B.SI_BF16, 2, 5, 16)
+    w = B._Weights()
+    w.kind, w.heads, w.dim_head, w.gn_groups, w.gn_eps, w.ln_eps, w.add_sin_pe = B.SI_BLOCK_SPATIAL, 2, 32, 8, 1e-6, 1e-5, 0
+    size = lambda **kw: si.lib().si_block_attn_workspace_bytes(C.byref(x), C.byref(w), C.byref(ctx), C.byref(si.AttnOptions(**kw).struct), B.SI_AXIS_F, 1)  # noqa: E731
+    assert size() > 0
+    for sizes in ((0, 0), (-1, 7), (1 << 40, 1 << 40), (1, 64)):
+        assert size(q_block=sizes[0], k_block=sizes[1], keep=0) == size(), sizes
+        assert size(q_block=sizes[0], k_block=sizes[1], keep=1) == 0 or sizes == (1, 64)

@@ -137,3 +137,13 @@ def test_all_blocks_kept_is_dense():
     x, w, ctx = _inputs(spec)
     rope = si.Rope((2, 8, 16), (0, 16, 16))
     assert np.array_equal(_run(spec, x, w, ctx, si.AttnOptions(rope, keep=2)), _run(spec, x, w, ctx, si.AttnOptions(rope)))
+
+
+@pytest.mark.parametrize("name", ["staged_640", "f32"])
+def test_without_lists_their_sizes_change_no_bit(name):
+    spec = _spec(name, 1)
+    x, w, ctx = _inputs(spec)
+    rope = si.Rope((spec.F, spec.H, spec.W), _pairs(spec.dim_head))
+    base = _run(spec, x, w, ctx, si.AttnOptions(rope))
+    for q_block, k_block in ((0, 0), (1, 64), (33, 192)):
+        assert np.array_equal(_run(spec, x, w, ctx, si.AttnOptions(rope, q_block=q_block, k_block=k_block)), base)
