@@ -13,6 +13,9 @@
 
 namespace si {
 
+constexpr int64_t kMostTokens = INT32_MAX - (1 << 22);  // of a sequence: kernels add tiles to token numbers in 31 bits
+constexpr int64_t kMostOfBlock = 1 << 20;               // tokens of a run or a key block
+
 static inline HeadsView view_of(const si_heads* t) { return HeadsView{t->ptr, t->stride_b, t->stride_n, t->stride_h}; }
 static inline int heads_esize(const si_heads* t) { return t->dtype == SI_F32 ? 4 : 2; }
 static inline bool heads_empty(const si_heads* t) { return t->N == 0; }
@@ -31,7 +34,7 @@ static si_status check_heads(const si_heads* t, bool written) {
   if (!t) return SI_ERR_NULL;
   if (t->dtype != SI_F32 && t->dtype != SI_BF16) return SI_ERR_DTYPE;
   if (t->B < 1 || t->N < 0 || t->heads < 1 || t->dim_head < 8 || t->dim_head > 128 || t->dim_head % 8) return SI_ERR_SHAPE;
-  if (t->B > (1 << 24) || t->N > INT32_MAX - (1 << 22) || t->heads > 65535 || t->B * t->heads > (1 << 28)) return SI_ERR_SHAPE;
+  if (t->B > (1 << 24) || t->N > kMostTokens || t->heads > 65535 || t->B * t->heads > (1 << 28)) return SI_ERR_SHAPE;
   const int64_t n[] = {t->B, t->N, t->heads}, s[] = {t->stride_b, t->stride_n, t->stride_h};
   const int vec = 16 / heads_esize(t);
   double far = (double)t->dim_head;
@@ -109,7 +112,7 @@ si_status check_rope(const si_rope* r, int d) {
     // further out, a position times a frequency has no digits left behind the point
     if (!(std::fabs(r->origin[i]) <= most) || !(std::fabs(r->step[i]) * (double)r->extent[i] <= most)) return SI_ERR_ARG;
   }
-  if (tokens > (double)(INT32_MAX - (1 << 22))) return SI_ERR_SHAPE;
+  if (tokens > (double)kMostTokens) return SI_ERR_SHAPE;
   if (pairs < 1 || pairs % 4 || 2 * pairs > d) return SI_ERR_SHAPE;
   if (r->layout != SI_ROPE_INTERLEAVED && r->layout != SI_ROPE_HALVES) return SI_ERR_ARG;
   if (!std::isfinite(r->norm_eps)) return SI_ERR_ARG;
@@ -195,7 +198,7 @@ constexpr int64_t kGridMost = 1 << 20;  // workgroups of a launch; kernels walk 
 si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block, BlocksPlan* p) {
   if (q->dtype != k->dtype) return SI_ERR_DTYPE;
   if (q->B != k->B || q->dim_head != k->dim_head || q->heads % k->heads) return SI_ERR_SHAPE;
-  if (q_block < 1 || q_block > (1 << 20) || k_block < 64 || k_block > (1 << 20) || k_block % 64) return SI_ERR_SHAPE;
+  if (q_block < 1 || q_block > kMostOfBlock || k_block < 64 || k_block > kMostOfBlock || k_block % 64) return SI_ERR_SHAPE;
   p->group = (int)(q->heads / k->heads);
   if (p->group * q_block >= (1 << 24)) return SI_ERR_SHAPE;
   if (k->N > 1 && k->stride_n >= (1 << 23)) return SI_ERR_SHAPE;  // 64 rows of keys inside 31 bits of bytes
@@ -401,7 +404,7 @@ si_status si_rope_forward(const si_heads* q, const si_heads* k, const si_rope* r
 }
 
 int64_t si_attn_block_words(int64_t n_keys, int64_t k_block) {
-  if (n_keys < 0 || k_block < 64 || k_block % 64) return 0;
+  if (n_keys < 0 || n_keys > si::kMostTokens || k_block < 64 || k_block > si::kMostOfBlock || k_block % 64) return 0;
   return ((n_keys + k_block - 1) / k_block + 31) / 32;
 }
 

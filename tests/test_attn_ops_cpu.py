@@ -285,3 +285,10 @@ def test_block_without_lists_takes_any_sizes_of_runs_and_blocks():
     for sizes in ((0, 0), (-1, 7), (1 << 40, 1 << 40), (1, 64)):
         assert size(q_block=sizes[0], k_block=sizes[1], keep=0) == size(), sizes
         assert size(q_block=sizes[0], k_block=sizes[1], keep=1) == 0 or sizes == (1, 64)
+
+
+def test_word_counts_of_sizes_that_no_call_takes():
+    most = 2 ** 31 - 1 - 2 ** 22  # tokens of a sequence
+    assert si.si_attn_block_words(most, 64) == -(-most // 2048) and si.si_attn_block_words(most, 1 << 20) == 64
+    for n_keys, k_block in ((most + 1, 64), (2 ** 63 - 1, 64), (2 ** 63 - 1, 1 << 20), (100, (1 << 20) + 64), (100, 1 << 40), (100, -64)):
+        assert si.si_attn_block_words(n_keys, k_block) == 0, (n_keys, k_block)
