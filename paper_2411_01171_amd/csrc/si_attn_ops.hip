@@ -103,7 +103,7 @@ si_status check_rope(const si_rope* r, int d) {
   if (!r) return SI_ERR_NULL;
   int64_t pairs = 0;
   double tokens = 1.0;
-  if (!(r->theta > 0.0) || !std::isfinite(r->theta)) return SI_ERR_ARG;
+  if (!(r->theta > 0.0) || !std::isnormal(r->theta)) return SI_ERR_ARG;  // 1 / theta is finite
   const double most = 1e12 * std::min(1.0, r->theta);  // frequencies are at most max(1, 1 / theta)
   for (int i = 0; i < 3; ++i) {
     if (r->extent[i] < 1 || r->extent[i] > INT32_MAX || r->pairs[i] < 0 || r->pairs[i] > d / 2) return SI_ERR_SHAPE;

@@ -292,3 +292,11 @@ def test_word_counts_of_sizes_that_no_call_takes():
     assert si.si_attn_block_words(most, 64) == -(-most // 2048) and si.si_attn_block_words(most, 1 << 20) == 64
     for n_keys, k_block in ((most + 1, 64), (2 ** 63 - 1, 64), (2 ** 63 - 1, 1 << 20), (100, (1 << 20) + 64), (100, 1 << 40), (100, -64)):
         assert si.si_attn_block_words(n_keys, k_block) == 0, (n_keys, k_block)
+
+
+def test_frequencies_that_double_cannot_hold():
+    """theta^(-i / pairs) of a subnormal theta is infinite, and zero times it no angle."""
+    still = dict(origin=(0, 0, 0), step=(0, 0, 0))
+    q = heads(N=1 << 30)  # behind the grid: what is no refusal of theta is this one, before any launch
+    for theta, want in ((1e-310, ARG), (5e-324, ARG), (2.3e-308, SHAPE), (1e308, SHAPE)):
+        assert rope_call(q=q, qo=heads(2 * FAR, N=1 << 30), lone=True, r=rope(theta=theta, **still)) == want, theta
