@@ -679,47 +679,46 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_attn_f32_kern
 // The shares of a query row joined: weights 2^(m - max m).  A wavefront per row: its lanes hold one share's maximum and sum
 // each (nsplit <= 64), then 64 / (d / 4) shares' outputs at a time, four channels per lane; the order of the sums is fixed.
 template <typename T>
-__global__ __launch_bounds__(256) void sparse_join_kernel(SparseArgs a, int64_t rows) {
+__global__ __launch_bounds__(256) void sparse_join_kernel(SparseArgs a, int rows) {
   const int lane = threadIdx.x % kWave, heads = a.heads_kv * a.group, quads = a.d / 4;
   // lanes of one share: the next power of two of quads
   const int width = quads <= 2 ? 2 : quads <= 4 ? 4 : quads <= 8 ? 8 : quads <= 16 ? 16 : 32, at_once = kWave / width;
   const int quad = lane % width, which = lane / width;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; row < rows; row += (int64_t)gridDim.x * 4) {
-    const int64_t bn = row / heads;
-    const int h = (int)(row - bn * heads), b = (int)(bn / a.Nq);
-    const int64_t token = bn - (int64_t)b * a.Nq;
-    if (a.q_len && token >= a.q_len[b]) continue;
-    const float2 ml = lane < a.nsplit ? a.part_ml[row * a.nsplit + lane] : make_float2(kSparseLow, 0.f);
-    const float w = __builtin_amdgcn_exp2f(ml.x - wave_max(ml.x));
-    const float l = wave_sum(ml.y * w);
-    const float* src = a.part + row * a.nsplit * a.d + 4 * quad;
-    f32x4_t o{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < a.nsplit; s0 += 4 * at_once) {
-      f32x4_t x[4];
+  const int row = (int)blockIdx.x * 4 + threadIdx.x / kWave;
+  if (row >= rows) return;
+  const int bn = row / heads;
+  const int h = row - bn * heads, b = bn / a.Nq, token = bn - b * a.Nq;
+  if (a.q_len && token >= a.q_len[b]) return;
+  const float2 ml = lane < a.nsplit ? a.part_ml[(int64_t)row * a.nsplit + lane] : make_float2(kSparseLow, 0.f);
+  const float w = __builtin_amdgcn_exp2f(ml.x - wave_max(ml.x));
+  const float l = wave_sum(ml.y * w);
+  const float* src = a.part + (int64_t)row * a.nsplit * a.d + 4 * quad;
+  f32x4_t o{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < a.nsplit; s0 += 4 * at_once) {
+    f32x4_t x[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int s = s0 + u * at_once + which;
-        x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (s < a.nsplit && quad < quads) x[u] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)s * a.d);
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float ws = __shfl(w, (s0 + u * at_once + which) % kWave, kWave);  // past the last share: times zero
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = fmaf(x[u][j], ws, o[j]);
-      }
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + u * at_once + which;
+      x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (s < a.nsplit && quad < quads) x[u] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)s * a.d);
     }
-    for (int step = width; step < kWave; step <<= 1)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], step, kWave);
-    if (which != 0 || quad >= quads) continue;
-    const float inv = 1.f / l;
+    for (int u = 0; u < 4; ++u) {
+      const float ws = __shfl(w, (s0 + u * at_once + which) % kWave, kWave);  // past the last share: times zero
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : o[j] * inv;
-    T* dst = static_cast<T*>(a.o) + b * a.ob + token * a.on + (int64_t)h * a.oh + 4 * quad;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
-    else *reinterpret_cast<f32x4_t*>(dst) = o;
+      for (int j = 0; j < 4; ++j) o[j] = fmaf(x[u][j], ws, o[j]);
+    }
   }
+  for (int step = width; step < kWave; step <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], step, kWave);
+  if (which != 0 || quad >= quads) return;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : o[j] * inv;
+  T* dst = static_cast<T*>(a.o) + b * a.ob + (int64_t)token * a.on + (int64_t)h * a.oh + 4 * quad;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+  else *reinterpret_cast<f32x4_t*>(dst) = o;
 }
 
 }  // namespace si

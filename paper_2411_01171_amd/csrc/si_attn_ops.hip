@@ -336,8 +336,8 @@ static void dispatch_sparse(const SparseArgs& a, const SparsePlan& p, hipStream_
     else launch(integral_constant<int, 8>());
   }
   if (a.nsplit > 1) {
-    const int64_t rows = p.rows;
-    sparse_join_kernel<T><<<(unsigned)std::min<int64_t>((rows + 3) / 4, kGridMost), 256, 0, st>>>(a, rows);
+    const int rows = (int)p.rows;  // at most 128 for each of 256 tiles: a split call has few
+    sparse_join_kernel<T><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, rows);
   }
 }
 
