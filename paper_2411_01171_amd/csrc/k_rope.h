@@ -5,7 +5,8 @@
 //   angle = (origin + step * coordinate) * theta^(-i / pairs of that axis),
 // (x1, x2) -> (x1 cos - x2 sin, x1 sin + x2 cos).  The angle is formed in float64 and in revolutions (the host divides the
 // frequencies by 2 pi), so that its whole part drops out exactly before the sine and cosine are taken in float32: positions
-// of 10^6 lose nothing.  Everything else is float32 with one rounding at the store.
+// of 10^6 lose nothing, and the digits that the rest loses in float32 come back to first order.  Everything else is float32
+// with one rounding at the store.
 //
 // Bound by HBM: every head is read and written once.  A thread owns eight channels (four pairs) of one token and walks the
 // heads of q and k: the sines of a token are computed once for all of them, and the loads of kRopeHeads heads are in
@@ -114,7 +115,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
     for (int i = 0; i < 4; ++i) {
       const int p = 4 * c + i;
       const double rev = (p < a.end_f ? pf : p < a.end_y ? py : px) * a.freq[p];
-      sincospif(2.f * (float)(rev - rint(rev)), &sn[i], &cs[i]);
+      const double turn = rev - rint(rev);  // the whole turns drop out exactly
+      const float near = (float)turn, rest = (float)(turn - (double)near) * 6.283185307f;  // what float32 cannot hold, in radians
+      float s, co;
+      sincospif(2.f * near, &s, &co);
+      sn[i] = fmaf(co, rest, s);
+      cs[i] = fmaf(-s, rest, co);
     }
   }
   Raw8<T> gq, gk;  // as they lie in memory: half the registers for bf16
