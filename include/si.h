@@ -324,7 +324,9 @@ si_status si_resample_forward(const si_tensor5* x, int32_t kind, const void* w_c
  * rows, of a cache, or head-major.  Strides are not negative, and of dimensions
  * longer than one a multiple of 16 bytes; the stride of a dimension of length one
  * is ignored.  dim_head is a multiple of 8, at most 128.  N == 0 is legal (ptr may
- * then be NULL).  What a call writes must have one address per element. */
+ * then be NULL).  What a call writes must have one address per element.
+ * At most (SI_ERR_SHAPE beyond): B 2^24, N 2^31 - 1 - 2^22, heads 65535, B * heads
+ * 2^28; strides are below 2^44 elements and all of them together below 2^46. */
 typedef struct {
   void* ptr; /* device */
   int32_t dtype;
@@ -344,8 +346,10 @@ typedef struct {
  * have no pairs.  norm_eps >= 0: every head is first divided by
  * sqrt(mean of its squares + norm_eps) and multiplied by q_gain / k_gain (device,
  * [dim_head] in the operands' type, NULL = one); norm_eps < 0: it is not.
- * Angles are formed in float64, everything else in float32 with one rounding.
- * |origin| and |step| * extent are at most 1e12 (theta < 1: 1e12 theta). */
+ * Angles are formed in float64, everything else in float32 (the norm's squares too:
+ * elements past 1e19 overflow them) with one rounding.  The grid has at most
+ * 2^31 - 1 - 2^22 tokens (SI_ERR_SHAPE).  theta is a normal number; |origin| and
+ * |step| * extent are at most 1e12 (theta < 1: 1e12 theta; SI_ERR_ARG). */
 typedef enum { SI_ROPE_INTERLEAVED = 0, SI_ROPE_HALVES = 1 } si_rope_layout;
 typedef struct {
   int64_t extent[3];
@@ -378,8 +382,11 @@ si_status si_rope_forward(const si_heads* q, const si_heads* k, const si_rope* r
  * that count, clamped to [0, N].  What lies behind them is never read as a value,
  * so it may hold anything.
  *
- * stride_n of keys and values is below 2^23 elements; lists, row tiles and blocks
- * of a call are counted in 31 bits (SI_ERR_SHAPE). */
+ * SI_ERR_SHAPE beyond: q_block and k_block 2^20, q_block times the query heads of a
+ * key head below 2^24, stride_n of keys and values below 2^23 elements; lists
+ * (B * k->heads * runs) and blocks of all key heads (B * k->heads * blocks) below
+ * 2^27 - 2^16, lists and their words together below 10^12, row tiles of the
+ * attention (16 to 128 rows of a list each) below 2^31 - 2^20. */
 
 /* Words of one list; 0 if the arguments are invalid or there are no keys.  Host-only. */
 int64_t si_attn_block_words(int64_t n_keys, int64_t k_block);
@@ -408,8 +415,10 @@ si_status si_attn_select(const si_heads* q, const si_heads* k, int64_t q_block, 
  * scores times scale are at most 1e9 in magnitude.
  * scale > 0.  q, k, v and out have one dtype; v is shaped like k, out like q.  No
  * element of out may lie on one of q, k or v.  bf16 operands: scores, maxima, sums
- * and outputs in float32, probabilities rounded to bf16 for the second product;
- * float32 operands: float32 throughout.  The same operands give the same bits.
+ * and outputs in float32, probabilities rounded to bf16 for the second product and
+ * for the sum that divides it (errors of 2.3e-3 of the output's norm, where the
+ * output's own rounding makes 1.7e-3); float32 operands: float32 throughout.  The
+ * same operands give the same bits.
  * workspace: device, 256-byte aligned, contents ignored; calls that overlap in time
  * must not share one. */
 si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_heads* v, int64_t q_block, int64_t k_block,
@@ -426,7 +435,12 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
  *            best key blocks of every run of q_block queries, per frame and head,
  *            as si_attn_select and si_attn_sparse_forward define them (scale
  *            1/sqrt(dim_head)).
- * Every slicing of a call gives the same bits.  Temporal blocks -> SI_ERR_ARG. */
+ * bf16 blocks round the probabilities as si_attn_sparse_forward does, also where
+ * si_block_forward_ex keeps them in float32 (heads other than 64, H*W no multiple
+ * of 8).  Every slicing of a call gives the same bits.  Temporal blocks ->
+ * SI_ERR_ARG.  si_windows_in_flight answers for these calls too;
+ * si_live_activation_bytes does not count the lists and the selection's means, and
+ * si_block_forward_rehash has no form with options. */
 typedef struct {
   const si_rope* rope;
   int64_t q_block, k_block, keep;

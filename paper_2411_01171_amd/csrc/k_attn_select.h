@@ -7,8 +7,10 @@
 // Everything behind the loads is float64: which block is the last one kept can hang on any digit of its score, and the
 // result is discrete.  The means are bound by HBM: every query and key is read once, 57600 tokens of 10 heads of 64, two batch
 // entries (295 MB), in 50 us (5.9 TB/s).  The scores take 2 d flop per (run, block) at some 60 TFLOP/s (450 runs x 900 blocks x
-// 20 heads: 16 us of matrix cores); the second kernel's 75 us there are latency: one workgroup fills a CU's LDS with the scores
-// of 16 runs, about 40 us go to fetching means from the L2 and 30 to the search for the threshold.  Means laid out as the
+// 20 heads: 16 us of matrix cores); the second kernel's 81 us there are latency: one workgroup fills a CU's LDS with the scores
+// of 16 runs, about half of the time goes to fetching means from the L2 and the rest to the search for the threshold.  2032
+// blocks, 1016 runs of 4 heads: 177 us a call; 16384 blocks, 8192 runs: 15.7 ms, with one run to a workgroup, whose search a
+// single wavefront walks.  Means laid out as the
 // matrix cores' fragments made that kernel 15 us shorter and the first one 7 longer, and calls of one frame 6 % slower; means of
 // the next blocks fetched ahead of the products made it 10 us longer.
 #pragma once
@@ -204,8 +206,8 @@ __global__ __launch_bounds__(NT) void block_select_kernel(SelectArgs a) {
         }
         return (int)lanes_join((unsigned)n, [](unsigned x, unsigned y) { return x + y; });
       };
-      // The upper words first.  (From zero on, by the bits of a threshold, all candidates counted to the end: 134 us against 124
-      // for 450 runs x 900 blocks x 20 heads.)
+      // The upper words first.  (From zero on, by the bits of a threshold, all candidates counted to the end: 144 us a call against
+      // 134 for 450 runs x 900 blocks x 20 heads.)
       unsigned top = 0;
       if constexpr (KPL > 0) {
 #pragma unroll

@@ -1,11 +1,12 @@
 // Attention of runs of queries over listed key blocks.
 //
 // A run is q_block consecutive queries of the `group` heads that share a key / value head: group * q_block rows, one list of
-// key blocks (a bitmap).  One workgroup takes NW x 32 rows of a run and walks the run's blocks, a stage of 64 (float32: 32)
-// keys at a time, with the running maximum and sum of a softmax:
+// key blocks (a bitmap).  One workgroup takes 16 to 128 rows of a run and walks the run's blocks, a stage of 64 (float32: 32)
+// keys at a time, with the running maximum and sum of a softmax.  bf16: 32 rows on one wavefront, 64 on four (two to the same
+// rows, SPLIT), 128 on four; float32: 16 rows to a wavefront, in workgroups of 16, 32 and 64, or 32 to each of four (H).
 //   S^T[key, row] = K Q^T       row operand: keys, column operand: rows
 //   O^T[chan, row] += V^T P^T   column operand: the softmax result registers as they stand
-// With queries as columns a lane holds scores of one query (float32: two), its running maximum and its part of the sum, so
+// With queries as columns a lane holds scores of one query (float32: of H), its running maximum and its part of the sum, so
 // the softmax needs no cross-lane traffic in the steady state.
 //
 // Keys and values go from their own rows to LDS with direct global->LDS loads, whole rows by neighbouring lanes (full
@@ -154,7 +155,7 @@ struct SparseGeo {
   static constexpr int LOADS = HALF / 1024;                           // wave-wide loads of a stage's keys
 
   // Piece p of row r lies in slot p ^ swizzle(r) of its row.  LDS reads 256 bytes per clock.  Keys: the lanes of a clock read
-  // one piece of 16 rows, which have to fall on 16 different groups of four banks.  Values: they read the pieces of 32 (bf16)
+  // one piece of 16 rows, which have to fall on 16 different groups of four banks (float32 still has conflicts).  Values: they read the pieces of 32 (bf16)
   // or 16 (float32) channels of four rows, which differ in bits 0 and 1 (bf16) or 2 and 3 (float32): those bits have to move
   // the slot by four.  (p ^ (r & 7) lost half of the LDS's cycles to conflicts: heads of 128, padded batch, 429 us against 388.)
   // Every bit of the row moves bits of the slot by itself: swizzle(a | b) = swizzle(a) ^ swizzle(b) for disjoint a and b.
@@ -315,9 +316,10 @@ __device__ __forceinline__ void sparse_put_ml(const SparseArgs& a, const SparseT
 // them, 32 exponentials (8 clocks each), 32 fma (the scale stays in float32: folded into q before a second rounding of q it
 // would save 4 % at 57600 tokens), 16 conversions and 16 sums of pairs; the two hardly overlap, whatever the number of
 // wavefronts (four per SIMD, sharing rows in pairs, 1958 us at 57600 tokens against 1858 with three); and by power: in long
-// launches the clock falls to 1.8 GHz.  72x128 frame over a quarter of its keys 67 us (809 TFLOP/s, 10 of them before the first
-// product and behind the last), 57600 tokens over a tenth 1858 us (914); a library product of 8192^3 reaches 1136.  Heads of
-// 128: 870 to 1030.  s_setprio around either half changes nothing.
+// launches the clock falls to 1.8 GHz.  72x128 frame over a quarter of its keys 69 us (784 TFLOP/s, 10 of them before the first
+// product and behind the last), 57600 tokens over a tenth 1867 us (910); a library product of 8192^3 reaches 1420.  Heads of
+// 128 in runs of 128: 9216 tokens of 5 heads 870 TFLOP/s, 28800 of 8 heads 1046; in runs of 400 rows, whose last tile of 128
+// holds 16, 750.  s_setprio around either half changes nothing.
 // PAD: d < 16 KS; what the keys' fragments hold past the head is made zero, as the queries are there.
 // SPLIT 2: two wavefronts share 32 rows and take half of a stage's keys each, joined at the end: a run of 64 rows then has four
 // wavefronts on a CU for every stage in its LDS, not two (72x128 frame, runs of 64: 112 -> 79 us).
@@ -514,7 +516,8 @@ __global__ __launch_bounds__(64 * NW, NW < 4 ? 1 : KS <= 4 ? 3 : 2) void sparse_
 // of 40: 121 -> 118 us).  A result lane (c, g), g = lane / 16, holds column c and rows 4 g + j.  Those four keys are, register by
 // register, the column operand of four steps of the second product.  16-channel tiles: heads of 40 contract 40 and produce
 // 48 channels (32 x 32 tiles: 48 and 64).  Bound by the float32 matrix rate, 256 flop per clock and CU: heads of 64 and 128
-// run at 120 TFLOP/s (a library product of 8192^3 at 153), heads of 40 at 104 of their own and 113 with the padded channels.
+// run at 123 and 124 TFLOP/s (a library product of 8192^3 at 153), heads of 40 at 103 of their own and 112 with the padded
+// channels; there 31 % of the active LDS cycles are conflicts.  One token against 115200 keys, 256 blocks: 4.35 TB/s.
 // D8: head channels / 8, exactly: the products of a stage are one block of instructions with its reads ahead of it.
 template <int D8, int NW, int H>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void sparse_attn_f32_kernel(SparseArgs a) {

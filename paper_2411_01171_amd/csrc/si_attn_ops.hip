@@ -261,8 +261,9 @@ si_status enqueue_select(const si_heads* q, const si_heads* k, const BlocksPlan&
     }
   };
   // The smallest store of scores that holds 16 runs, for as many workgroups on a CU as possible, and a wavefront for every run;
-  // lists of up to 32 blocks have too little work for that many (32x32 frames, 16 blocks: 22.0 us with 512 threads, 24.5 with
-  // 1024; 64 blocks 12.7 and 12.5, 144 blocks 16.5 and 15.2, 900 blocks 129 and 124).
+  // lists of up to 32 blocks have too little work for that many.  Calls with 512 and with 1024 threads: 16 blocks (32 batch entries
+  // of 1024 tokens) 22.8 and 25.4 us, 64 (float32, padded) 15.1 and 14.7, 144 (9216 tokens) 22.5 and 21.7, 400 (25600 tokens) 49.2
+  // and 54.8 (there alone fewer would be better), 900 (57600 tokens) 139 and 134.
   using std::integral_constant;
   if (p.blocks <= 32) launch(integral_constant<int, 16 * 34>(), integral_constant<int, 1>(), integral_constant<int, 512>());
   else if (p.blocks <= 64) launch(integral_constant<int, 16 * 66>(), integral_constant<int, 1>(), integral_constant<int, 1024>());
