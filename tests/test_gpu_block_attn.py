@@ -147,3 +147,35 @@ def test_without_lists_their_sizes_change_no_bit(name):
     base = _run(spec, x, w, ctx, si.AttnOptions(rope))
     for q_block, k_block in ((0, 0), (1, 64), (33, 192)):
         assert np.array_equal(_run(spec, x, w, ctx, si.AttnOptions(rope, q_block=q_block, k_block=k_block)), base)
+
+
+@pytest.mark.parametrize("slice_len", [12, 1])
+def test_block_on_another_stream_and_captured(slice_len):
+    """One window, and twelve with three in flight, whose streams join the capture."""
+    spec = wl.BlockSpec("many", wl.SPATIAL, "bf16", 2, 128, 12, 8, 40, 2, 64, gn_groups=8, ctx_tokens=5, ctx_dim=24, slice_axis=wl.AXIS_F,
+                        slice_len=slice_len, seed=9)
+    x, w, ctx = _inputs(spec)
+    xd, cd, wd = to_dev(x, spec.dtype), to_dev(ctx, spec.dtype), device_weights(spec, w)
+    attn = si.AttnOptions(si.Rope((12, 8, 40), (0, 16, 16), norm_eps=1e-6), q_block=64, k_block=64, keep=2)
+    ws = torch.empty(si.si_block_attn_workspace_bytes(xd, wd, cd, attn, si.SI_AXIS_F, slice_len), dtype=torch.uint8, device="cuda")
+    ref, out = torch.empty_like(xd), torch.empty_like(xd)
+
+    def call(to, **kw):
+        si.si_block_forward_attn(xd, wd, cd, attn, to, si.SI_AXIS_F, slice_len, ws, **kw)
+
+    call(ref)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    call(out, stream=stream)
+    stream.synchronize()
+    assert torch.equal(out, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for i in range(3):
+        xd.copy_(torch.randn(xd.shape, device="cuda"))
+        call(ref)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref), i
