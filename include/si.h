@@ -425,6 +425,99 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
                                  float scale, const int32_t* q_len, const int32_t* k_len, const uint32_t* blocks,
                                  si_heads* out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* A cache of keys and values in 4 bits.
+ *
+ * A token's head of dim_head channels is held in groups of 32 (the last may be
+ * shorter; G = ceil(dim_head / 32)): channel c of a group as an e2m1 code -- 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 for 0 .. 7, bit 3 the sign -- in the low (c even) or high half
+ * of byte c / 2, and one byte s for the group; the value is code * 2^(s - 127), and
+ * NaN where s is 255.  Device arrays
+ *   codes   [B][heads][capacity][16 G]
+ *   scales  [B][heads][capacity][S], S = 1, 2, 4, 4 for G = 1 .. 4
+ * each for keys and for values, 16-byte aligned, contiguous: 16 G + S bytes for a
+ * token's head (dim_head 128: 68, where bf16 has 256).  Codes of channels past
+ * dim_head are zero, and a fourth scale of three groups is not read.  dim_head is a
+ * multiple of 8, at most 128.  capacity == 0 is legal (the arrays may then be NULL).
+ * Tokens are kept as they come (rotated before they are stored, where positions are
+ * wanted): attention does not depend on the order of what a query sees.
+ * At most (SI_ERR_SHAPE beyond): B 2^24, heads 65535, B * heads 2^28, capacity
+ * 2^31 - 1 - 2^22, 2^40 tokens of all heads, workgroups of 16 tokens and more below
+ * 2^32 - 2^20. */
+typedef struct {
+  void *k_codes, *k_scales, *v_codes, *v_scales; /* device */
+  int64_t B, heads, capacity, dim_head;
+} si_cache4;
+
+/* Stores tokens of k and v (heads of the cache's shape, one dtype, bf16 or float32):
+ * token n of batch entry b goes to slot first[b] + n of every head, for n <
+ * length[b] (device int32 [B], NULL: 0 and N; lengths are clamped to [0, N]).  A
+ * token whose slot is negative or at or past the capacity is left out; nothing else
+ * in the cache changes.  For a group of largest magnitude m,
+ *   s = the smallest byte with m <= 7 * 2^(s - 127), but 2 at least and 252 at most,
+ *   code = the nearest to x / 2^(s - 127), ties to the even code, at most 6;
+ * a NaN or an infinity makes s 255 and the codes zero.
+ * weight: NULL, or [B][heads][capacity] (si_cache4_attn_forward), set to zero at the
+ * slots that are stored to. */
+si_status si_cache4_store(const si_heads* k, const si_heads* v, const int32_t* first, const int32_t* length, const si_cache4* cache,
+                          float* weight, void* stream);
+
+/* The other way round: token n of k and v receives the values of slot first[b] + n.
+ * Values are exact in both dtypes.  Tokens at and behind length, and those whose
+ * slot the cache does not have, are left as they were. */
+si_status si_cache4_load(const si_cache4* cache, const int32_t* first, const int32_t* length, si_heads* k, si_heads* v, void* stream);
+
+/* Attention of new tokens over the cache, the new ones (already stored) among its
+ * first k_len[b] slots.
+ *
+ *   out[b, n, h] = sum_j softmax_j(scale * <q[b, n, h], k[b, j, hk]>) v[b, j, hk], hk = h / (q->heads / cache->heads)
+ *   weight_out[b, hk, j] = decay * weight_in[b, hk, j] + sum over n < q_len[b] and the heads h of hk of that softmax weight
+ *
+ * run == 0: every query sees slots j < k_len[b].  run >= 1: the queries are the last
+ * q_len[b] of these slots, in runs (frames) of `run` tokens, and a query sees its own
+ * run and what lies before: j < k_len[b] - q_len[b] + min((n / run + 1) * run, q_len[b]);
+ * run == 1: nothing behind itself.  q_len, k_len: device int32 [B], NULL: N,
+ * capacity; clamped to [0, N], [0, capacity].  What no query sees may hold anything.
+ * A row that sees no key gives zeros and adds no weight; rows at and behind q_len
+ * are left as they were.  A NaN among the keys that a row sees, or a score of
+ * +infinity, makes the row NaN, and the weight of all that it sees; a NaN among the
+ * values that it sees makes the 32 channels of that group NaN.
+ * weight_out NULL: no weights.  weight_in NULL: zeros; it may be weight_out itself,
+ * and otherwise lies apart.  Slots at and behind k_len are left as they were.
+ * decay >= 0, read with weight_in.
+ * scale > 0.  q and out: one dtype.  The cache's values are taken exactly.  bf16:
+ * probabilities are rounded to bf16 for the second product and for the sum that
+ * divides it, everything else is float32 and so are the weights; float32: float32
+ * throughout.  Finite scores times scale are at most 1e9 in magnitude.  The same
+ * operands give the same bits.
+ * workspace: device, 256-byte aligned, contents ignored; calls that overlap in time
+ * must not share one.  (q->heads / cache->heads) * N is below 2^31 - 2^20, and so are
+ * the row tiles (of 16 rows and more) of all key heads (SI_ERR_SHAPE).
+ * si_cache4_attn_workspace_bytes: weights != 0 where weight_out will be given; 0 if
+ * the arguments are invalid.  Host-only. */
+size_t si_cache4_attn_workspace_bytes(const si_heads* q, const si_cache4* cache, int64_t run, int32_t weights);
+si_status si_cache4_attn_forward(const si_heads* q, const si_cache4* cache, float scale, int64_t run, const int32_t* q_len,
+                                 const int32_t* k_len, const float* weight_in, float decay, float* weight_out, si_heads* out,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction: of every batch entry and head the `keep` slots that stay, moved in their
+ * order to the first slots of another cache.  With n = k_len[b] (NULL: capacity;
+ * clamped) at most `keep` all stay.  Otherwise the first `first` and the last `last`
+ * of the n stay, and of those between them the keep - first - last with the largest
+ * weight; equal weights: the lowest slot; a NaN ranks as -infinity.
+ *   out         a cache of the same B, heads and dim_head, capacity >= min(keep,
+ *               capacity), apart from `cache`; m = min(n, keep) slots are written
+ *   weight_out  [B][heads][out capacity]: the weights of what stayed
+ *   kept        device int32 [B][heads][keep]: the slots that it had
+ *   out_len     device int32 [B]: m
+ * Of weight_out and kept, what lies behind m is left as it was.  keep >= 1, first and
+ * last >= 0, first + last <= keep (SI_ERR_ARG).
+ * workspace: device, 256-byte aligned, contents ignored; calls that overlap in time
+ * must not share one. */
+size_t si_cache4_evict_workspace_bytes(const si_cache4* cache, int64_t keep);
+si_status si_cache4_evict(const si_cache4* cache, const int32_t* k_len, const float* weight, int64_t keep, int64_t first, int64_t last,
+                          const si_cache4* out, float* weight_out, int32_t* kept, int32_t* out_len, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
 /* A spatial block whose self-attention takes rotary positions and attends over
  * selected key blocks; everything else as si_block_forward_ex (same flags).
  *   rope     NULL: queries and keys are not rotated.  Else, after their projection,

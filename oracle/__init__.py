@@ -1,5 +1,6 @@
 """CPU oracle for the sliced transformer-block forward, the Step Rehash test and walks, and the
-Spatial ResBlock operator group with its Up/DownSample, and the operators on heads of video tokens.
+Spatial ResBlock operator group with its Up/DownSample, the operators on heads of video tokens, and the
+cache of keys and values in 4 bits.
 
 TEST INFRASTRUCTURE ONLY.  Plain NumPy in float64, full tensors, one operator
 after the other, no blocking or fusion.  Nothing here is imported by the HIP
@@ -28,4 +29,7 @@ from .resblock_ref import (  # noqa: F401
 from .attn_ref import (  # noqa: F401
     rope_angles_ref, rms_norm_ref, rope_ref, block_scores_ref, pack_blocks_ref, select_ref, sparse_attention_ref,
     block_forward_attn_ref,
+)
+from .cache4_ref import (  # noqa: F401
+    scale_room_ref, encode_group_ref, encode_ref, decode_ref, seen_ref, cache_attention_ref, evict_ref,
 )

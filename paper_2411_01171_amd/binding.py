@@ -72,6 +72,11 @@ class _AttnOptions(C.Structure):
     _fields_ = [("rope", C.POINTER(_Rope)), ("q_block", C.c_int64), ("k_block", C.c_int64), ("keep", C.c_int64)]
 
 
+class _Cache4(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+                ("B", C.c_int64), ("heads", C.c_int64), ("capacity", C.c_int64), ("dim_head", C.c_int64)]
+
+
 class _RehashCache(C.Structure):
     _fields_ = [("x_key", C.c_void_p), ("y_key", C.c_void_p), ("valid", C.c_int32)]
 
@@ -126,6 +131,19 @@ def lib() -> C.CDLL:
     L.si_attn_sparse_workspace_bytes.argtypes = [ph, ph, i64, i64]
     L.si_attn_sparse_forward.restype = i32
     L.si_attn_sparse_forward.argtypes = [ph, ph, ph, i64, i64, C.c_float, vp, vp, vp, ph, vp, sz, vp]
+    pc = C.POINTER(_Cache4)
+    L.si_cache4_store.restype = i32
+    L.si_cache4_store.argtypes = [ph, ph, vp, vp, pc, vp, vp]
+    L.si_cache4_load.restype = i32
+    L.si_cache4_load.argtypes = [pc, vp, vp, ph, ph, vp]
+    L.si_cache4_attn_workspace_bytes.restype = sz
+    L.si_cache4_attn_workspace_bytes.argtypes = [ph, pc, i64, i32]
+    L.si_cache4_attn_forward.restype = i32
+    L.si_cache4_attn_forward.argtypes = [ph, pc, C.c_float, i64, vp, vp, vp, C.c_float, vp, ph, vp, sz, vp]
+    L.si_cache4_evict_workspace_bytes.restype = sz
+    L.si_cache4_evict_workspace_bytes.argtypes = [pc, i64]
+    L.si_cache4_evict.restype = i32
+    L.si_cache4_evict.argtypes = [pc, vp, vp, i64, i64, i64, pc, vp, vp, vp, vp, sz, vp]
     po = C.POINTER(_AttnOptions)
     L.si_block_attn_workspace_bytes.restype = sz
     L.si_block_attn_workspace_bytes.argtypes = L.si_workspace_bytes.argtypes[:3] + [po, i32, i64]
@@ -441,6 +459,96 @@ def si_attn_sparse_forward(q, k, v, q_block: int, k_block: int, blocks, out, wor
     _call("si_attn_sparse_forward", stream, (q, k, v, blocks, out, workspace, q_len, k_len),
           (C.byref(_heads(q)), C.byref(_heads(k)), C.byref(_heads(v)), q_block, k_block, q.shape[3] ** -0.5 if scale is None else scale,
            ql, kl, bits, C.byref(_heads(out)), workspace.data_ptr(), workspace.nbytes))
+
+
+class Cache4:
+    """Keys and values in 4 bits: si_cache4 over uint8 tensors codes [B, heads, capacity, 16 G], scales [B, heads, capacity, S]."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, dim_head: int):
+        import torch
+        groups, room = self.row_bytes(dim_head)
+        self.tensors = (k_codes, k_scales, v_codes, v_scales)
+        for t, n in zip(self.tensors, (groups, room, groups, room)):
+            if t.dtype != torch.uint8 or t.dim() != 4 or tuple(t.shape) != (*k_codes.shape[:3], n) or not t.is_contiguous():
+                raise ValueError(f"codes and scales must be contiguous uint8 tensors [B, heads, capacity, {groups}] and [.., {room}]")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = self.tensors
+        self.dim_head = dim_head
+        self.struct = _Cache4(*(t.data_ptr() for t in self.tensors), *k_codes.shape[:3], dim_head)
+
+    @staticmethod
+    def row_bytes(dim_head: int) -> Tuple[int, int]:
+        """Bytes of a token's codes and of its scales."""
+        if dim_head < 8 or dim_head > 128 or dim_head % 8:
+            raise ValueError("dim_head must be a multiple of 8, at most 128")
+        groups = -(-dim_head // 32)
+        return 16 * groups, (1, 2, 4, 4)[groups - 1]
+
+    @classmethod
+    def empty(cls, B: int, heads: int, capacity: int, dim_head: int, device="cuda") -> "Cache4":
+        import torch
+        codes, scales = cls.row_bytes(dim_head)
+        return cls(*(torch.empty(B, heads, capacity, n, dtype=torch.uint8, device=device) for n in (codes, scales, codes, scales)), dim_head)
+
+    @property
+    def shape(self) -> Tuple[int, int, int, int]:
+        """B, heads, capacity, dim_head."""
+        return (*self.k_codes.shape[:3], self.dim_head)
+
+
+def _weights(t, cache: Cache4, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.float32 or tuple(t.shape) != cache.shape[:3] or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 tensor {list(cache.shape[:3])}")
+    return t.data_ptr()
+
+
+def si_cache4_store(k, v, cache: Cache4, first=None, length=None, weight=None, stream=None) -> None:
+    """Stores the tokens of k and v [B,N,heads,dim_head] from slot first[b] on (int32 [B]; None: 0), length[b] of them (None: N).
+    weight: zeroed at these slots."""
+    B = cache.shape[0]
+    args = (C.byref(_heads(k)), C.byref(_heads(v)), _lengths(first, B), _lengths(length, B), C.byref(cache.struct), _weights(weight, cache, "weight"))
+    _call("si_cache4_store", stream, (k, v, first, length, weight, *cache.tensors), args)
+
+
+def si_cache4_load(cache: Cache4, k, v, first=None, length=None, stream=None) -> None:
+    """Writes what slots first[b] + n stand for to the tokens of k and v."""
+    B = cache.shape[0]
+    args = (C.byref(cache.struct), _lengths(first, B), _lengths(length, B), C.byref(_heads(k)), C.byref(_heads(v)))
+    _call("si_cache4_load", stream, (k, v, first, length, *cache.tensors), args)
+
+
+def si_cache4_attn_workspace_bytes(q, cache: Cache4, run: int = 0, weights: bool = False) -> int:
+    return int(lib().si_cache4_attn_workspace_bytes(C.byref(_heads(q)), C.byref(cache.struct), run, int(bool(weights))))
+
+
+def si_cache4_attn_forward(q, cache: Cache4, out, workspace, scale: Optional[float] = None, q_len=None, k_len=None, run: int = 0,
+                           weight_in=None, weight_out=None, decay: float = 1.0, stream=None) -> None:
+    """Attention of q [B,N,heads,dim_head] over the first k_len[b] slots; run > 0: a query sees no later run of `run` queries.
+    scale: 1/sqrt(dim_head) unless given.  weight_out = decay * weight_in + the softmax weight that every slot received."""
+    B = cache.shape[0]
+    args = (C.byref(_heads(q)), C.byref(cache.struct), q.shape[3] ** -0.5 if scale is None else scale, run, _lengths(q_len, B), _lengths(k_len, B),
+            _weights(weight_in, cache, "weight_in"), decay, _weights(weight_out, cache, "weight_out"), C.byref(_heads(out)),
+            workspace.data_ptr(), workspace.nbytes)
+    _call("si_cache4_attn_forward", stream, (q, out, workspace, q_len, k_len, weight_in, weight_out, *cache.tensors), args)
+
+
+def si_cache4_evict_workspace_bytes(cache: Cache4, keep: int) -> int:
+    return int(lib().si_cache4_evict_workspace_bytes(C.byref(cache.struct), keep))
+
+
+def si_cache4_evict(cache: Cache4, weight, keep: int, out: Cache4, weight_out, kept, out_len, workspace, first: int = 0, last: int = 0,
+                    k_len=None, stream=None) -> None:
+    """Moves the `keep` slots that stay (the first `first`, the last `last`, and the largest weights between) to `out`, with their
+    weights; kept int32 [B, heads, keep] receives the slots that they had, out_len int32 [B] how many there are."""
+    import torch
+    B, heads = cache.shape[:2]
+    if kept.dtype != torch.int32 or tuple(kept.shape) != (B, heads, keep) or not kept.is_contiguous():
+        raise ValueError(f"kept must be a contiguous int32 tensor {[B, heads, keep]}")
+    args = (C.byref(cache.struct), _lengths(k_len, B), _weights(weight, cache, "weight"), keep, first, last, C.byref(out.struct),
+            _weights(weight_out, out, "weight_out"), kept.data_ptr(), _lengths(out_len, B), workspace.data_ptr(), workspace.nbytes)
+    _call("si_cache4_evict", stream, (weight, weight_out, kept, out_len, workspace, k_len, *cache.tensors, *out.tensors), args)
 
 
 class AttnOptions:

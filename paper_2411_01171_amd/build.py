@@ -9,7 +9,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libsi.so")
-SOURCES = ("si_api.hip", "si_attn_ops.hip")
+SOURCES = ("si_api.hip", "si_attn_ops.hip", "si_cache4.hip")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

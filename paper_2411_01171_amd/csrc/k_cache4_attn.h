@@ -1,0 +1,565 @@
+// Attention of new tokens over a cache in 4 bits (k_cache4.h), and the weight that every cached token received.
+//
+// All queries of a key head walk the same keys, or with runs those up to the end of their own run.  The rows of a key head
+// (tokens times the query heads that share it) are cut into tiles, a tile's keys into steps of 32 that are dealt out to the
+// wavefronts of a workgroup and, where there are few tiles, to several workgroups.  Every wavefront keeps the running maximum
+// and sum of a softmax and its own output; they are joined in a fixed order.
+//   S^T[key, row] = K Q^T       row operand: keys, column operand: rows
+//   O^T[chan, row] += V^T P^T   column operand: the softmax result registers as they stand
+// Codes are read once, become bf16 (exactly) in registers, and go to the matrix cores: keys straight from where they were
+// loaded, as a lane's channels of a key lie next to each other there; values by way of LDS, which transposes them.
+// float32 queries are three bf16 parts whose sum is the value, and so are their probabilities: the products are exact and
+// the sums float32.
+#pragma once
+#include "k_attn_sparse.h"
+#include "k_cache4.h"
+
+namespace si {
+
+struct CacheAttnArgs {
+  const void* q;
+  void* o;
+  int64_t qb, qn, qh, ob, on, oh;  // strides in elements
+  Cache4View c;
+  const int *q_len, *k_len;  // per batch entry, or NULL
+  int Nq, group, d;
+  int run;                   // tokens of a run, 0: every query sees every key
+  int runs, run_len;         // of the tiling: tiles end with a run unless a run is shorter than a tile
+  int tiles_per_run;
+  unsigned work;             // B * heads * runs * tiles_per_run * nsplit
+  int nsplit;
+  float scale_log2;          // softmax scale * log2(e)
+  float* part;               // nsplit > 1: outputs [query row][nsplit][d]; query row = (b Nq + n) heads + h
+  f32x4_t* part_stat;        // nsplit > 1: (maximum, sum of the rounded weights, sum of the weights) [query row][nsplit]
+  float2* row_stat;          // or NULL: (maximum, 1 / sum of the weights) [query row]
+};
+
+// Batch entry, key head, tile and share of a piece of work, and which keys its rows see.
+struct CacheTile {
+  int part, tile, run, hk, b, q_len, k_len;
+  __device__ __forceinline__ CacheTile(const CacheAttnArgs& a, unsigned work) {
+    auto pop = [&](int n) {  // the fastest index
+      const unsigned up = work / (unsigned)n;
+      const int i = (int)(work - up * n);
+      work = up;
+      return i;
+    };
+    part = a.nsplit > 1 ? pop(a.nsplit) : 0;
+    tile = a.tiles_per_run > 1 ? pop(a.tiles_per_run) : 0;
+    run = a.runs > 1 ? pop(a.runs) : 0;
+    hk = pop(a.c.heads);
+    b = (int)work;
+    q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq;
+    k_len = a.k_len ? min(max(a.k_len[b], 0), a.c.cap) : a.c.cap;
+  }
+  // token of row `rho` of the tiling's run, or -1; sub: its head among those of the key head
+  __device__ __forceinline__ int token(const CacheAttnArgs& a, int rho, int& sub) const {
+    const int in_run = a.group > 1 ? rho / a.group : rho;
+    const int64_t n = (int64_t)run * a.run_len + in_run;
+    sub = rho - in_run * a.group;
+    return in_run < a.run_len && n < q_len ? (int)n : -1;
+  }
+  // keys that token n sees, the first so many
+  __device__ __forceinline__ int seen(const CacheAttnArgs& a, int n) const { return cache_seen(a.run, n, q_len, k_len); }
+  __device__ __forceinline__ static int cache_seen(int run, int n, int q_len, int k_len) {
+    if (run == 0) return k_len;
+    const int64_t end = min(((int64_t)(n / run) + 1) * run, (int64_t)q_len);
+    return (int)max((int64_t)0, k_len - q_len + end);
+  }
+};
+
+// A pair of values as bf16 parts: one, rounded, or three that add up to it, eight of its 24 bits each.
+template <int TERMS>
+__device__ __forceinline__ void bf16_parts(float lo, float hi, unsigned (&out)[TERMS]) {
+  if constexpr (TERMS == 1) {
+    out[0] = pack_bf16x2(lo, hi);
+  } else {
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) {
+      out[t] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);  // upper halves
+      lo -= __uint_as_float(out[t] << 16);
+      hi -= __uint_as_float(out[t] & 0xFFFF0000u);
+    }
+  }
+}
+
+// Eight query channels as column operands.
+template <typename T, int TERMS>
+__device__ __forceinline__ void query_parts(const T* p, u32x4_t (&out)[TERMS]) {
+  if constexpr (sizeof(T) == 2) {
+    out[0] = *reinterpret_cast<const u32x4_t*>(p);
+  } else {
+    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p), y = *reinterpret_cast<const f32x4_t*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      unsigned w[TERMS];
+      const float lo = i < 2 ? x[2 * i] : y[2 * i - 4], hi = i < 2 ? x[2 * i + 1] : y[2 * i - 3];
+      bf16_parts<TERMS>(lo, hi, w);
+      // an infinity's rest would be a NaN: it has none
+      if (__builtin_isinf(lo) || __builtin_isinf(hi))
+#pragma unroll
+        for (int t = 1; t < TERMS; ++t) w[t] &= (__builtin_isinf(lo) ? 0xFFFF0000u : ~0u) & (__builtin_isinf(hi) ? 0x0000FFFFu : ~0u);
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) out[t][i] = w[t];
+    }
+  }
+}
+
+// The codes of two tiles of 16 keys as the lanes of a row operand hold them: lane (r, g) channels 8 G g .. 8 G g + 8 G - 1 of keys
+// r and 16 + r, and the two keys' scales.
+template <int G>
+struct KeyCodes {
+  static constexpr int S = cache4_scale_bytes(G);
+  unsigned w[2][G];
+  unsigned s[2];
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int key0, int end, int r, int g) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int64_t key = min(key0 + 16 * t + r, end - 1);
+      const unsigned* p = reinterpret_cast<const unsigned*>(codes + key * (16 * G) + g * (4 * G));
+      if constexpr (G == 4) {
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[t][i] = v[i];
+      } else if constexpr (G == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[t][0] = v.x; w[t][1] = v.y;
+      } else {
+#pragma unroll
+        for (int i = 0; i < G; ++i) w[t][i] = p[i];
+      }
+      if constexpr (S == 4) s[t] = *reinterpret_cast<const unsigned*>(scales + key * 4);
+      else if constexpr (S == 2) s[t] = *reinterpret_cast<const unsigned short*>(scales + key * 2);
+      else s[t] = scales[key];
+    }
+  }
+  // Channels 8 G g + 8 i .. + 7 of key tile t.  Groups of 32 channels are 4 / G lanes' or, with three of them, end inside a lane's.
+  __device__ __forceinline__ u32x4_t operand(int t, int i, int g) const {
+    const unsigned group = G == 4 ? g : G == 2 ? g / 2 : G == 1 ? 0 : (3 * g + i) / 4;
+    return cache4_bf16x8(w[t][i], __uint_as_float(((s[t] >> (8 * group)) & 255u) << 23));
+  }
+};
+
+// Rows of up to 32 of a tile: four wavefronts that each take every fourth step of 32 keys.
+// T: of queries and outputs.  G: groups of 32 channels of a head.  NT: columns of rows, 16 each.
+template <typename T, int G, int NT>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? 4 : 2) void cache4_attn_few_kernel(CacheAttnArgs a) {
+  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
+  constexpr int ROW = G == 1 ? 64 : G == 2 ? 128 : 256;  // bytes of a key's values in LDS
+  constexpr int UNITS = 32 * G, PER = (UNITS + 63) / 64;  // groups of a step's values, and a lane's share
+  constexpr int KEEP = 2 * G * 4 * NT + 3 * NT;           // what a wavefront hands over at the end, a lane
+  constexpr int BYTES = 4 * 32 * ROW > 2 * KEEP * 256 ? 4 * 32 * ROW : 2 * KEEP * 256;
+  constexpr int SB = cache4_scale_bytes(G);
+  __shared__ __align__(1024) u32x4_t lds[BYTES / 16];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = lane % 16, g = lane / 16;
+  auto swizzle = [](int key) { return ROW == 64 ? (key >> 2) & 3 : ROW == 128 ? (key >> 1) & 7 : (key & 3) << 2 | ((key >> 2) & 3); };
+  const unsigned vals = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&lds[0]) + wave * 32 * ROW;
+
+  const unsigned chunk = (a.work + 7) / 8;  // contiguous per XCD: a head's codes are fetched into one L2
+  const unsigned chunk_end = min(a.work, (blockIdx.x % 8 + 1) * chunk);
+  for (unsigned work = blockIdx.x % 8 * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
+    const CacheTile t(a, work);
+    int first_sub;
+    const int first = t.token(a, t.tile * 16 * NT, first_sub);
+    if (first < 0) continue;  // the tile's first row is its earliest token
+    // keys that every row sees, and that any sees
+    const int64_t last = min(min((int64_t)t.run * a.run_len + min((t.tile * 16 * NT + 16 * NT - 1) / a.group, a.run_len - 1), (int64_t)t.q_len - 1), (int64_t)a.Nq - 1);
+    const int all = t.seen(a, first), any = t.seen(a, (int)last);
+    int token[NT], sub[NT], seen[NT];
+    u32x4_t q[NT][G][TERMS];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      token[c] = t.token(a, (t.tile * NT + c) * 16 + r, sub[c]);
+      seen[c] = token[c] < 0 ? any : t.seen(a, token[c]);
+      const T* row = static_cast<const T*>(a.q) + t.b * a.qb + (int64_t)max(token[c], 0) * a.qn + (int64_t)(t.hk * a.group + (token[c] < 0 ? 0 : sub[c])) * a.qh;
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const int ch = 8 * (G * g + i);
+#pragma unroll
+        for (int x = 0; x < TERMS; ++x) q[c][i][x] = u32x4_t{0, 0, 0, 0};
+        if (ch < a.d && token[c] >= 0) query_parts<T, TERMS>(row + ch, q[c][i]);
+      }
+    }
+    const int64_t head = ((int64_t)t.b * a.c.heads + t.hk) * a.c.cap;
+    const uint8_t *kc = a.c.kc + head * (16 * G), *ks = a.c.ks + head * SB, *vc = a.c.vc + head * (16 * G), *vs = a.c.vs + head * SB;
+
+    f32x4_t o[2 * G][NT];
+    float mref[NT], lsum[NT], lwt[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      mref[c] = kSparseLow;
+      lsum[c] = lwt[c] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2 * G; ++i) o[i][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    const unsigned steps = ((unsigned)any + 31u) / 32u;
+    const unsigned lo = (unsigned)((uint64_t)steps * t.part / a.nsplit), hi = (unsigned)((uint64_t)steps * (t.part + 1) / a.nsplit);
+    KeyCodes<G> kn;
+    u32x4_t vn[PER];
+    unsigned vsn[PER];
+    auto fetch = [&](unsigned step) {
+      const int key0 = (int)(step * 32);
+      kn.load(kc, ks, key0, any, r, g);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int unit = i * 64 + lane, key = key0 + unit / G, group = unit % G;
+        vn[i] = u32x4_t{0, 0, 0, 0};
+        vsn[i] = 127u;  // what no row sees counts as zero
+        if (unit < UNITS && key < any) {
+          vn[i] = *reinterpret_cast<const u32x4_t*>(vc + ((int64_t)key * G + group) * 16);
+          vsn[i] = vs[(int64_t)key * SB + group];
+        }
+      }
+    };
+    if (lo + wave < hi) fetch(lo + wave);
+    for (unsigned step = lo + wave; step < hi; step += 4) {
+      const int key0 = (int)(step * 32);
+      const KeyCodes<G> k = kn;
+      u32x4_t v[PER];
+      unsigned vsc[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) { v[i] = vn[i]; vsc[i] = vsn[i]; }
+      if (step + 4 < hi) fetch(step + 4);
+
+      // ---- values to LDS
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int unit = i * 64 + lane, key = unit / G, group = unit % G;
+        if (UNITS % 64 && unit >= UNITS) continue;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+          *reinterpret_cast<__attribute__((address_space(3))) u32x4_t*>((size_t)(vals + key * ROW + ((4 * group + p) ^ swizzle(key)) * 16)) =
+              cache4_bf16x8(v[i][p], __uint_as_float(vsc[i] << 23));
+      }
+      asm volatile("" ::: "memory");
+
+      // ---- scores
+      f32x4_t sc[2][NT];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int c = 0; c < NT; ++c) sc[u][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, k.operand(u, i, g));
+#pragma unroll
+          for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int x = TERMS - 1; x >= 0; --x)  // the smallest part first
+              sc[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8_t, q[c][i][x]), sc[u][c], 0, 0, 0);
+        }
+      const bool mixed = key0 + 32 > all;
+      if (mixed) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+          const int lim = seen[c] - key0 - 4 * g;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (16 * u + j >= lim) sc[u][c][j] = -INFINITY;
+        }
+      }
+
+      // ---- probabilities against a reference maximum that is raised only when a partial sum has grown past it
+      u32x4_t pk[NT][TERMS];
+      float rs[NT], rw[NT];
+      auto exponentiate = [&]() {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+          rs[c] = rw[c] = 0.f;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[u][c][j], a.scale_log2, -mref[c])), p1 = __builtin_amdgcn_exp2f(fmaf(sc[u][c][j + 1], a.scale_log2, -mref[c]));
+              unsigned w[TERMS];
+              bf16_parts<TERMS>(p0, p1, w);
+#pragma unroll
+              for (int x = 0; x < TERMS; ++x) pk[c][x][2 * u + j / 2] = w[x];
+              if constexpr (TERMS == 1) rs[c] = dot2_ones(w[0], rs[c]);
+              rw[c] += p0 + p1;
+            }
+          if constexpr (TERMS > 1) rs[c] = rw[c];
+        }
+      };
+      exponentiate();
+      bool grown = false;
+#pragma unroll
+      for (int c = 0; c < NT; ++c) grown = grown || !(rs[c] <= kSparseTrigger);
+      if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+          float mx = sc[0][c][0];
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[u][c][j]);
+          mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * a.scale_log2;  // the four parts of the row agree on the new reference
+          const float up = fmaxf(mx, mref[c]), alpha = __builtin_amdgcn_exp2f(mref[c] - up);
+          mref[c] = up;
+          lsum[c] *= alpha;
+          lwt[c] *= alpha;
+#pragma unroll
+          for (int i = 0; i < 2 * G; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][c][j] *= alpha;
+        }
+        exponentiate();
+      }
+#pragma unroll
+      for (int c = 0; c < NT; ++c) { lsum[c] += rs[c]; lwt[c] += rw[c]; }
+
+      // ---- O^T += V^T P^T: slots e < 4 of group g are keys 4 g + e, the others 16 + 4 g + e - 4
+#pragma unroll
+      for (int i = 0; i < 2 * G; ++i) {
+        const int row = 4 * g + r / 4, piece = 2 * i + (r % 4) / 2;
+        const uint2 x = lds_read_tr(vals + row * ROW + (piece ^ swizzle(row)) * 16 + (r % 2) * 8);
+        const uint2 y = lds_read_tr(vals + (16 + row) * ROW + (piece ^ swizzle(16 + row)) * 16 + (r % 2) * 8);
+        u32x4_t vf{x.x, x.y, y.x, y.y};
+        if (mixed) {
+          // A NaN among the values is one for the rows that see its key, and nothing for the others, whose weight of zero would
+          // not hide it.
+          u32x4_t bad;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const unsigned low = (vf[w] & 0x7FFFu) > 0x7F80u ? 0xFFFFu : 0u, high = (vf[w] & 0x7FFF0000u) > 0x7F800000u ? 0xFFFF0000u : 0u;
+            bad[w] = (low | high) & 0x3F803F80u;
+            vf[w] &= ~(low | high);
+          }
+          if (__builtin_amdgcn_ballot_w64((bad[0] | bad[1] | bad[2] | bad[3]) != 0u) != 0) {
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+              const int lim = seen[c] - key0 - 4 * g;
+              u32x4_t sees;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                const int key = 16 * (w / 2) + 2 * (w % 2);
+                sees[w] = (key < lim ? 0x3F80u : 0u) | (key + 1 < lim ? 0x3F800000u : 0u);
+              }
+              const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, bad), __builtin_bit_cast(bf16x8_t, sees), f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (hit[j] > 0.f) o[i][c][j] = NAN;
+            }
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+          for (int x2 = TERMS - 1; x2 >= 0; --x2)
+            o[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[c][x2]), o[i][c], 0, 0, 0);
+      }
+      asm volatile("" ::: "memory");
+    }
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      lsum[c] += __shfl_xor(lsum[c], 16, kWave);
+      lsum[c] += __shfl_xor(lsum[c], 32, kWave);
+      lwt[c] += __shfl_xor(lwt[c], 16, kWave);
+      lwt[c] += __shfl_xor(lwt[c], 32, kWave);
+    }
+
+    // ---- four wavefronts' results become one: 2 and 3 into 0 and 1, then 1 into 0
+    float* img = reinterpret_cast<float*>(&lds[0]) + lane;
+#pragma unroll
+    for (int half = 2; half >= 1; half /= 2) {
+      __syncthreads();
+      if (wave >= half && wave < 2 * half) {
+        float* to = img + (wave - half) * KEEP * kWave;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+#pragma unroll
+          for (int i = 0; i < 2 * G; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[((c * 2 * G + i) * 4 + j) * kWave] = o[i][c][j];
+          to[(8 * G * NT + 3 * c) * kWave] = mref[c];
+          to[(8 * G * NT + 3 * c + 1) * kWave] = lsum[c];
+          to[(8 * G * NT + 3 * c + 2) * kWave] = lwt[c];
+        }
+      }
+      __syncthreads();
+      if (wave < half) {
+        const float* from = img + wave * KEEP * kWave;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+          const float m2 = from[(8 * G * NT + 3 * c) * kWave], top = fmaxf(mref[c], m2);
+          const float w1 = __builtin_amdgcn_exp2f(mref[c] - top), w2 = __builtin_amdgcn_exp2f(m2 - top);
+          mref[c] = top;
+          lsum[c] = lsum[c] * w1 + from[(8 * G * NT + 3 * c + 1) * kWave] * w2;
+          lwt[c] = lwt[c] * w1 + from[(8 * G * NT + 3 * c + 2) * kWave] * w2;
+#pragma unroll
+          for (int i = 0; i < 2 * G; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][c][j] = o[i][c][j] * w1 + from[((c * 2 * G + i) * 4 + j) * kWave] * w2;
+        }
+      }
+    }
+    if (wave == 0) {
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        if (token[c] < 0) continue;
+        const int h = t.hk * a.group + sub[c];
+        const int64_t row = ((int64_t)t.b * a.Nq + token[c]) * (a.c.heads * a.group) + h;
+        const float inv = lsum[c] == 0.f ? 0.f : 1.f / lsum[c];  // a row without keys gives zero
+        T* dst = static_cast<T*>(a.o) + t.b * a.ob + (int64_t)token[c] * a.on + (int64_t)h * a.oh;
+#pragma unroll
+        for (int i = 0; i < 2 * G; ++i) {
+          const int ch = 16 * i + 4 * g;
+          if (ch >= a.d) continue;
+          if (a.nsplit > 1) {
+            *reinterpret_cast<f32x4_t*>(a.part + (row * a.nsplit + t.part) * a.d + ch) = o[i][c];
+            continue;
+          }
+          f32x4_t y = o[i][c];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = lsum[c] == 0.f ? 0.f : y[j] * inv;
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst + ch) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+          else *reinterpret_cast<f32x4_t*>(dst + ch) = y;
+        }
+        if (g == 0) {
+          if (a.nsplit > 1) a.part_stat[row * a.nsplit + t.part] = f32x4_t{mref[c], lsum[c], lwt[c], 0.f};
+          else if (a.row_stat) a.row_stat[row] = make_float2(mref[c], lwt[c] == 0.f ? 0.f : 1.f / lwt[c]);
+        }
+      }
+    }
+    __syncthreads();  // the next tile's values overwrite what was handed over
+  }
+}
+
+// The shares of a query row joined: weights 2^(m - max m).  A wavefront per row: its lanes hold one share's maximum and sums
+// each (nsplit <= 64), then 64 / (d / 4) shares' outputs at a time, four channels per lane; the order of the sums is fixed.
+template <typename T>
+__global__ __launch_bounds__(256) void cache4_join_kernel(CacheAttnArgs a, int rows) {
+  const int lane = threadIdx.x % kWave, heads = a.c.heads * a.group, quads = a.d / 4;
+  // lanes of one share: the next power of two of quads
+  const int width = quads <= 2 ? 2 : quads <= 4 ? 4 : quads <= 8 ? 8 : quads <= 16 ? 16 : 32, at_once = kWave / width;
+  const int quad = lane % width, which = lane / width;
+  const int row = (int)blockIdx.x * 4 + threadIdx.x / kWave;
+  if (row >= rows) return;
+  const int bn = row / heads;
+  const int h = row - bn * heads, b = bn / a.Nq, token = bn - b * a.Nq;
+  if (a.q_len && token >= a.q_len[b]) return;
+  const f32x4_t stat = lane < a.nsplit ? a.part_stat[(int64_t)row * a.nsplit + lane] : f32x4_t{kSparseLow, 0.f, 0.f, 0.f};
+  const float top = wave_max(stat[0]), w = __builtin_amdgcn_exp2f(stat[0] - top);
+  const float l = wave_sum(stat[1] * w), lw = wave_sum(stat[2] * w);
+  const float* src = a.part + (int64_t)row * a.nsplit * a.d + 4 * quad;
+  f32x4_t o{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < a.nsplit; s0 += 4 * at_once) {
+    f32x4_t x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + u * at_once + which;
+      x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (s < a.nsplit && quad < quads) x[u] = *reinterpret_cast<const f32x4_t*>(src + (int64_t)s * a.d);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float ws = __shfl(w, (s0 + u * at_once + which) % kWave, kWave);  // past the last share: times zero
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = fmaf(x[u][j], ws, o[j]);
+    }
+  }
+  for (int step = width; step < kWave; step <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], step, kWave);
+  if (a.row_stat && lane == 0) a.row_stat[row] = make_float2(top, lw == 0.f ? 0.f : 1.f / lw);
+  if (which != 0 || quad >= quads) return;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : o[j] * inv;
+  T* dst = static_cast<T*>(a.o) + b * a.ob + (int64_t)token * a.on + (int64_t)h * a.oh + 4 * quad;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+  else *reinterpret_cast<f32x4_t*>(dst) = o;
+}
+
+struct CacheWeightArgs {
+  const void* q;
+  int64_t qb, qn, qh;
+  Cache4View c;
+  const int *q_len, *k_len;
+  int Nq, group, d, run;
+  int chunks;                // of 128 keys
+  unsigned work;             // B * heads * chunks
+  float scale_log2, decay;
+  const float2* row_stat;
+  const float* in;           // or NULL: zeros
+  float* out;
+};
+
+// out[key] = decay in[key] + sum over the rows that see it of their softmax weight, in an order that depends on sizes only.  The scores are
+// taken again, against the rows' maxima and sums of the whole call.  A wavefront keeps 32 keys and walks the rows.
+template <typename T, int G>
+__global__ __launch_bounds__(256) void cache4_weight_kernel(CacheWeightArgs a) {
+  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
+  constexpr int SB = cache4_scale_bytes(G);
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = lane % 16, g = lane / 16;
+  const unsigned part = (a.work + 7) / 8, part_end = min(a.work, (blockIdx.x % 8 + 1) * part);
+  for (unsigned work = blockIdx.x % 8 * part + blockIdx.x / 8; work < part_end; work += gridDim.x / 8) {
+    const unsigned bh = work / (unsigned)a.chunks;
+    const int b = (int)(bh / (unsigned)a.c.heads), hk = (int)(bh % (unsigned)a.c.heads);
+    const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.c.cap) : a.c.cap;
+    const int64_t key64 = (int64_t)(work % (unsigned)a.chunks) * 128 + wave * 32;
+    if (key64 >= k_len) continue;
+    const int key0 = (int)key64;
+    const int64_t head = ((int64_t)b * a.c.heads + hk) * a.c.cap;
+    KeyCodes<G> k;
+    k.load(a.c.kc + head * (16 * G), a.c.ks + head * SB, key0, k_len, r, g);
+    bf16x8_t kf[2][G];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < G; ++i) kf[u][i] = __builtin_bit_cast(bf16x8_t, k.operand(u, i, g));
+    f32x4_t sum[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+    const int64_t rows = (int64_t)q_len * a.group;
+    for (int64_t rho0 = 0; rho0 < rows; rho0 += 16) {
+      const int64_t rho = min(rho0 + r, rows - 1);
+      const int n = (int)(rho / a.group), h = hk * a.group + (int)(rho % a.group);
+      const int seen = CacheTile::cache_seen(a.run, n, q_len, k_len);
+      float2 stat = a.row_stat[((int64_t)b * a.Nq + n) * (a.c.heads * a.group) + h];
+      if (rho0 + r >= rows) stat = make_float2(INFINITY, 0.f);  // no row: 2^-inf
+      const T* row = static_cast<const T*>(a.q) + b * a.qb + (int64_t)n * a.qn + (int64_t)h * a.qh;
+      f32x4_t sc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const int ch = 8 * (G * g + i);
+        u32x4_t q[TERMS];
+#pragma unroll
+        for (int x = 0; x < TERMS; ++x) q[x] = u32x4_t{0, 0, 0, 0};
+        if (ch < a.d) query_parts<T, TERMS>(row + ch, q);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int x = TERMS - 1; x >= 0; --x)
+            sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u][i], __builtin_bit_cast(bf16x8_t, q[x]), sc[u], 0, 0, 0);
+      }
+      const int lim = rho0 + r >= rows ? 0 : seen - key0 - 4 * g;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][j], a.scale_log2, -stat.x)) * stat.y;
+          sum[u][j] += 16 * u + j < lim ? p : 0.f;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int step = 1; step < 16; step <<= 1) sum[u][j] += __shfl_xor(sum[u][j], step, kWave);
+      // lane (r, g) holds keys 4 g + j of the tile: lanes r < 4 write them
+      const int key = key0 + 16 * u + 4 * g + r;
+      const float mine = r == 0 ? sum[u][0] : r == 1 ? sum[u][1] : r == 2 ? sum[u][2] : sum[u][3];
+      if (r < 4 && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + mine;
+    }
+  }
+}
+
+}  // namespace si

@@ -22,11 +22,6 @@ namespace si {
 
 constexpr int kRopeThreads = 256, kRopeHeads = 4, kRopeMaxPairs = 64;
 
-struct HeadsView {  // element (b, n, h, c) at p + b*sb + n*sn + h*sh + c
-  void* p;
-  int64_t sb, sn, sh;
-};
-
 struct RopeArgs {
   HeadsView q, k, qo, ko;
   const void *q_gain, *k_gain;

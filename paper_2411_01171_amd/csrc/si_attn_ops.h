@@ -1,4 +1,4 @@
-// Operators on heads of video tokens, as the spatial block's path calls them (defined in si_attn_ops.hip).
+// Operators on heads of video tokens, as the spatial block's path calls them, and checks of heads (defined in si_attn_ops.hip).
 #pragma once
 #include "../../include/si.h"
 
@@ -6,6 +6,8 @@
 
 namespace si {
 
+constexpr int64_t kMostTokens = INT32_MAX - (1 << 22);  // of a sequence: kernels add tiles to token numbers in 31 bits
+constexpr int64_t kGridMost = 1 << 20;                  // workgroups of a launch; kernels walk longer lists
 constexpr int64_t kSelectMaxBlocks = 16384;  // one run's scores fill the LDS of a workgroup
 
 struct BlocksPlan {
@@ -19,6 +21,14 @@ struct SparsePlan {
   int64_t rows;  // of all queries and heads
   size_t part_bytes;
 };
+
+// Elements from the first to behind the last one, over the dimensions whose stride is below `below`.
+int64_t heads_extent(const si_heads* t, int64_t below = INT64_MAX);
+// Sizes, strides and alignment of one operand.  `written`: its elements must have addresses of their own.
+si_status check_heads(const si_heads* t, bool written);
+// Whether no element of one lies on an element of the other.
+bool heads_apart(const si_heads* a, const si_heads* b);
+bool heads_overlap_range(const si_heads* t, const void* p, size_t bytes);
 
 si_status check_rope(const si_rope* r, int d);
 bool rope_gain_in(const si_rope* r, int d, int esize, const void* p, size_t bytes);

@@ -13,15 +13,13 @@
 
 namespace si {
 
-constexpr int64_t kMostTokens = INT32_MAX - (1 << 22);  // of a sequence: kernels add tiles to token numbers in 31 bits
 constexpr int64_t kMostOfBlock = 1 << 20;               // tokens of a run or a key block
 
 static inline HeadsView view_of(const si_heads* t) { return HeadsView{t->ptr, t->stride_b, t->stride_n, t->stride_h}; }
 static inline int heads_esize(const si_heads* t) { return t->dtype == SI_F32 ? 4 : 2; }
 static inline bool heads_empty(const si_heads* t) { return t->N == 0; }
 
-// Elements from the first to behind the last one, over the dimensions whose stride is below `below`.
-static int64_t heads_extent(const si_heads* t, int64_t below = INT64_MAX) {
+int64_t heads_extent(const si_heads* t, int64_t below) {
   int64_t e = t->dim_head;
   const int64_t n[] = {t->B, t->N, t->heads}, s[] = {t->stride_b, t->stride_n, t->stride_h};
   for (int i = 0; i < 3; ++i)
@@ -29,8 +27,7 @@ static int64_t heads_extent(const si_heads* t, int64_t below = INT64_MAX) {
   return e;
 }
 
-// Sizes, strides and alignment of one operand.  `written`: its elements must have addresses of their own.
-static si_status check_heads(const si_heads* t, bool written) {
+si_status check_heads(const si_heads* t, bool written) {
   if (!t) return SI_ERR_NULL;
   if (t->dtype != SI_F32 && t->dtype != SI_BF16) return SI_ERR_DTYPE;
   if (t->B < 1 || t->N < 0 || t->heads < 1 || t->dim_head < 8 || t->dim_head > 128 || t->dim_head % 8) return SI_ERR_SHAPE;
@@ -65,9 +62,9 @@ static bool same_heads(const si_heads* a, const si_heads* b) {
          (a->B <= 1 || a->stride_b == b->stride_b) && (a->N <= 1 || a->stride_n == b->stride_n) && (a->heads <= 1 || a->stride_h == b->stride_h);
 }
 
-// Whether no element of one lies on an element of the other: their ranges are apart, or they repeat with a common period
+// Their ranges are apart, or they repeat with a common period
 // (rows of one projection, halves of one buffer) and occupy different parts of it.
-static bool heads_apart(const si_heads* a, const si_heads* b) {
+bool heads_apart(const si_heads* a, const si_heads* b) {
   if (heads_empty(a) || heads_empty(b)) return true;
   const int64_t ea = heads_esize(a), eb = heads_esize(b);
   if (!ranges_overlap(a->ptr, (size_t)(heads_extent(a) * ea), b->ptr, (size_t)(heads_extent(b) * eb))) return true;
@@ -93,7 +90,7 @@ static bool heads_apart(const si_heads* a, const si_heads* b) {
   return false;
 }
 
-static bool heads_overlap_range(const si_heads* t, const void* p, size_t bytes) {
+bool heads_overlap_range(const si_heads* t, const void* p, size_t bytes) {
   return !heads_empty(t) && bytes && ranges_overlap(t->ptr, (size_t)heads_extent(t) * (size_t)heads_esize(t), p, bytes);
 }
 
@@ -191,8 +188,6 @@ si_status enqueue_rope(const si_heads* q, const si_heads* k, const si_rope* r, i
 }
 
 // ----------------------------------------------------------------------------- runs and blocks
-
-constexpr int64_t kGridMost = 1 << 20;  // workgroups of a launch; kernels walk longer lists
 
 // Sizes that the selection and the attention share.
 si_status plan_blocks(const si_heads* q, const si_heads* k, int64_t q_block, int64_t k_block, BlocksPlan* p) {

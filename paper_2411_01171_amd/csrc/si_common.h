@@ -13,6 +13,11 @@ struct bf16 {
   unsigned short v;
 };
 
+struct HeadsView {  // element (b, n, h, c) at p + b*sb + n*sn + h*sh + c
+  void* p;
+  int64_t sb, sn, sh;
+};
+
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
