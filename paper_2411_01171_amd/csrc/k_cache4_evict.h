@@ -1,5 +1,11 @@
-// Eviction from a cache in 4 bits: which tokens stay, by the weight they received, and their move to another cache.
+// Eviction from a cache in 4 bits: which slots stay, by the weight they received, and their move to another cache.
+//
+// Weights are ordered as unsigned integers.  The least weight that stays is found digit by digit from the top, by counting in
+// LDS; then how many slots of every 1024 are above it and how many equal it.  From these counts the last kernel's workgroups, one
+// for every 1024 slots, know where what they keep begins.  All counts are whole numbers: no order changes them.
 #pragma once
+#include <type_traits>
+
 #include "k_cache4.h"
 
 namespace si {
@@ -10,12 +16,19 @@ struct EvictArgs {
   float* weight_out;
   int *kept, *out_len;
   const int* k_len;  // or NULL
-  int keep, first, last, code_bytes, scale_bytes;
+  int keep, first, last;
   unsigned lists;    // B * heads
-  unsigned chunks, work;  // of the move
+  unsigned chunks;   // of 1024 slots of a list
+  unsigned work;     // lists * chunks
+  int2* counts;      // [lists][chunks]: slots that stay without question, slots that equal the threshold
+  uint2* least;      // [lists]: the threshold, and how many of those that equal it stay
+  unsigned parts;    // workgroups of a list of more than 16384 slots
+  int64_t part_slots;
+  int* hist[2];      // [lists][parts][2048], of one step and the next
+  struct EvictSearch* search;  // [2][lists]
 };
 
-// Order of a weight as an unsigned integer: NaN as -infinity, -0 as +0.  At least 0x007fffff.
+// Order of a weight as an unsigned integer: NaN as -infinity, -0 as +0.  At least 0x007fffff, at most 0xff800000.
 __device__ __forceinline__ unsigned weight_key(float x) {
   if (!(x == x)) x = -INFINITY;
   const unsigned b = __float_as_uint(x + 0.f);
@@ -23,104 +36,341 @@ __device__ __forceinline__ unsigned weight_key(float x) {
 }
 
 constexpr int kEvictThreads = 1024;
+constexpr int kEvictPer = 16;                                // weights of a thread at a time
+constexpr int kEvictBatch = kEvictThreads * kEvictPer;
+constexpr int kEvictChunk = kEvictThreads;                   // slots that are counted together; the second kernel's piece
+constexpr int kEvictBins = 2048;                             // digits of 11, 11 and 10 bits
 
-// One workgroup per list: the threshold's 32 bits, eight at a time by counting, then the tokens that stay in their order.
-__global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a) {
-  __shared__ int hist[256], above[kEvictThreads / kWave], equal[kEvictThreads / kWave];
-  __shared__ unsigned found_digit;
-  __shared__ int found_left;
+// Whether the weight of a slot of a list of n > keep counts; of those whose weight does not, all stay.
+__device__ __forceinline__ bool evict_open(const EvictArgs& a, int n, int64_t i) { return i >= a.first && i < n - a.last; }
+
+__host__ __device__ constexpr int evict_shift(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+
+// The threshold as far as it is known: its upper digits, and how many weights of those that share them stay.
+struct EvictSearch {
+  unsigned least;
+  int left;
+};
+
+// What a workgroup of kEvictThreads shares.
+struct EvictShared {
+  int hist[kEvictBins];
+  int wave_total[kEvictThreads / kWave];
+  int count[kEvictPer][2];
+  EvictSearch found;
+};
+
+// Inclusive sums over the lanes of a wavefront.
+__device__ __forceinline__ int wave_upto(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);  // row_shr 1, 2, 4, 8: within 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast 15: lane 15 to row 1, 47 to row 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast 31: to rows 2 and 3
+  return v;
+}
+
+// The next digit, from the thread's two counts: those of digits 2047 - 2 t and 2046 - 2 t.  It is the one with which the count from the top
+// reaches what is left.
+__device__ __forceinline__ EvictSearch evict_digit(EvictShared& sh, EvictSearch at, int digit, int h0, int h1) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  for (unsigned list = blockIdx.x; list < a.lists; list += gridDim.x) {
-    const int b = (int)(list / (unsigned)a.from.heads);
-    const int n = a.k_len ? min(max(a.k_len[b], 0), a.from.cap) : a.from.cap;
-    const float* w = a.weight + (int64_t)list * a.from.cap;
-    int* kept = a.kept + (int64_t)list * a.keep;
-    float* wo = a.weight_out + (int64_t)list * a.to.cap;
-    if (tid == 0 && list % (unsigned)a.from.heads == 0) a.out_len[b] = min(n, a.keep);
-    if (n <= a.keep) {
-      for (int i = tid; i < n; i += kEvictThreads) {
-        kept[i] = i;
-        wo[i] = w[i];
-      }
-      continue;
-    }
-    const int lo = a.first, hi = n - a.last;  // candidates
-    int left = a.keep - a.first - a.last;     // of them that stay
-    unsigned prefix = 0u;
-    for (int shift = 24; shift >= 0 && left > 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kEvictThreads) hist[i] = 0;
-      __syncthreads();
-      for (int64_t i = (int64_t)lo + tid; i < hi; i += kEvictThreads) {
-        const unsigned key = weight_key(w[i]);
-        if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[(key >> shift) & 255u], 1);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        int d = 255, more = left;
-        for (; d > 0 && hist[d] < more; --d) more -= hist[d];
-        found_digit = (unsigned)d;
-        found_left = more;
-      }
-      __syncthreads();
-      prefix |= found_digit << shift;
-      left = found_left;
-    }
-    // what is above `prefix` stays, and the first `left` that equal it; none at all if nothing was to be found
-    const bool none = a.keep - a.first - a.last == 0;
-    int done = 0, eq = 0;
-    for (int64_t i0 = 0; i0 < n; i0 += kEvictThreads) {
-      const int64_t i = i0 + tid;
-      const float x = i < n ? w[i] : 0.f;
-      const unsigned key = weight_key(x);
-      const bool open = i >= lo && i < hi && !none;
-      const bool sure = i < n && (i < lo || i >= hi || (open && key > prefix)), tie = open && key == prefix;
-      const unsigned long long ties = __builtin_amdgcn_ballot_w64(tie), below = lane ? ~0ull >> (64 - lane) : 0ull;
-      if (lane == 0) equal[wave] = __popcll(ties);
-      __syncthreads();
-      int ties_before = eq + __popcll(ties & below);
-      for (int v = 0; v < kEvictThreads / kWave; ++v) {
-        if (v < wave) ties_before += equal[v];
-        eq += equal[v];
-      }
-      const bool stay = sure || (tie && ties_before < left);
-      const unsigned long long stays = __builtin_amdgcn_ballot_w64(stay);
-      if (lane == 0) above[wave] = __popcll(stays);
-      __syncthreads();
-      int at = done + __popcll(stays & below);
-      for (int v = 0; v < kEvictThreads / kWave; ++v) {
-        if (v < wave) at += above[v];
-        done += above[v];
-      }
-      if (stay) {
-        kept[at] = (int)i;
-        wo[at] = x;
-      }
-    }
-    __syncthreads();
+  int upto = wave_upto(h0 + h1);
+  if (lane == kWave - 1) sh.wave_total[wave] = upto;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kEvictThreads / kWave; ++v) upto += v < wave ? sh.wave_total[v] : 0;
+  const int before = upto - h0 - h1;
+  if (before < at.left && at.left <= upto) {  // one thread's
+    const bool second = before + h0 < at.left;
+    sh.found.least = at.least | (unsigned)(second ? 2046 - 2 * tid : 2047 - 2 * tid) << evict_shift(digit);
+    sh.found.left = at.left - before - (second ? h0 : 0);
+  }
+  __syncthreads();
+  return sh.found;
+}
+
+// A batch: slots base + 1024 j + t, which of them there are and which weights count, from its first slot on.
+struct EvictBatch {
+  int there, lo, hi;
+  __device__ __forceinline__ EvictBatch(const EvictArgs& a, int n, int64_t base, int64_t end) {
+    auto from_base = [&](int64_t i) { return (int)min(max(i - base, (int64_t)0), (int64_t)kEvictBatch); };
+    there = from_base(end);
+    lo = min(from_base(a.first), there);
+    hi = max(lo, min(from_base((int64_t)n - a.last), there));
+  }
+  __device__ __forceinline__ bool any(int j) const { return j * kEvictThreads < there; }  // of a thread's slot j, over the workgroup
+  __device__ __forceinline__ bool open(int i) const { return i >= lo && i < hi; }
+};
+
+// The weights in their order; 0: no weight that counts.
+__device__ __forceinline__ void evict_load(const EvictArgs& a, const float* w, const EvictBatch& of, int64_t base, unsigned (&key)[kEvictPer]) {
+  float x[kEvictPer];
+#pragma unroll
+  for (int j = 0; j < kEvictPer; ++j) {
+    const int i = j * kEvictThreads + (int)threadIdx.x;
+    x[j] = 0.f;
+    if (of.any(j) && i < of.there) x[j] = w[base + i];
+  }
+#pragma unroll
+  for (int j = 0; j < kEvictPer; ++j) key[j] = of.any(j) && of.open(j * kEvictThreads + (int)threadIdx.x) ? weight_key(x[j]) : 0u;
+}
+
+// Adds the weights that share the digits found so far to sh.hist, which is zero.
+__device__ __forceinline__ void evict_count(EvictShared& sh, const unsigned (&key)[kEvictPer], const EvictBatch& of, EvictSearch at, int digit) {
+#pragma unroll
+  for (int j = 0; j < kEvictPer; ++j) {
+    if (!of.any(j)) continue;
+    const bool counts = key[j] != 0u && (digit == 0 || (key[j] ^ at.least) >> evict_shift(digit - 1) == 0u);
+    if (counts) atomicAdd(&sh.hist[(key[j] >> evict_shift(digit)) & (digit == 2 ? 1023u : 2047u)], 1);
   }
 }
 
-// The tokens that stay, 16 bytes of codes to a thread.
-__global__ __launch_bounds__(256) void cache4_move_kernel(EvictArgs a) {
-  const int pieces = a.code_bytes / 16, tokens = 256 / (2 * pieces);
-  const int t = threadIdx.x / (2 * pieces), x = threadIdx.x % (2 * pieces) / pieces, piece = threadIdx.x % pieces;
-  const uint8_t *fc = x ? a.from.vc : a.from.kc, *fs = x ? a.from.vs : a.from.ks;
-  uint8_t *tc = x ? a.to.vc : a.to.kc, *ts = x ? a.to.vs : a.to.ks;
-  for (unsigned work = blockIdx.x; work < a.work; work += gridDim.x) {
-    const unsigned list = work / a.chunks;
-    const int b = (int)(list / (unsigned)a.from.heads);
-    const int n = min(a.k_len ? min(max(a.k_len[b], 0), a.from.cap) : a.from.cap, a.keep);
+// For every 1024 slots from `base` on, those that stay without question and those that equal the threshold.
+__device__ __forceinline__ void evict_counts(const EvictArgs& a, EvictShared& sh, const unsigned (&key)[kEvictPer], const EvictBatch& of, unsigned least, unsigned list,
+                                             int64_t base) {
+  const int tid = threadIdx.x;
+  if (tid < 2 * kEvictPer) sh.count[tid / 2][tid % 2] = 0;
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t slot = ((int64_t)(work % a.chunks) * 4 + i) * tokens + t;
-      if (t >= tokens || slot >= n) continue;
-      const int64_t src = (int64_t)list * a.from.cap + a.kept[(int64_t)list * a.keep + slot], dst = (int64_t)list * a.to.cap + slot;
-      *reinterpret_cast<u32x4_t*>(tc + dst * a.code_bytes + piece * 16) = *reinterpret_cast<const u32x4_t*>(fc + src * a.code_bytes + piece * 16);
-      if (piece == 0) {
-        if (a.scale_bytes == 4) *reinterpret_cast<unsigned*>(ts + dst * 4) = *reinterpret_cast<const unsigned*>(fs + src * 4);
-        else if (a.scale_bytes == 2) *reinterpret_cast<unsigned short*>(ts + dst * 2) = *reinterpret_cast<const unsigned short*>(fs + src * 2);
-        else ts[dst] = fs[src];
+  for (int j = 0; j < kEvictPer; ++j) {
+    if (!of.any(j)) continue;
+    const int i = j * kEvictThreads + tid;
+    const int above = (int)__popcll(__builtin_amdgcn_ballot_w64(of.open(i) ? key[j] > least : i < of.there));  // of slots that are not open all stay
+    const int equal = (int)__popcll(__builtin_amdgcn_ballot_w64(key[j] == least && key[j] != 0u));
+    if (tid % kWave == 0) {
+      if (above) atomicAdd(&sh.count[j][0], above);
+      if (equal) atomicAdd(&sh.count[j][1], equal);
+    }
+  }
+  __syncthreads();
+  if (tid < kEvictPer && of.any(tid)) a.counts[(int64_t)list * a.chunks + (unsigned)(base / kEvictChunk) + tid] = make_int2(sh.count[tid][0], sh.count[tid][1]);
+  __syncthreads();
+}
+
+__device__ __forceinline__ int evict_length(const EvictArgs& a, unsigned list) {
+  const int b = (int)(list / (unsigned)a.from.heads);
+  return a.k_len ? min(max(a.k_len[b], 0), a.from.cap) : a.from.cap;
+}
+__device__ __forceinline__ void evict_put_length(const EvictArgs& a, unsigned list, int n) {
+  if (threadIdx.x == 0 && list % (unsigned)a.from.heads == 0) a.out_len[list / (unsigned)a.from.heads] = min(n, a.keep);
+}
+// Where a search begins.  Nothing that counts stays: no weight is above the highest number.
+__device__ __forceinline__ EvictSearch evict_begin(const EvictArgs& a) {
+  const int left = a.keep - a.first - a.last;
+  return EvictSearch{left > 0 ? 0u : ~0u, left};
+}
+
+// Lists of up to 16384 slots, one workgroup each; the weights stay in registers.  A chain of latencies: 4096 slots.
+__global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a) {
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x;
+  for (unsigned list = blockIdx.x; list < a.lists; list += gridDim.x) {
+    const int n = evict_length(a, list);
+    evict_put_length(a, list, n);
+    if (n <= a.keep) {  // all: above a threshold of zero
+      if (tid == 0) a.least[list] = make_uint2(0u, 0u);
+      continue;
+    }
+    unsigned key[kEvictPer];
+    const EvictBatch of(a, n, 0, n);
+    evict_load(a, a.weight + (int64_t)list * a.from.cap, of, 0, key);
+    sh.hist[tid] = 0;
+    sh.hist[tid + kEvictThreads] = 0;
+    EvictSearch at = evict_begin(a);
+    if (at.left > 0)
+#pragma unroll
+      for (int digit = 0; digit < 3; ++digit) {
+        __syncthreads();
+        evict_count(sh, key, of, at, digit);
+        __syncthreads();
+        const int h0 = sh.hist[2047 - 2 * tid], h1 = sh.hist[2046 - 2 * tid];
+        sh.hist[2047 - 2 * tid] = sh.hist[2046 - 2 * tid] = 0;
+        at = evict_digit(sh, at, digit, h0, h1);
       }
+    if (tid == 0) a.least[list] = make_uint2(at.least, (unsigned)at.left);
+    evict_counts(a, sh, key, of, at.least, list, 0);
+  }
+}
+
+// Longer lists, a workgroup for each of a.parts pieces of one.  STEP 0, 1, 2: the counts of that digit of a piece's weights; 1, 2, 3: before
+// that, the digit before it from all pieces' counts; 3: the counts of every 1024 slots.  A launch per step: 115200 slots of 32 lists in one
+// workgroup each took 98 us.
+template <int STEP>
+__global__ __launch_bounds__(kEvictThreads) void cache4_search_kernel(EvictArgs a) {
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x;
+  for (unsigned work = blockIdx.x; work < a.lists * a.parts; work += gridDim.x) {
+    const unsigned list = work / a.parts, part = work % a.parts;
+    const int n = evict_length(a, list);
+    if (STEP == 0 && part == 0) evict_put_length(a, list, n);
+    if (n <= a.keep) {
+      if (STEP == 3 && part == 0 && tid == 0) a.least[list] = make_uint2(0u, 0u);
+      continue;
+    }
+    const int64_t begin = (int64_t)part * a.part_slots, end = min((int64_t)n, begin + a.part_slots);
+    unsigned key[kEvictPer];
+    const float* w = a.weight + (int64_t)list * a.from.cap;
+    EvictBatch of(a, n, begin, end);
+    evict_load(a, w, of, begin, key);  // on its way while the digit is found
+    __syncthreads();                       // the piece before has been counted
+    if (STEP < 3) {
+      sh.hist[tid] = 0;
+      sh.hist[tid + kEvictThreads] = 0;
+    }
+    EvictSearch at = evict_begin(a);
+    if (STEP > 0 && at.left > 0) {
+      if (STEP > 1) at = a.search[(STEP % 2) * a.lists + list];
+      const int2* counts = reinterpret_cast<const int2*>(a.hist[(STEP + 1) % 2] + (int64_t)list * a.parts * kEvictBins) + (kEvictThreads - 1 - tid);
+      int h0 = 0, h1 = 0;
+      for (unsigned p = 0; p < a.parts; ++p) {
+        const int2 v = counts[(int64_t)p * (kEvictBins / 2)];
+        h1 += v.x;
+        h0 += v.y;
+      }
+      at = evict_digit(sh, at, STEP - 1, h0, h1);
+      if (part == 0 && tid == 0) a.search[((STEP + 1) % 2) * a.lists + list] = at;
+    }
+    if (STEP == 3 && part == 0 && tid == 0) a.least[list] = make_uint2(at.least, (unsigned)at.left);
+    __syncthreads();
+    for (int64_t base = begin; base < end; base += kEvictBatch) {
+      if (base != begin) {
+        of = EvictBatch(a, n, base, end);
+        evict_load(a, w, of, base, key);
+      }
+      if constexpr (STEP < 3) {
+        if (at.left > 0) evict_count(sh, key, of, at, STEP);
+      } else {
+        evict_counts(a, sh, key, of, at.least, list, base);
+      }
+    }
+    if constexpr (STEP < 3) {
+      __syncthreads();
+      int2* out = reinterpret_cast<int2*>(a.hist[STEP % 2] + ((int64_t)list * a.parts + part) * kEvictBins);
+      out[tid] = make_int2(sh.hist[2 * tid], sh.hist[2 * tid + 1]);
+    }
+  }
+}
+
+constexpr int kMoveThreads = 256;
+
+// The slots of a chunk that stay: listed in LDS in their order, then moved, 16 bytes of codes to a thread.
+template <int G>
+__global__ __launch_bounds__(kMoveThreads) void cache4_move_kernel(EvictArgs a) {
+  constexpr int WAVES = kMoveThreads / kWave, PER = kEvictChunk / kMoveThreads, S = cache4_scale_bytes(G);
+  __shared__ int stays[kEvictChunk];
+  __shared__ int sums[3][WAVES];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const unsigned long long below = lane ? ~0ull >> (64 - lane) : 0ull;
+  for (unsigned work = blockIdx.x; work < a.work; work += gridDim.x) {
+    const unsigned list = work / a.chunks, chunk = work % a.chunks;
+    const int n = evict_length(a, list);
+    const int64_t slot0 = (int64_t)chunk * kEvictChunk;
+    if (slot0 >= n) continue;
+    const float* w = a.weight + (int64_t)list * a.from.cap;
+    const uint2 least = a.least[list];
+    float x[PER];
+    unsigned long long sure[PER], tie[PER];
+    int my_ties = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int64_t i = slot0 + (wave * PER + j) * kWave + lane;
+      x[j] = i < n ? w[i] : 0.f;
+    }
+    int above = 0, equal = 0;  // of the chunks before
+    if (n > a.keep)
+      for (unsigned c = tid; c < chunk; c += kMoveThreads) {
+        const int2 v = a.counts[(int64_t)list * a.chunks + c];
+        above += v.x;
+        equal += v.y;
+      }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int64_t i = slot0 + (wave * PER + j) * kWave + lane;
+      const unsigned key = weight_key(x[j]);
+      const bool open = n > a.keep && evict_open(a, n, i);
+      sure[j] = __builtin_amdgcn_ballot_w64(open ? key > least.x : i < n);  // of slots that are not open all stay
+      tie[j] = __builtin_amdgcn_ballot_w64(open && key == least.x);
+      my_ties += __popcll(tie[j]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      above += __shfl_xor(above, o, kWave);
+      equal += __shfl_xor(equal, o, kWave);
+    }
+    __syncthreads();  // the piece before has been moved
+    if (lane == 0) {
+      sums[0][wave] = above;
+      sums[1][wave] = equal;
+      sums[2][wave] = my_ties;
+    }
+    __syncthreads();
+    int base = 0, ties = 0, left;  // slots that stayed and ties before this chunk
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) {
+      base += sums[0][v];
+      ties += sums[1][v];
+    }
+    left = (int)least.y - ties;  // ties of this chunk and later ones that stay; below zero where they ended before
+    base = n > a.keep ? base + min(ties, (int)least.y) : (int)slot0;
+    int ties_before = 0, at = 0, in_chunk = 0;
+    for (int v = 0; v < wave; ++v) ties_before += sums[2][v];
+    unsigned long long stay[PER];
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const bool in = (tie[j] >> lane & 1ull) && ties_before + (int)__popcll(tie[j] & below) < left;
+      stay[j] = sure[j] | __builtin_amdgcn_ballot_w64(in);
+      ties_before += __popcll(tie[j]);
+      mine += __popcll(stay[j]);
+    }
+    __syncthreads();
+    if (lane == 0) sums[0][wave] = mine;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) {
+      if (v < wave) at += sums[0][v];
+      in_chunk += sums[0][v];
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if (stay[j] >> lane & 1ull) {
+        const int k = at + (int)__popcll(stay[j] & below), i = (int)(slot0 + (wave * PER + j) * kWave + lane);
+        stays[k] = i;
+        a.kept[(int64_t)list * a.keep + base + k] = i;
+        a.weight_out[(int64_t)list * a.to.cap + base + k] = x[j];
+      }
+      at += __popcll(stay[j]);
+    }
+    __syncthreads();
+    const int64_t src0 = (int64_t)list * a.from.cap, dst0 = (int64_t)list * a.to.cap + base;
+    const int pieces = in_chunk * G;
+    for (int u0 = 0; u0 < pieces; u0 += 2 * kMoveThreads) {
+      u32x4_t kv[2][2];
+      int64_t to[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int u = u0 + i * kMoveThreads + tid, t = u / G;
+        to[i] = -1;
+        if (u >= pieces) continue;
+        const int64_t src = (src0 + stays[t]) * (16 * G) + (u % G) * 16;
+        to[i] = (dst0 + t) * (16 * G) + (u % G) * 16;
+        kv[i][0] = *reinterpret_cast<const u32x4_t*>(a.from.kc + src);
+        kv[i][1] = *reinterpret_cast<const u32x4_t*>(a.from.vc + src);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (to[i] >= 0) {
+          *reinterpret_cast<u32x4_t*>(a.to.kc + to[i]) = kv[i][0];
+          *reinterpret_cast<u32x4_t*>(a.to.vc + to[i]) = kv[i][1];
+        }
+    }
+    using Word = std::conditional_t<S == 4, unsigned, std::conditional_t<S == 2, unsigned short, uint8_t>>;
+    for (int t = tid; t < in_chunk; t += kMoveThreads) {
+      const int64_t src = (src0 + stays[t]) * S, dst = (dst0 + t) * S;
+      const Word k = *reinterpret_cast<const Word*>(a.from.ks + src), v = *reinterpret_cast<const Word*>(a.from.vs + src);
+      *reinterpret_cast<Word*>(a.to.ks + dst) = k;
+      *reinterpret_cast<Word*>(a.to.vs + dst) = v;
     }
   }
 }

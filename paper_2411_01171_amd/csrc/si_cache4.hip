@@ -203,10 +203,28 @@ static si_status launch_cache_attn(const CacheAttnArgs& a, const CacheWeightArgs
 
 // ----------------------------------------------------------------------------- eviction
 
-static si_status check_evict(const si_cache4* c, int64_t keep) {
+struct EvictPlan {
+  int64_t lists, chunks, parts, part_slots;
+  size_t count_bytes, least_bytes, search_bytes, hist_bytes, bytes;
+};
+
+static si_status plan_evict(const si_cache4* c, int64_t keep, EvictPlan* p) {
   const si_status s = check_cache(c, false);
   if (s != SI_OK) return s;
-  return keep < 1 || keep > kMostTokens ? SI_ERR_SHAPE : SI_OK;
+  if (keep < 1 || keep > kMostTokens) return SI_ERR_SHAPE;
+  p->lists = c->B * c->heads;
+  p->chunks = (c->capacity + kEvictChunk - 1) / kEvictChunk;
+  if ((double)p->lists * (double)p->chunks >= 4294967296.0 - kGridMost || (double)p->lists * (double)keep >= 1099511627776.0) return SI_ERR_SHAPE;
+  p->count_bytes = align_up((size_t)(p->lists * p->chunks) * sizeof(int2), 256);
+  p->least_bytes = align_up((size_t)p->lists * sizeof(uint2), 256);
+  // Lists that do not fit a workgroup's registers are cut into up to 16 parts, as long as there are few lists: every part adds up all parts' counts.
+  p->parts = c->capacity <= kEvictBatch ? 0 : std::min<int64_t>(std::min<int64_t>(16, (c->capacity + kEvictBatch - 1) / kEvictBatch), std::max<int64_t>(1, 1024 / p->lists));
+  const int64_t batches = (c->capacity + kEvictBatch - 1) / kEvictBatch;
+  p->part_slots = p->parts ? (batches + p->parts - 1) / p->parts * kEvictBatch : 0;
+  p->search_bytes = p->parts ? align_up((size_t)p->lists * 2 * sizeof(EvictSearch), 256) : 0;
+  p->hist_bytes = (size_t)(p->lists * p->parts) * kEvictBins * sizeof(int);
+  p->bytes = p->count_bytes + p->least_bytes + p->search_bytes + 2 * p->hist_bytes + 256;
+  return SI_OK;
 }
 
 }  // namespace si
@@ -293,30 +311,29 @@ si_status si_cache4_attn_forward(const si_heads* q, const si_cache4* cache, floa
 }
 
 size_t si_cache4_evict_workspace_bytes(const si_cache4* cache, int64_t keep) {
-  return si::check_evict(cache, keep) == SI_OK ? 256 : 0;
+  si::EvictPlan p;
+  return si::plan_evict(cache, keep, &p) == SI_OK ? p.bytes : 0;
 }
 
 si_status si_cache4_evict(const si_cache4* cache, const int32_t* k_len, const float* weight, int64_t keep, int64_t first, int64_t last,
                           const si_cache4* out, float* weight_out, int32_t* kept, int32_t* out_len, void* workspace,
                           size_t workspace_bytes, void* stream) {
-  si_status s = si::check_evict(cache, keep);
+  si::EvictPlan p;
+  si_status s = si::plan_evict(cache, keep, &p);
   if (s == SI_OK) s = si::check_cache(out, true);
   if (s != SI_OK) return s;
   if (out->B != cache->B || out->heads != cache->heads || out->dim_head != cache->dim_head || out->capacity < std::min(keep, cache->capacity)) return SI_ERR_SHAPE;
   if (first < 0 || last < 0 || first > keep || last > keep - first) return SI_ERR_ARG;
   if (!out_len || !workspace || (cache->capacity > 0 && (!weight || !weight_out || !kept))) return SI_ERR_NULL;
-  for (const void* p : {static_cast<const void*>(k_len), static_cast<const void*>(weight), static_cast<const void*>(weight_out), static_cast<const void*>(kept),
+  for (const void* q : {static_cast<const void*>(k_len), static_cast<const void*>(weight), static_cast<const void*>(weight_out), static_cast<const void*>(kept),
                         static_cast<const void*>(out_len)})
-    if (!si::aligned4(p)) return SI_ERR_ALIGN;
+    if (!si::aligned4(q)) return SI_ERR_ALIGN;
   if (reinterpret_cast<uintptr_t>(workspace) & 255u) return SI_ERR_ALIGN;
-  const size_t need = 256;
-  if (workspace_bytes < need) return SI_ERR_WORKSPACE;
-  const size_t lists = (size_t)(cache->B * cache->heads);
-  if ((double)lists * (double)keep >= 1099511627776.0) return SI_ERR_SHAPE;
+  if (workspace_bytes < p.bytes) return SI_ERR_WORKSPACE;
   const si::CacheSpans from(cache), to(out);
   const si::Span in[] = {from.s[0], from.s[1], from.s[2], from.s[3], {weight, si::cache_rows(cache) * 4}, {k_len, (size_t)cache->B * 4}};
-  const si::Span written[] = {to.s[0], to.s[1], to.s[2], to.s[3], {weight_out, si::cache_rows(out) * 4}, {kept, lists * (size_t)keep * 4},
-                              {out_len, (size_t)cache->B * 4}, {workspace, need}};
+  const si::Span written[] = {to.s[0], to.s[1], to.s[2], to.s[3], {weight_out, si::cache_rows(out) * 4}, {kept, (size_t)(p.lists * keep) * 4},
+                              {out_len, (size_t)cache->B * 4}, {workspace, p.bytes}};
   for (size_t i = 0; i < std::size(written); ++i) {
     for (const si::Span& x : in)
       if (si::meet(x, written[i])) return SI_ERR_ARG;
@@ -329,24 +346,31 @@ si_status si_cache4_evict(const si_cache4* cache, const int32_t* k_len, const fl
   a.weight = weight; a.weight_out = weight_out;
   a.kept = kept; a.out_len = out_len; a.k_len = k_len;
   a.keep = (int)keep; a.first = (int)first; a.last = (int)last;
-  a.code_bytes = (int)si::code_bytes(cache); a.scale_bytes = (int)si::scale_bytes(cache);
-  a.lists = (unsigned)lists;
-  const int64_t tokens = 256 / (2 * a.code_bytes / 16) * 4, most = std::min(keep, cache->capacity);
-  const double work = (double)lists * (double)((most + tokens - 1) / tokens);
-  if (work >= 4294967296.0 - si::kGridMost) return SI_ERR_SHAPE;
-  a.chunks = (unsigned)((most + tokens - 1) / tokens);
-  a.work = (unsigned)work;
+  a.lists = (unsigned)p.lists;
+  a.chunks = (unsigned)p.chunks;
+  a.work = (unsigned)(p.lists * p.chunks);
+  a.counts = static_cast<int2*>(workspace);
+  char* at = static_cast<char*>(workspace) + p.count_bytes;
+  a.least = reinterpret_cast<uint2*>(at);
+  a.parts = (unsigned)p.parts;
+  a.part_slots = p.part_slots;
+  a.search = reinterpret_cast<si::EvictSearch*>(at += p.least_bytes);
+  a.hist[0] = reinterpret_cast<int*>(at += p.search_bytes);
+  a.hist[1] = reinterpret_cast<int*>(at + p.hist_bytes);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  {
-    si::StageScope scope("cache4_pick", st);
-    si::cache4_pick_kernel<<<(unsigned)std::min<int64_t>((int64_t)lists, si::kGridMost), si::kEvictThreads, 0, st>>>(a);
-    SI_CHECK_LAUNCH();
+  si::StageScope scope("cache4_evict", st);
+  if (p.parts == 0) {
+    si::cache4_pick_kernel<<<(unsigned)std::min<int64_t>(p.lists, si::kGridMost), si::kEvictThreads, 0, st>>>(a);
+  } else {
+    const unsigned grid = (unsigned)std::min<int64_t>(p.lists * p.parts, si::kGridMost);
+    si::cache4_search_kernel<0><<<grid, si::kEvictThreads, 0, st>>>(a);
+    si::cache4_search_kernel<1><<<grid, si::kEvictThreads, 0, st>>>(a);
+    si::cache4_search_kernel<2><<<grid, si::kEvictThreads, 0, st>>>(a);
+    si::cache4_search_kernel<3><<<grid, si::kEvictThreads, 0, st>>>(a);
   }
-  if (a.work > 0) {
-    si::StageScope scope("cache4_move", st);
-    si::cache4_move_kernel<<<(unsigned)std::min<int64_t>(a.work, si::kGridMost), 256, 0, st>>>(a);
-    SI_CHECK_LAUNCH();
-  }
+  if (a.work > 0)
+    si::by_groups(cache, [&](auto g) { si::cache4_move_kernel<g.value><<<(unsigned)std::min<int64_t>(a.work, si::kGridMost), si::kMoveThreads, 0, st>>>(a); });
+  SI_CHECK_LAUNCH();
   return SI_OK;
 }
 
