@@ -112,11 +112,11 @@ struct KeyCodes {
   static constexpr int S = cache4_scale_bytes(G);
   unsigned w[2][G];
   unsigned s[2];
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int key0, int end, int r, int g) {
+  // The key's row begins at codes + at[t] * 16 G, with an offset that lanes have of their own from a base that they share.
+  __device__ __forceinline__ void load_rows(const uint8_t* codes, const uint8_t* scales, const unsigned (&at)[2], int g) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int64_t key = min(key0 + 16 * t + r, end - 1);
-      const unsigned* p = reinterpret_cast<const unsigned*>(codes + key * (16 * G) + g * (4 * G));
+      const unsigned* p = reinterpret_cast<const unsigned*>(codes + (at[t] * (16u * G) + g * (4u * G)));
       if constexpr (G == 4) {
         const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p);
 #pragma unroll
@@ -128,10 +128,16 @@ struct KeyCodes {
 #pragma unroll
         for (int i = 0; i < G; ++i) w[t][i] = p[i];
       }
-      if constexpr (S == 4) s[t] = *reinterpret_cast<const unsigned*>(scales + key * 4);
-      else if constexpr (S == 2) s[t] = *reinterpret_cast<const unsigned short*>(scales + key * 2);
-      else s[t] = scales[key];
+      if constexpr (S == 4) s[t] = *reinterpret_cast<const unsigned*>(scales + at[t] * 4u);
+      else if constexpr (S == 2) s[t] = *reinterpret_cast<const unsigned short*>(scales + at[t] * 2u);
+      else s[t] = scales[at[t]];
     }
+  }
+  // Keys key0 .. key0 + 31 of a head, those at and behind `end` as the last one before it.
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int key0, int end, int r, int g) {
+    const int last = end - 1 - key0;
+    const unsigned at[2] = {(unsigned)min(r, last), (unsigned)min(16 + r, last)};
+    load_rows(codes + (int64_t)key0 * (16 * G), scales + (int64_t)key0 * S, at, g);
   }
   // Channels 8 G g + 8 i .. + 7 of key tile t.  Groups of 32 channels are 4 / G lanes' or, with three of them, end inside a lane's.
   __device__ __forceinline__ u32x4_t operand(int t, int i, int g) const {
@@ -143,7 +149,7 @@ struct KeyCodes {
 // Rows of up to 32 of a tile: four wavefronts that each take every fourth step of 32 keys.
 // T: of queries and outputs.  G: groups of 32 channels of a head.  NT: columns of rows, 16 each.
 template <typename T, int G, int NT>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? 4 : 2) void cache4_attn_few_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 2) void cache4_attn_few_kernel(CacheAttnArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
   constexpr int ROW = G == 1 ? 64 : G == 2 ? 128 : 256;  // bytes of a key's values in LDS
   constexpr int UNITS = 32 * G, PER = (UNITS + 63) / 64;  // groups of a step's values, and a lane's share
@@ -153,7 +159,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? 4 : 2) void cache4
   __shared__ __align__(1024) u32x4_t lds[BYTES / 16];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 16, g = lane / 16;
-  auto swizzle = [](int key) { return ROW == 64 ? (key >> 2) & 3 : ROW == 128 ? (key >> 1) & 7 : (key & 3) << 2 | ((key >> 2) & 3); };
+  // A key's values lie in 16-byte pieces; piece p in slot p ^ swizzle(key).  LDS has 64 banks of 4 bytes: the transposing reads of 32 lanes take
+  // two pieces of eight keys, and 16 lanes write one of every four pieces of the keys that key_of gives them; both fall on different banks.
+  auto swizzle = [](int key) { return ROW == 64 ? ((key >> 2) & 1) << 1 | ((key >> 3) & 1) : ROW == 128 ? (key & 6) | ((key >> 3) & 1) : (key & 7) << 1 | ((key >> 3) & 1); };
+  auto key_of = [](int unit) {  // a step's values in groups of 32 channels: unit / G with some of its bits in another order
+    const int n = unit / G;
+    return G == 4 ? (n & 17) | (n & 2) << 2 | (n & 12) >> 1 : G == 2 ? (n & 19) | (n & 4) << 1 | (n & 8) >> 1 : n;
+  };
   const unsigned vals = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&lds[0]) + wave * 32 * ROW;
 
   const unsigned chunk = (a.work + 7) / 8;  // contiguous per XCD: a head's codes are fetched into one L2
@@ -199,16 +211,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? 4 : 2) void cache4
     u32x4_t vn[PER];
     unsigned vsn[PER];
     auto fetch = [&](unsigned step) {
-      const int key0 = (int)(step * 32);
+      const int key0 = (int)(step * 32), left = any - key0;
       kn.load(kc, ks, key0, any, r, g);
+      const uint8_t *codes = vc + (int64_t)key0 * (16 * G), *scales = vs + (int64_t)key0 * SB;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int unit = i * 64 + lane, key = key0 + unit / G, group = unit % G;
+        const int unit = i * 64 + lane, key = key_of(unit), group = unit % G;
         vn[i] = u32x4_t{0, 0, 0, 0};
         vsn[i] = 127u;  // what no row sees counts as zero
-        if (unit < UNITS && key < any) {
-          vn[i] = *reinterpret_cast<const u32x4_t*>(vc + ((int64_t)key * G + group) * 16);
-          vsn[i] = vs[(int64_t)key * SB + group];
+        if ((UNITS % 64 == 0 || unit < UNITS) && key < left) {
+          vn[i] = *reinterpret_cast<const u32x4_t*>(codes + (unsigned)((key * G + group) * 16));
+          vsn[i] = scales[(unsigned)(key * SB + group)];
         }
       }
     };
@@ -226,7 +239,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? 4 : 2) void cache4
       asm volatile("" ::: "memory");
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int unit = i * 64 + lane, key = unit / G, group = unit % G;
+        const int unit = i * 64 + lane, key = key_of(unit), group = unit % G;
         if (UNITS % 64 && unit >= UNITS) continue;
 #pragma unroll
         for (int p = 0; p < 4; ++p)
