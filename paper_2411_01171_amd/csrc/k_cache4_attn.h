@@ -146,6 +146,14 @@ struct KeyCodes {
   }
 };
 
+// A NaN among the values would make one of every row's weight of zero as well.  It is stored as zeros instead, and the lowest slot that has one
+// in a group is noted: rows that see it receive NaN in that group in the end.
+__device__ __forceinline__ void note_nan(int* bad_key, int group, int key, u32x4_t& codes, unsigned& scale) {
+  atomicMin(&bad_key[group], key);
+  codes = u32x4_t{0, 0, 0, 0};
+  scale = 127u;
+}
+
 // Rows of up to 32 of a tile: four wavefronts that each take every fourth step of 32 keys.
 // T: of queries and outputs.  G: groups of 32 channels of a head.  NT: columns of rows, 16 each.
 template <typename T, int G, int NT>
@@ -157,6 +165,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
   constexpr int BYTES = 4 * 32 * ROW > 2 * KEEP * 256 ? 4 * 32 * ROW : 2 * KEEP * 256;
   constexpr int SB = cache4_scale_bytes(G);
   __shared__ __align__(1024) u32x4_t lds[BYTES / 16];
+  __shared__ int bad_key[4];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 16, g = lane / 16;
   // A key's values lie in 16-byte pieces; piece p in slot p ^ swizzle(key).  LDS has 64 banks of 4 bytes: the transposing reads of 32 lanes take
@@ -175,6 +184,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
     int first_sub;
     const int first = t.token(a, t.tile * 16 * NT, first_sub);
     if (first < 0) continue;  // the tile's first row is its earliest token
+    if (threadIdx.x < 4) bad_key[threadIdx.x] = INT32_MAX;
+    __syncthreads();
     // keys that every row sees, and that any sees
     const int64_t last = min(min((int64_t)t.run * a.run_len + min((t.tile * 16 * NT + 16 * NT - 1) / a.group, a.run_len - 1), (int64_t)t.q_len - 1), (int64_t)a.Nq - 1);
     const int all = t.seen(a, first), any = t.seen(a, (int)last);
@@ -241,6 +252,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
       for (int i = 0; i < PER; ++i) {
         const int unit = i * 64 + lane, key = key_of(unit), group = unit % G;
         if (UNITS % 64 && unit >= UNITS) continue;
+        if (vsc[i] == 255u) note_nan(bad_key, group, key0 + key, v[i], vsc[i]);
 #pragma unroll
         for (int p = 0; p < 4; ++p)
           *reinterpret_cast<__attribute__((address_space(3))) u32x4_t*>((size_t)(vals + key * ROW + ((4 * group + p) ^ swizzle(key)) * 16)) =
@@ -265,8 +277,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
             for (int x = TERMS - 1; x >= 0; --x)  // the smallest part first
               sc[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8_t, q[c][i][x]), sc[u][c], 0, 0, 0);
         }
-      const bool mixed = key0 + 32 > all;
-      if (mixed) {
+      if (key0 + 32 > all) {
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
           const int lim = seen[c] - key0 - 4 * g;
@@ -334,34 +345,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
         const int row = 4 * g + r / 4, piece = 2 * i + (r % 4) / 2;
         const uint2 x = lds_read_tr(vals + row * ROW + (piece ^ swizzle(row)) * 16 + (r % 2) * 8);
         const uint2 y = lds_read_tr(vals + (16 + row) * ROW + (piece ^ swizzle(16 + row)) * 16 + (r % 2) * 8);
-        u32x4_t vf{x.x, x.y, y.x, y.y};
-        if (mixed) {
-          // A NaN among the values is one for the rows that see its key, and nothing for the others, whose weight of zero would
-          // not hide it.
-          u32x4_t bad;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const unsigned low = (vf[w] & 0x7FFFu) > 0x7F80u ? 0xFFFFu : 0u, high = (vf[w] & 0x7FFF0000u) > 0x7F800000u ? 0xFFFF0000u : 0u;
-            bad[w] = (low | high) & 0x3F803F80u;
-            vf[w] &= ~(low | high);
-          }
-          if (__builtin_amdgcn_ballot_w64((bad[0] | bad[1] | bad[2] | bad[3]) != 0u) != 0) {
-#pragma unroll
-            for (int c = 0; c < NT; ++c) {
-              const int lim = seen[c] - key0 - 4 * g;
-              u32x4_t sees;
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const int key = 16 * (w / 2) + 2 * (w % 2);
-                sees[w] = (key < lim ? 0x3F80u : 0u) | (key + 1 < lim ? 0x3F800000u : 0u);
-              }
-              const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, bad), __builtin_bit_cast(bf16x8_t, sees), f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (hit[j] > 0.f) o[i][c][j] = NAN;
-            }
-          }
-        }
+        const u32x4_t vf{x.x, x.y, y.x, y.y};
 #pragma unroll
         for (int c = 0; c < NT; ++c)
 #pragma unroll
@@ -425,11 +409,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
         for (int i = 0; i < 2 * G; ++i) {
           const int ch = 16 * i + 4 * g;
           if (ch >= a.d) continue;
+          f32x4_t y = o[i][c];
+          if (seen[c] > bad_key[i / 2]) y = f32x4_t{NAN, NAN, NAN, NAN};
           if (a.nsplit > 1) {
-            *reinterpret_cast<f32x4_t*>(a.part + (row * a.nsplit + t.part) * a.d + ch) = o[i][c];
+            *reinterpret_cast<f32x4_t*>(a.part + (row * a.nsplit + t.part) * a.d + ch) = y;
             continue;
           }
-          f32x4_t y = o[i][c];
 #pragma unroll
           for (int j = 0; j < 4; ++j) y[j] = lsum[c] == 0.f ? 0.f : y[j] * inv;
           if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst + ch) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
@@ -442,6 +427,277 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
       }
     }
     __syncthreads();  // the next tile's values overwrite what was handed over
+  }
+}
+
+// Rows by the hundred: tiles of 128 CT rows, 32 CT to each of four wavefronts, that share stages of 64 keys.  A stage's codes are
+// fetched into registers one stage ahead, a quarter of a key's and of a value's row to a thread, and become bf16 in LDS while
+// the stage before is multiplied.
+// W: the sums of the unrounded weights are wanted too.
+template <int G, int CT, bool W>
+__global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_many_kernel(CacheAttnArgs a) {
+  using Geo = SparseGeo<bf16, 2 * G, 4>;  // rows of LDS and their swizzle
+  constexpr int ROW = Geo::ROW, HALF = 64 * ROW, KS = 2 * G, SB = cache4_scale_bytes(G);
+  constexpr int UT = CT == 1 && G < 4 ? 2 : 1;  // 32-key tiles that are in work together, as far as registers go
+  __shared__ __align__(1024) u32x4_t ring[4 * HALF / 16];
+  __shared__ int bad_key[4];
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = lane % 32, g = lane / 32;
+  // LDS addresses of the first fragments, as in k_attn_sparse.h
+  const unsigned kat = lds0 + r * ROW + (g ^ Geo::swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
+  const int vr = 4 * g + (lane % 16) / 4;
+  const unsigned vat = lds0 + HALF + vr * ROW + ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ Geo::swizzle(vr)) * 16 + (lane % 2) * 8;
+  // This thread's part of a stage: 8 G channels of one key.  The keys are dealt out so that 16 lanes' pieces fall on different banks.
+  const int n = threadIdx.x / 4, quarter = threadIdx.x % 4;
+  const int key = G >= 3 ? (n & 3) << 2 | ((n >> 2) & 3) | (n & 48) : G == 2 ? (n & 1) | (n & 2) << 2 | (n & 12) >> 1 | (n & 48) : n;
+  const unsigned wat = lds0 + key * ROW;
+  const unsigned code_at = key * (16 * G) + quarter * (4 * G), scale_at = key * SB;
+
+  const unsigned chunk = (a.work + 7) / 8;  // contiguous per XCD
+  const unsigned chunk_end = min(a.work, (blockIdx.x % 8 + 1) * chunk);
+  for (unsigned work = blockIdx.x % 8 * chunk + blockIdx.x / 8; work < chunk_end; work += gridDim.x / 8) {
+    const CacheTile t(a, work);
+    int first_sub;
+    const int rho0 = t.tile * 128 * CT, first = t.token(a, rho0, first_sub);
+    if (first < 0) continue;
+    if (threadIdx.x < 4) bad_key[threadIdx.x] = INT32_MAX;
+    const int64_t last = min(min((int64_t)t.run * a.run_len + min((rho0 + 128 * CT - 1) / a.group, a.run_len - 1), (int64_t)t.q_len - 1), (int64_t)a.Nq - 1);
+    const int all = t.seen(a, first), any = t.seen(a, (int)last);
+    int token[CT], sub[CT], seen[CT];
+    u32x4_t q[CT][KS];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      token[c] = t.token(a, rho0 + (wave * CT + c) * 32 + r, sub[c]);
+      seen[c] = token[c] < 0 ? any : t.seen(a, token[c]);
+      const bf16* row = static_cast<const bf16*>(a.q) + t.b * a.qb + (int64_t)max(token[c], 0) * a.qn + (int64_t)(t.hk * a.group + (token[c] < 0 ? 0 : sub[c])) * a.qh;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int ch = 16 * s + 8 * g;
+        q[c][s] = u32x4_t{0, 0, 0, 0};
+        if (ch < a.d && token[c] >= 0) q[c][s] = *reinterpret_cast<const u32x4_t*>(row + ch);
+      }
+    }
+    const int64_t head = ((int64_t)t.b * a.c.heads + t.hk) * a.c.cap;
+    const uint8_t *kc = a.c.kc + head * (16 * G), *ks = a.c.ks + head * SB, *vc = a.c.vc + head * (16 * G), *vs = a.c.vs + head * SB;
+    const unsigned stages = ((unsigned)any + 63u) / 64u;
+    const unsigned lo = (unsigned)((uint64_t)stages * t.part / a.nsplit), hi = (unsigned)((uint64_t)stages * (t.part + 1) / a.nsplit);
+
+    unsigned kn[G], vn[G], ksn, vsn;
+    auto fetch = [&](unsigned st) {
+      const int key0 = (int)(st * 64), left = any - key0;
+      const bool in = key < left;
+      auto words = [&](const uint8_t* p, unsigned (&w)[G]) {
+        if constexpr (G == 4) {
+          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = v[i];
+        } else if constexpr (G == 2) {
+          const uint2 v = *reinterpret_cast<const uint2*>(p);
+          w[0] = v.x; w[1] = v.y;
+        } else {
+#pragma unroll
+          for (int i = 0; i < G; ++i) w[i] = reinterpret_cast<const unsigned*>(p)[i];
+        }
+      };
+      auto scale = [&](const uint8_t* p) -> unsigned {
+        if constexpr (SB == 4) return *reinterpret_cast<const unsigned*>(p);
+        else if constexpr (SB == 2) return *reinterpret_cast<const unsigned short*>(p);
+        else return *p;
+      };
+      ksn = vsn = 0x7F7F7F7Fu;  // what no row sees counts as zero
+#pragma unroll
+      for (int i = 0; i < G; ++i) kn[i] = vn[i] = 0u;
+      if (in) {
+        words(kc + (int64_t)key0 * (16 * G) + code_at, kn);
+        ksn = scale(ks + (int64_t)key0 * SB + scale_at);
+        words(vc + (int64_t)key0 * (16 * G) + code_at, vn);
+        vsn = scale(vs + (int64_t)key0 * SB + scale_at);
+      }
+    };
+    auto place = [&](unsigned st, unsigned slot) {  // the fetched codes, as bf16
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const unsigned group = G == 4 ? quarter : G == 2 ? quarter / 2 : G == 1 ? 0 : (3 * quarter + i) / 4;
+        const unsigned kscale = (ksn >> (8 * group)) & 255u;
+        unsigned vscale = (vsn >> (8 * group)) & 255u, vw = vn[i];
+        if (vscale == 255u) {
+          u32x4_t none;
+          note_nan(bad_key, group, (int)(st * 64) + key, none, vscale);
+          vw = 0u;
+        }
+        const unsigned at = wat + slot + ((G * quarter + i) ^ Geo::swizzle(key)) * 16;
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4_t*>((size_t)at) = cache4_bf16x8(kn[i], __uint_as_float(kscale << 23));
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4_t*>((size_t)(at + HALF)) = cache4_bf16x8(vw, __uint_as_float(vscale << 23));
+      }
+    };
+
+    f32x16_t o[CT][G];
+    float mref[CT], lsum[CT], lwt[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      mref[c] = kSparseLow;
+      lsum[c] = lwt[c] = 0.f;
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[c][i][e] = 0.f;
+    }
+    unsigned slot = 0;
+    __syncthreads();  // bad_key
+    if (lo < hi) {
+      fetch(lo);
+      place(lo, 0);
+      if (lo + 1 < hi) fetch(lo + 1);
+    }
+    __syncthreads();
+    for (unsigned st = lo; st < hi; ++st) {
+      if (st + 1 < hi) {
+        place(st + 1, slot ^ (2 * HALF));
+        if (st + 2 < hi) fetch(st + 2);
+      }
+#pragma unroll
+      for (int part = 0; part < 2 / UT; ++part) {
+        const unsigned at = slot + part * 32 * UT * ROW;
+        u32x4_t kf[KS][UT];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int u = 0; u < UT; ++u) kf[s][u] = lds_read<u32x4_t>(((kat + at) ^ (32 * s)) + 32 * u * ROW);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16_t sc[CT][UT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int u = 0; u < UT; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[c][u][e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int u = 0; u < UT; ++u)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+              sc[c][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s][u]), __builtin_bit_cast(bf16x8_t, q[c][s]), sc[c][u], 0, 0, 0);
+        const int key0 = (int)(st * 64) + part * 32 * UT;
+        if (key0 + 32 * UT > all) {
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            const int lim = seen[c] - key0 - 4 * g;  // register e of tile u is key 32 u + 8 (e / 4) + e % 4 + 4 g
+#pragma unroll
+            for (int u = 0; u < UT; ++u)
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (32 * u + 8 * (e / 4) + e % 4 >= lim) sc[c][u][e] = -INFINITY;
+          }
+        }
+        // the values are on their way while the exponentials are taken
+        uint2 vlo[2 * UT][G], vhi[2 * UT][G];
+#pragma unroll
+        for (int k16 = 0; k16 < 2 * UT; ++k16)
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            vlo[k16][i] = lds_read_tr(((vat + at) ^ (64 * i)) + 16 * k16 * ROW);
+            vhi[k16][i] = lds_read_tr(((vat + at) ^ (64 * i) ^ (Geo::swizzle(8) * 16)) + (16 * k16 + 8) * ROW);
+          }
+        __builtin_amdgcn_sched_barrier(0);
+
+        // ---- probabilities, as in the kernel above
+        u32x4_t pk[CT][2 * UT];
+        float rs[CT], rw[CT];
+        auto exponentiate = [&]() {
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            rs[c] = rw[c] = 0.f;
+#pragma unroll
+            for (int u = 0; u < UT; ++u)
+#pragma unroll
+              for (int e = 0; e < 16; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[c][u][e], a.scale_log2, -mref[c])), p1 = __builtin_amdgcn_exp2f(fmaf(sc[c][u][e + 1], a.scale_log2, -mref[c]));
+                const unsigned w = pack_bf16x2(p0, p1);
+                pk[c][2 * u + e / 8][e % 8 / 2] = w;
+                rs[c] = dot2_ones(w, rs[c]);
+                if constexpr (W) rw[c] += p0 + p1;
+              }
+          }
+        };
+        exponentiate();
+        bool grown = false;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) grown = grown || !(rs[c] <= kSparseTrigger);
+        if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            float mx = sc[c][0][0];
+#pragma unroll
+            for (int u = 0; u < UT; ++u)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[c][u][e]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * a.scale_log2;
+            const float up = fmaxf(mx, mref[c]), alpha = __builtin_amdgcn_exp2f(mref[c] - up);
+            mref[c] = up;
+            lsum[c] *= alpha;
+            if constexpr (W) lwt[c] *= alpha;
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[c][i][e] *= alpha;
+          }
+          exponentiate();
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          lsum[c] += rs[c];
+          if constexpr (W) lwt[c] += rw[c];
+        }
+
+        // ---- O^T += V^T P^T
+#pragma unroll
+        for (int k16 = 0; k16 < 2 * UT; ++k16)
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            const u32x4_t vf{vlo[k16][i].x, vlo[k16][i].y, vhi[k16][i].x, vhi[k16][i].y};
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+              o[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[c][k16]), o[c][i], 0, 0, 0);
+          }
+      }
+      slot ^= 2 * HALF;
+      __syncthreads();
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      lsum[c] += __shfl_xor(lsum[c], 32, kWave);
+      if constexpr (W) lwt[c] += __shfl_xor(lwt[c], 32, kWave);
+      if (token[c] < 0) continue;
+      const int h = t.hk * a.group + sub[c];
+      const int64_t row = ((int64_t)t.b * a.Nq + token[c]) * (a.c.heads * a.group) + h;
+      const float inv = lsum[c] == 0.f ? 0.f : 1.f / lsum[c];  // a row without keys gives zero
+      bf16* dst = static_cast<bf16*>(a.o) + t.b * a.ob + (int64_t)token[c] * a.on + (int64_t)h * a.oh;
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const bool bad = seen[c] > bad_key[i];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int ch = 32 * i + 8 * p + 4 * g;
+          if (ch >= a.d) continue;
+          f32x4_t y{o[c][i][4 * p], o[c][i][4 * p + 1], o[c][i][4 * p + 2], o[c][i][4 * p + 3]};
+          if (bad) y = f32x4_t{NAN, NAN, NAN, NAN};
+          if (a.nsplit > 1) {
+            *reinterpret_cast<f32x4_t*>(a.part + (row * a.nsplit + t.part) * a.d + ch) = y;
+            continue;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = lsum[c] == 0.f ? 0.f : y[j] * inv;
+          *reinterpret_cast<uint2*>(dst + ch) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+        }
+      }
+      if (g == 0) {
+        if (a.nsplit > 1) a.part_stat[row * a.nsplit + t.part] = f32x4_t{mref[c], lsum[c], lwt[c], 0.f};
+        else if (W) a.row_stat[row] = make_float2(mref[c], lwt[c] == 0.f ? 0.f : 1.f / lwt[c]);
+      }
+    }
+    __syncthreads();  // bad_key and the ring are the next tile's
   }
 }
 

@@ -143,12 +143,31 @@ static si_status enqueue_copy(const si_heads* k, const si_heads* v, const si_cac
 // ----------------------------------------------------------------------------- attention
 
 struct CachePlan {
-  int group, columns;  // query heads of a key head; columns of 16 rows of a tile
+  int group, tile_rows;  // query heads of a key head; rows of a tile: up to 32 by the few kernel, 128 and 256 by the other
   int64_t runs, run_len, tiles_per_run, work, rows, weight_chunks;
   int nsplit;
   size_t part_bytes, stat_bytes, row_bytes;
   size_t bytes() const { return part_bytes + stat_bytes + row_bytes + 256; }
 };
+
+// Into how many shares the keys of a tile are dealt out.  Few rows: until there are four workgroups for every CU, 256 keys at least to
+// each.  Many: the busiest CU's number of workgroups bounds the time (360 tiles on 256 CUs: 2 of 1.4, and 1.5 of 1.4 in two shares), and
+// the shares cost their way through memory; one workgroup alone on a CU takes three quarters of the time that two take.  A workgroup's
+// 64 keys of a row and channel take 0.073 ns at the rate of a whole chip's.
+static int64_t shares_of_tiles(int64_t tiles, int tile_rows, int64_t capacity, int64_t rows, int64_t d) {
+  if (tiles == 0) return 1;
+  const int64_t most = std::min<int64_t>(64, std::max<int64_t>(1, capacity / 256));
+  if (tile_rows <= 32) return tiles <= 512 ? std::min<int64_t>(1024 / tiles, most) : 1;
+  int64_t best = 1;
+  double least = 0.0;
+  for (int64_t n = 1; n <= most && n * tiles <= 4096; ++n) {
+    const double on_cu = (double)((tiles * n + 255) / 256);
+    const double us = std::max(on_cu, 1.5) / (double)n * (double)((capacity + 63) / 64) * (double)(tile_rows * d) * 0.073e-3 +
+                      (n > 1 ? 5.0 + (double)(rows * n) * (double)(d + 4) * 8.0 / 4e6 : 0.0);
+    if (n == 1 || us < least) { least = us; best = n; }
+  }
+  return best;
+}
 
 static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t run, bool weights, CachePlan* p) {
   si_status s = check_heads(q, false);
@@ -158,18 +177,18 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   if (run < 0 || run > kMostTokens) return SI_ERR_SHAPE;
   p->group = (int)(q->heads / c->heads);
   if ((double)p->group * (double)q->N >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;  // rows of a key head in 31 bits
-  // A tile ends with its run, so that its rows see the same keys; runs shorter than the smallest tile share them.
-  const bool own = run > 0 && run < q->N && p->group * run >= 16;
+  const int64_t rows_of_run = p->group * (run > 0 && run < q->N ? run : std::max<int64_t>(q->N, 1)), rows = p->group * std::max<int64_t>(q->N, 1);
+  const bool many = q->dtype == SI_BF16 && rows > 64;
+  p->tile_rows = !many ? (rows <= 16 ? 16 : 32) : cache_groups(c) <= 2 && rows > 128 ? 256 : 128;
+  // A tile ends with its run, so that its rows see the same keys; runs shorter than a tile share them.
+  const bool own = run > 0 && run < q->N && rows_of_run >= p->tile_rows;
   p->run_len = own ? run : std::max<int64_t>(q->N, 1);
   p->runs = q->N == 0 ? 0 : (q->N + p->run_len - 1) / p->run_len;
-  const int64_t rows_of_run = p->group * p->run_len;
-  p->columns = rows_of_run <= 16 ? 1 : 2;
-  p->tiles_per_run = (rows_of_run + 16 * p->columns - 1) / (16 * p->columns);
+  p->tiles_per_run = (p->group * p->run_len + p->tile_rows - 1) / p->tile_rows;
   const double tiles = (double)(c->B * c->heads) * (double)p->runs * (double)p->tiles_per_run;
   if (tiles >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
-  // Keys are dealt out while there are fewer than four workgroups for every CU, 256 keys at least to each.
   const int64_t t = (int64_t)tiles;
-  p->nsplit = t > 0 && t <= 512 ? (int)std::min<int64_t>(std::min<int64_t>(1024 / t, 64), std::max<int64_t>(1, c->capacity / 256)) : 1;
+  p->nsplit = (int)shares_of_tiles(t, p->tile_rows, c->capacity, q->B * q->N * q->heads, q->dim_head);
   p->work = t * p->nsplit;
   p->rows = q->B * q->N * q->heads;
   p->part_bytes = p->nsplit > 1 ? align_up((size_t)(p->rows * p->nsplit * q->dim_head) * 4, 256) : 0;
@@ -186,9 +205,18 @@ template <typename T>
 static si_status launch_cache_attn(const CacheAttnArgs& a, const CacheWeightArgs* w, const si_cache4* c, const CachePlan& p, hipStream_t st) {
   if (p.work > 0) {
     StageScope scope("cache4_attn", st);
+    const unsigned grid = grid_of(p.work);
     by_groups(c, [&](auto g) {
-      if (p.columns == 1) cache4_attn_few_kernel<T, g.value, 1><<<grid_of(p.work), 256, 0, st>>>(a);
-      else cache4_attn_few_kernel<T, g.value, 2><<<grid_of(p.work), 256, 0, st>>>(a);
+      if (p.tile_rows == 16) cache4_attn_few_kernel<T, g.value, 1><<<grid, 256, 0, st>>>(a);
+      else if (p.tile_rows == 32) cache4_attn_few_kernel<T, g.value, 2><<<grid, 256, 0, st>>>(a);
+      else if constexpr (sizeof(T) == 2) {
+        auto launch = [&](auto ct) {
+          if (w) cache4_attn_many_kernel<g.value, ct.value, true><<<grid, 256, 0, st>>>(a);
+          else cache4_attn_many_kernel<g.value, ct.value, false><<<grid, 256, 0, st>>>(a);
+        };
+        if (p.tile_rows == 128) launch(std::integral_constant<int, 1>());
+        else if constexpr (g.value <= 2) launch(std::integral_constant<int, 2>());
+      }
     });
     if (p.nsplit > 1) cache4_join_kernel<T><<<(unsigned)((p.rows + 3) / 4), 256, 0, st>>>(a, (int)p.rows);
     SI_CHECK_LAUNCH();
