@@ -753,7 +753,7 @@ struct CacheWeightArgs {
   Cache4View c;
   const int *q_len, *k_len;
   int Nq, group, d, run;
-  int chunks;                // of 128 keys
+  int chunks;                // of 128 keys, or 256
   unsigned work;             // B * heads * chunks
   float scale_log2, decay;
   const float2* row_stat;
@@ -828,6 +828,142 @@ __global__ __launch_bounds__(256) void cache4_weight_kernel(CacheWeightArgs a) {
       const float mine = r == 0 ? sum[u][0] : r == 1 ? sum[u][1] : r == 2 ? sum[u][2] : sum[u][3];
       if (r < 4 && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + mine;
     }
+  }
+}
+
+// The same for rows by the hundred, in bf16.  A wavefront keeps 64 keys as bf16 operands, a workgroup 256, and walks the rows in tiles of 32
+// that all four share in LDS (direct global->LDS loads, one tile ahead): a tile's products are 2 G chains of matrix
+// instructions beside an fma, an exponential and an fma for every score.
+template <int G>
+__global__ __launch_bounds__(256, G <= 2 ? 3 : 2) void cache4_weight_many_kernel(CacheWeightArgs a) {
+  using Geo = SparseGeo<bf16, 2 * G, 4>;
+  constexpr int ROW = Geo::ROW, TILE = 32 * ROW, KS = 2 * G, SB = cache4_scale_bytes(G);
+  constexpr int LOADS = TILE / 4096 > 0 ? TILE / 4096 : 1;  // of a wavefront and tile, 1 KiB each; tiles of 2 KiB leave two wavefronts without
+  __shared__ __align__(1024) u32x4_t ring[2 * TILE / 16];
+  __shared__ float2 stats[2][32];
+  __shared__ int ends[2][32];
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = lane % 32, g = lane / 32;
+  const unsigned qat = lds0 + r * ROW + (g ^ Geo::swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
+  const unsigned part = (a.work + 7) / 8, part_end = min(a.work, (blockIdx.x % 8 + 1) * part);
+  for (unsigned work = blockIdx.x % 8 * part + blockIdx.x / 8; work < part_end; work += gridDim.x / 8) {
+    const unsigned bh = work / (unsigned)a.chunks;
+    const int b = (int)(bh / (unsigned)a.c.heads), hk = (int)(bh % (unsigned)a.c.heads);
+    const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.c.cap) : a.c.cap;
+    const int64_t first_key = (int64_t)(work % (unsigned)a.chunks) * 256;
+    if (first_key >= k_len) continue;
+    const int key0 = (int)first_key + wave * 64, last_key = min((int)min(first_key + 256, (int64_t)k_len), k_len);  // behind the workgroup's last
+    const int64_t head = ((int64_t)b * a.c.heads + hk) * a.c.cap;
+
+    // ---- this wavefront's keys: tile u, step s: channels 16 s + 8 g .. + 7 of key 32 u + r
+    u32x4_t kf[2][KS];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t key = head + min(key0 + 32 * u + r, k_len - 1);
+      const uint8_t* codes = a.c.kc + key * (16 * G);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        kf[u][s] = cache4_bf16x8(*reinterpret_cast<const unsigned*>(codes + (16 * s + 8 * g) / 2), __uint_as_float((unsigned)a.c.ks[key * SB + s / 2] << 23));
+    }
+    f32x16_t sum[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum[u][e] = 0.f;
+
+    // ---- rows: q_len tokens times `group` heads; the first that see one of these keys
+    const int rows = q_len * a.group;
+    int begin = 0;
+    if (a.run) {
+      // token n sees key j iff the end of its run, min((n / run + 1) run, q_len), is beyond j + q_len - k_len
+      const int64_t over = first_key + q_len - k_len;
+      begin = over < 0 ? 0 : (int)(over / a.run * a.run) * a.group;
+    }
+    const int tiles = rows > begin ? (rows - begin + 31) / 32 : 0;
+    // what tile i's loads of a wavefront bring: rows of 16-byte pieces, by neighbouring lanes
+    auto issue = [&](int i, unsigned slot) {
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l) {
+        if (TILE < 4096 && wave * 1024 >= TILE) continue;
+        const int row = (wave + 4 * l) * (64 / Geo::PR) + lane / Geo::PR, at = (lane % Geo::PR) ^ Geo::swizzle(row), piece = at * 8 < a.d ? at : 0;
+        const int rho = min(begin + 32 * i + row, rows - 1), n = a.group > 1 ? rho / a.group : rho;
+        const bf16* src = static_cast<const bf16*>(a.q) + b * a.qb + (int64_t)n * a.qn + (int64_t)(hk * a.group + rho - n * a.group) * a.qh + piece * 8;
+        load_to_lds(src, lds0 + slot * TILE + (wave + 4 * l) * 1024);
+      }
+    };
+    float2 next_stat;
+    int next_end;
+    auto stat_of = [&](int i) {  // of row r of tile i, by every wavefront's lanes
+      const int rho = begin + 32 * i + r;
+      next_stat = make_float2(INFINITY, 0.f);  // no row: 2^-inf
+      next_end = 0;
+      if (rho < rows) {
+        const int n = a.group > 1 ? rho / a.group : rho;
+        next_stat = a.row_stat[((int64_t)b * a.Nq + n) * (a.c.heads * a.group) + hk * a.group + rho - n * a.group];
+        next_end = CacheTile::cache_seen(a.run, n, q_len, k_len);
+      }
+    };
+    __syncthreads();  // nobody reads the ring of the piece before
+    if (tiles > 0) {
+      stat_of(0);
+      if (wave == 0 && g == 0) { stats[0][r] = next_stat; ends[0][r] = next_end; }
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      issue(0, 0);
+    }
+    for (int i = 0; i < tiles; ++i) {
+      const int slot = i & 1;
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // tile i
+      __syncthreads();
+      if (i + 1 < tiles) {
+        if (wave == 0) stat_of(i + 1);
+        issue(i + 1, slot ^ 1);
+      }
+      u32x4_t qf[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        qf[s] = lds_read<u32x4_t>((qat ^ (32 * s)) + slot * TILE);
+        if (16 * s + 8 * g >= a.d) qf[s] = u32x4_t{0, 0, 0, 0};
+      }
+      const float2 stat = stats[slot][r];
+      f32x16_t sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[u][s]), __builtin_bit_cast(bf16x8_t, qf[s]), sc[u], 0, 0, 0);
+      // does the tile's first row, which sees the fewest keys, see all of this workgroup's, and is there a last row
+      if (__builtin_amdgcn_readfirstlane(ends[slot][0]) < last_key || begin + 32 * i + 32 > rows) {
+        const int lim = ends[slot][r] - key0 - 4 * g;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][e], a.scale_log2, -stat.x)) * stat.y;
+            sum[u][e] += 32 * u + 8 * (e / 4) + e % 4 < lim ? p : 0.f;
+          }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum[u][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[u][e], a.scale_log2, -stat.x)), stat.y, sum[u][e]);
+      }
+      if (i + 1 < tiles && wave == 0 && g == 0) { stats[slot ^ 1][r] = next_stat; ends[slot ^ 1][r] = next_end; }
+    }
+    // register e of tile u, lanes of half g: key 32 u + 8 (e / 4) + 4 g + e % 4, summed over the half's 32 rows
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+#pragma unroll
+        for (int step = 1; step < 32; step <<= 1) sum[u][e] += __shfl_xor(sum[u][e], step, kWave);
+        const int key = key0 + 32 * u + 8 * (e / 4) + 4 * g + e % 4;
+        if (r == e && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + sum[u][e];
+      }
   }
 }
 

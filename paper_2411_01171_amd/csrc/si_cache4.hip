@@ -145,6 +145,7 @@ static si_status enqueue_copy(const si_heads* k, const si_heads* v, const si_cac
 struct CachePlan {
   int group, tile_rows;  // query heads of a key head; rows of a tile: up to 32 by the few kernel, 128 and 256 by the other
   int64_t runs, run_len, tiles_per_run, work, rows, weight_chunks;
+  int weight_keys;  // of a workgroup of the weights' kernel
   int nsplit;
   size_t part_bytes, stat_bytes, row_bytes;
   size_t bytes() const { return part_bytes + stat_bytes + row_bytes + 256; }
@@ -194,7 +195,8 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   p->part_bytes = p->nsplit > 1 ? align_up((size_t)(p->rows * p->nsplit * q->dim_head) * 4, 256) : 0;
   p->stat_bytes = p->nsplit > 1 ? align_up((size_t)(p->rows * p->nsplit) * 16, 256) : 0;
   p->row_bytes = weights ? align_up((size_t)p->rows * 8, 256) : 0;
-  p->weight_chunks = (c->capacity + 127) / 128;
+  p->weight_keys = q->dtype == SI_BF16 && p->group * q->N > 64 ? 256 : 128;
+  p->weight_chunks = (c->capacity + p->weight_keys - 1) / p->weight_keys;
   if ((double)(c->B * c->heads) * (double)p->weight_chunks >= 4294967296.0 - kGridMost) return SI_ERR_SHAPE;
   return SI_OK;
 }
@@ -223,7 +225,11 @@ static si_status launch_cache_attn(const CacheAttnArgs& a, const CacheWeightArgs
   }
   if (w && w->work > 0) {
     StageScope scope("cache4_weight", st);
-    by_groups(c, [&](auto g) { cache4_weight_kernel<T, g.value><<<grid_of(w->work), 256, 0, st>>>(*w); });
+    const unsigned grid = grid_of(w->work);
+    by_groups(c, [&](auto g) {
+      if (sizeof(T) == 2 && p.weight_keys == 256) cache4_weight_many_kernel<g.value><<<grid, 256, 0, st>>>(*w);
+      else cache4_weight_kernel<T, g.value><<<grid, 256, 0, st>>>(*w);
+    });
     SI_CHECK_LAUNCH();
   }
   return SI_OK;
