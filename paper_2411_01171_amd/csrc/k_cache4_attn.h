@@ -31,7 +31,7 @@ struct CacheAttnArgs {
   float scale_log2;          // softmax scale * log2(e)
   float* part;               // nsplit > 1: outputs [query row][nsplit][d]; query row = (b Nq + n) heads + h
   f32x4_t* part_stat;        // nsplit > 1: (maximum, sum of the rounded weights, sum of the weights) [query row][nsplit]
-  float2* row_stat;          // or NULL: (maximum, 1 / sum of the weights) [query row]
+  float2* row_stat;          // or NULL: row_stat() of every query row
 };
 
 // Batch entry, key head, tile and share of a piece of work, and which keys its rows see.
@@ -67,6 +67,13 @@ struct CacheTile {
     return (int)max((int64_t)0, k_len - q_len + end);
   }
 };
+
+// What turns a score s of a row into its softmax weight, 2^(c s - x) y: the maximum and 1 / sum of the weights.  No keys: y = 0; NaN: x is NaN and
+// y is not, so that what the row does not see can be left out by a weight of zero.
+__device__ __forceinline__ float2 row_stat(float maximum, float sum) {
+  if (!(sum == sum)) return make_float2(NAN, 1.f);
+  return make_float2(maximum, sum == 0.f ? 0.f : 1.f / sum);
+}
 
 // A pair of values as bf16 parts: one, rounded, or three that add up to it, eight of its 24 bits each.
 template <int TERMS>
@@ -422,7 +429,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
         }
         if (g == 0) {
           if (a.nsplit > 1) a.part_stat[row * a.nsplit + t.part] = f32x4_t{mref[c], lsum[c], lwt[c], 0.f};
-          else if (a.row_stat) a.row_stat[row] = make_float2(mref[c], lwt[c] == 0.f ? 0.f : 1.f / lwt[c]);
+          else if (a.row_stat) a.row_stat[row] = row_stat(mref[c], lwt[c]);
         }
       }
     }
@@ -694,7 +701,7 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
       }
       if (g == 0) {
         if (a.nsplit > 1) a.part_stat[row * a.nsplit + t.part] = f32x4_t{mref[c], lsum[c], lwt[c], 0.f};
-        else if (W) a.row_stat[row] = make_float2(mref[c], lwt[c] == 0.f ? 0.f : 1.f / lwt[c]);
+        else if (W) a.row_stat[row] = row_stat(mref[c], lwt[c]);
       }
     }
     __syncthreads();  // bad_key and the ring are the next tile's
@@ -737,7 +744,7 @@ __global__ __launch_bounds__(256) void cache4_join_kernel(CacheAttnArgs a, int r
   for (int step = width; step < kWave; step <<= 1)
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], step, kWave);
-  if (a.row_stat && lane == 0) a.row_stat[row] = make_float2(top, lw == 0.f ? 0.f : 1.f / lw);
+  if (a.row_stat && lane == 0) a.row_stat[row] = row_stat(top, lw);
   if (which != 0 || quad >= quads) return;
   const float inv = 1.f / l;
 #pragma unroll
@@ -747,13 +754,15 @@ __global__ __launch_bounds__(256) void cache4_join_kernel(CacheAttnArgs a, int r
   else *reinterpret_cast<f32x4_t*>(dst) = o;
 }
 
+constexpr int kWeightTiles = 2;  // of 32 keys, that a wavefront of the kernel for many rows keeps
+
 struct CacheWeightArgs {
   const void* q;
   int64_t qb, qn, qh;
   Cache4View c;
   const int *q_len, *k_len;
   int Nq, group, d, run;
-  int chunks;                // of 128 keys, or 256
+  int chunks;                // pieces of a head's keys: of 128, of 128 kWeightTiles, or shares
   unsigned work;             // B * heads * chunks
   float scale_log2, decay;
   const float2* row_stat;
@@ -762,9 +771,105 @@ struct CacheWeightArgs {
 };
 
 // out[key] = decay in[key] + sum over the rows that see it of their softmax weight, in an order that depends on sizes only.  The scores are
-// taken again, against the rows' maxima and sums of the whole call.  A wavefront keeps 32 keys and walks the rows.
+// taken again, against the rows' maxima and sums of the whole call: keys come from memory a second time, where keeping
+// the scores would write and read 8 bytes of every row.
+//   S[row, key] = Q K^T         row operand: rows, column operand: keys
+// Up to 16 NT rows, kept as operands with their statistics; a wavefront walks every fourth step of 32 keys of its workgroup's share.
+template <typename T, int G, int NT>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? (NT == 1 ? 4 : 3) : 2) void cache4_weight_few_kernel(CacheWeightArgs a) {
+  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
+  constexpr int SB = cache4_scale_bytes(G);
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = lane % 16, g = lane / 16;
+  const unsigned part = (a.work + 7) / 8, part_end = min(a.work, (blockIdx.x % 8 + 1) * part);
+  for (unsigned work = blockIdx.x % 8 * part + blockIdx.x / 8; work < part_end; work += gridDim.x / 8) {
+    const unsigned bh = work / (unsigned)a.chunks, share = work % (unsigned)a.chunks;
+    const int b = (int)(bh / (unsigned)a.c.heads), hk = (int)(bh % (unsigned)a.c.heads), heads = a.c.heads * a.group;
+    const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.c.cap) : a.c.cap;
+    const unsigned steps = ((unsigned)k_len + 31u) / 32u;
+    const unsigned lo = (unsigned)((uint64_t)steps * share / (unsigned)a.chunks), hi = (unsigned)((uint64_t)steps * (share + 1) / (unsigned)a.chunks);
+    if (lo + wave >= hi) continue;
+    const int64_t head = ((int64_t)b * a.c.heads + hk) * a.c.cap;
+    const uint8_t *codes = a.c.kc + head * (16 * G), *scales = a.c.ks + head * SB;
+    KeyCodes<G> kn;
+    kn.load(codes, scales, (int)((lo + wave) * 32), k_len, r, g);
+    const int rows = q_len * a.group;
+    u32x4_t q[NT][G][TERMS];
+    float2 stat[NT][4];
+    int seen[NT][4], all = k_len;  // keys that every row sees
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      const int rho = 16 * c + r, n = rho / a.group, h = hk * a.group + rho - n * a.group;
+      const T* row = static_cast<const T*>(a.q) + b * a.qb + (int64_t)n * a.qn + (int64_t)h * a.qh;
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const int ch = 8 * (G * g + i);
+#pragma unroll
+        for (int x = 0; x < TERMS; ++x) q[c][i][x] = u32x4_t{0, 0, 0, 0};
+        if (ch < a.d && rho < rows) query_parts<T, TERMS>(row + ch, q[c][i]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {  // of row 4 g + j, as the scores lie
+        const int of = 16 * c + 4 * g + j, token = of / a.group;
+        stat[c][j] = make_float2(INFINITY, 0.f);  // no row: 2^-inf
+        seen[c][j] = 0;
+        if (of < rows) {
+          stat[c][j] = a.row_stat[((int64_t)b * a.Nq + token) * heads + hk * a.group + of - token * a.group];
+          seen[c][j] = CacheTile::cache_seen(a.run, token, q_len, k_len);
+        }
+      }
+    }
+    if (rows < 16 * NT) all = 0;
+    else if (a.run) all = CacheTile::cache_seen(a.run, 0, q_len, k_len);
+    for (unsigned step = lo + wave; step < hi; step += 4) {
+      const int key0 = (int)(step * 32);
+      const KeyCodes<G> k = kn;
+      if (step + 4 < hi) kn.load(codes, scales, key0 + 128, k_len, r, g);
+      float total[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8_t kf[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) kf[i] = __builtin_bit_cast(bf16x8_t, k.operand(u, i, g));
+        f32x4_t sc[NT];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) sc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int x = TERMS - 1; x >= 0; --x)  // the smallest part first
+              sc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, q[c][i][x]), kf[i], sc[c], 0, 0, 0);
+        float p[NT][4];
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p[c][j] = __builtin_amdgcn_exp2f(fmaf(sc[c][j], a.scale_log2, -stat[c][j].x));
+        if (key0 + 32 > all) {
+#pragma unroll
+          for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (key0 + 16 * u + r >= seen[c][j]) p[c][j] = 0.f;
+        }
+        float t = 0.f;
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t = fmaf(p[c][j], stat[c][j].y, t);
+        t += __shfl_xor(t, 16, kWave);
+        total[u] = t + __shfl_xor(t, 32, kWave);
+      }
+      const int key = key0 + lane;  // lanes of the first two groups write a tile's keys each
+      if (lane < 32 && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + (g == 0 ? total[0] : total[1]);
+    }
+  }
+}
+
+// The same for more rows than that in float32: a wavefront keeps 32 keys and walks the rows.
 template <typename T, int G>
-__global__ __launch_bounds__(256) void cache4_weight_kernel(CacheWeightArgs a) {
+__global__ __launch_bounds__(256) void cache4_weight_rows_kernel(CacheWeightArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
   constexpr int SB = cache4_scale_bytes(G);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -831,44 +936,64 @@ __global__ __launch_bounds__(256) void cache4_weight_kernel(CacheWeightArgs a) {
   }
 }
 
-// The same for rows by the hundred, in bf16.  A wavefront keeps 64 keys as bf16 operands, a workgroup 256, and walks the rows in tiles of 32
-// that all four share in LDS (direct global->LDS loads, one tile ahead): a tile's products are 2 G chains of matrix
-// instructions beside an fma, an exponential and an fma for every score.
+// The same for more rows in bf16.  A wavefront keeps 64 keys as bf16 operands, a workgroup 256, and walks the rows in tiles of 32
+// that all four share in LDS (direct global->LDS loads, one tile ahead).  Bound by the vector ALUs: an fma, an exponential and an fma
+// for every score, beside 2 G matrix instructions of 32 clocks for 32 of them.
+// A row's address and statistics are found by steps from tile to tile, without a division.
 template <int G>
 __global__ __launch_bounds__(256, G <= 2 ? 3 : 2) void cache4_weight_many_kernel(CacheWeightArgs a) {
   using Geo = SparseGeo<bf16, 2 * G, 4>;
+  constexpr int KT = kWeightTiles;
   constexpr int ROW = Geo::ROW, TILE = 32 * ROW, KS = 2 * G, SB = cache4_scale_bytes(G);
   constexpr int LOADS = TILE / 4096 > 0 ? TILE / 4096 : 1;  // of a wavefront and tile, 1 KiB each; tiles of 2 KiB leave two wavefronts without
   __shared__ __align__(1024) u32x4_t ring[2 * TILE / 16];
-  __shared__ float2 stats[2][32];
-  __shared__ int ends[2][32];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int r = lane % 32, g = lane / 32;
+  const int r = lane % 32, g = lane / 32, heads = a.c.heads * a.group;
   const unsigned qat = lds0 + r * ROW + (g ^ Geo::swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
+  const int step_n = 32 / a.group, step_sub = 32 % a.group;          // from a tile to the next
+  // Row rho of a key head, as a token and one of its query heads, and an offset that grows with both.
+  struct Row {
+    int rho, sub;
+    int64_t at;
+    __device__ __forceinline__ Row(int rho_, int group, int64_t per_token, int64_t per_head) : rho(rho_) {
+      const int n = group > 1 ? rho / group : rho;
+      sub = rho - n * group;
+      at = n * per_token + sub * per_head;
+    }
+    __device__ __forceinline__ void step(int group, int n, int s, int64_t per_token, int64_t per_head) {
+      rho += 32;
+      sub += s;
+      at += n * per_token + s * per_head;
+      if (sub >= group) {
+        sub -= group;
+        at += per_token - group * per_head;
+      }
+    }
+  };
   const unsigned part = (a.work + 7) / 8, part_end = min(a.work, (blockIdx.x % 8 + 1) * part);
   for (unsigned work = blockIdx.x % 8 * part + blockIdx.x / 8; work < part_end; work += gridDim.x / 8) {
     const unsigned bh = work / (unsigned)a.chunks;
     const int b = (int)(bh / (unsigned)a.c.heads), hk = (int)(bh % (unsigned)a.c.heads);
     const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.c.cap) : a.c.cap;
-    const int64_t first_key = (int64_t)(work % (unsigned)a.chunks) * 256;
+    const int64_t first_key = (int64_t)(work % (unsigned)a.chunks) * (128 * KT);
     if (first_key >= k_len) continue;
-    const int key0 = (int)first_key + wave * 64, last_key = min((int)min(first_key + 256, (int64_t)k_len), k_len);  // behind the workgroup's last
+    const int key0 = (int)first_key + wave * 32 * KT, last_key = (int)min(first_key + 128 * KT, (int64_t)k_len);  // behind the workgroup's last
     const int64_t head = ((int64_t)b * a.c.heads + hk) * a.c.cap;
 
     // ---- this wavefront's keys: tile u, step s: channels 16 s + 8 g .. + 7 of key 32 u + r
-    u32x4_t kf[2][KS];
+    u32x4_t kf[KT][KS];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < KT; ++u) {
       const int64_t key = head + min(key0 + 32 * u + r, k_len - 1);
       const uint8_t* codes = a.c.kc + key * (16 * G);
 #pragma unroll
       for (int s = 0; s < KS; ++s)
         kf[u][s] = cache4_bf16x8(*reinterpret_cast<const unsigned*>(codes + (16 * s + 8 * g) / 2), __uint_as_float((unsigned)a.c.ks[key * SB + s / 2] << 23));
     }
-    f32x16_t sum[2];
+    f32x16_t sum[KT];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < KT; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sum[u][e] = 0.f;
 
@@ -881,89 +1006,88 @@ __global__ __launch_bounds__(256, G <= 2 ? 3 : 2) void cache4_weight_many_kernel
       begin = over < 0 ? 0 : (int)(over / a.run * a.run) * a.group;
     }
     const int tiles = rows > begin ? (rows - begin + 31) / 32 : 0;
-    // what tile i's loads of a wavefront bring: rows of 16-byte pieces, by neighbouring lanes
-    auto issue = [&](int i, unsigned slot) {
+    // what a wavefront's loads bring: rows of 16-byte pieces, by neighbouring lanes
+    const bf16* q0 = static_cast<const bf16*>(a.q) + b * a.qb + (int64_t)hk * a.group * a.qh;
+    auto load_row = [&](int l) { return (wave + 4 * l) * (64 / Geo::PR) + lane / Geo::PR; };
+    auto load_piece = [&](int l) {
+      const int at = (lane % Geo::PR) ^ Geo::swizzle(load_row(l));
+      return at * 8 < a.d ? at * 8 : 0;
+    };
+    Row of[2] = {Row(begin + load_row(0), a.group, a.qn, a.qh), Row(begin + load_row(LOADS - 1), a.group, a.qn, a.qh)};
+    Row mine(begin + r, a.group, heads, 1);  // whose statistics this lane holds
+    const float2* stat0 = a.row_stat + (int64_t)b * a.Nq * heads + hk * a.group;
+    float2 next_stat;
+    auto issue = [&](unsigned slot) {
+      next_stat = stat0[mine.rho < rows ? mine.at : 0];
+      if (mine.rho >= rows) next_stat = make_float2(INFINITY, 0.f);  // no row: 2^-inf
+      mine.step(a.group, step_n, step_sub, heads, 1);
 #pragma unroll
       for (int l = 0; l < LOADS; ++l) {
-        if (TILE < 4096 && wave * 1024 >= TILE) continue;
-        const int row = (wave + 4 * l) * (64 / Geo::PR) + lane / Geo::PR, at = (lane % Geo::PR) ^ Geo::swizzle(row), piece = at * 8 < a.d ? at : 0;
-        const int rho = min(begin + 32 * i + row, rows - 1), n = a.group > 1 ? rho / a.group : rho;
-        const bf16* src = static_cast<const bf16*>(a.q) + b * a.qb + (int64_t)n * a.qn + (int64_t)(hk * a.group + rho - n * a.group) * a.qh + piece * 8;
-        load_to_lds(src, lds0 + slot * TILE + (wave + 4 * l) * 1024);
-      }
-    };
-    float2 next_stat;
-    int next_end;
-    auto stat_of = [&](int i) {  // of row r of tile i, by every wavefront's lanes
-      const int rho = begin + 32 * i + r;
-      next_stat = make_float2(INFINITY, 0.f);  // no row: 2^-inf
-      next_end = 0;
-      if (rho < rows) {
-        const int n = a.group > 1 ? rho / a.group : rho;
-        next_stat = a.row_stat[((int64_t)b * a.Nq + n) * (a.c.heads * a.group) + hk * a.group + rho - n * a.group];
-        next_end = CacheTile::cache_seen(a.run, n, q_len, k_len);
+        if (TILE >= 4096 || wave * 1024 < TILE)
+          load_to_lds(q0 + (of[l].rho < rows ? of[l].at : 0) + load_piece(l), lds0 + slot * TILE + (wave + 4 * l) * 1024);
+        of[l].step(a.group, step_n, step_sub, a.qn, a.qh);
       }
     };
     __syncthreads();  // nobody reads the ring of the piece before
-    if (tiles > 0) {
-      stat_of(0);
-      if (wave == 0 && g == 0) { stats[0][r] = next_stat; ends[0][r] = next_end; }
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-      issue(0, 0);
-    }
+    if (tiles > 0) issue(0);
     for (int i = 0; i < tiles; ++i) {
       const int slot = i & 1;
+      const float2 stat = next_stat;
       __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // tile i
       __syncthreads();
-      if (i + 1 < tiles) {
-        if (wave == 0) stat_of(i + 1);
-        issue(i + 1, slot ^ 1);
-      }
+      if (i + 1 < tiles) issue(slot ^ 1);
       u32x4_t qf[KS];
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         qf[s] = lds_read<u32x4_t>((qat ^ (32 * s)) + slot * TILE);
-        if (16 * s + 8 * g >= a.d) qf[s] = u32x4_t{0, 0, 0, 0};
+        if (s >= 2 * G - 2 && 16 * s + 8 * g >= a.d) qf[s] = u32x4_t{0, 0, 0, 0};  // d is more than 32 (G - 1)
       }
-      const float2 stat = stats[slot][r];
-      f32x16_t sc[2];
+      f32x16_t sc[KT];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < KT; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < KT; ++u)
           sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[u][s]), __builtin_bit_cast(bf16x8_t, qf[s]), sc[u], 0, 0, 0);
-      // does the tile's first row, which sees the fewest keys, see all of this workgroup's, and is there a last row
-      if (__builtin_amdgcn_readfirstlane(ends[slot][0]) < last_key || begin + 32 * i + 32 > rows) {
-        const int lim = ends[slot][r] - key0 - 4 * g;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < KT; ++u)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][e], a.scale_log2, -stat.x)) * stat.y;
-            sum[u][e] += 32 * u + 8 * (e / 4) + e % 4 < lim ? p : 0.f;
-          }
-      } else {
+        for (int e = 0; e < 16; ++e) sc[u][e] = __builtin_amdgcn_exp2f(fmaf(sc[u][e], a.scale_log2, -stat.x));
+      // is there a last row among these, or one, then the first, that does not see all of the workgroup's keys
+      const int rho0 = begin + 32 * i;
+      if (rho0 + 32 > rows || (a.run && CacheTile::cache_seen(a.run, rho0 / a.group, q_len, k_len) < last_key)) {
+        const int lim = rho0 + r < rows ? CacheTile::cache_seen(a.run, (rho0 + r) / a.group, q_len, k_len) - key0 - 4 * g : 0;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < KT; ++u)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sum[u][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[u][e], a.scale_log2, -stat.x)), stat.y, sum[u][e]);
+          for (int e = 0; e < 16; ++e)
+            if (32 * u + 8 * (e / 4) + e % 4 >= lim) sc[u][e] = 0.f;
       }
-      if (i + 1 < tiles && wave == 0 && g == 0) { stats[slot ^ 1][r] = next_stat; ends[slot ^ 1][r] = next_end; }
+#pragma unroll
+      for (int u = 0; u < KT; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[u][e] = fmaf(sc[u][e], stat.y, sum[u][e]);
     }
-    // register e of tile u, lanes of half g: key 32 u + 8 (e / 4) + 4 g + e % 4, summed over the half's 32 rows
+    // Register e of tile u, lanes of half g: key 32 u + 8 (e / 4) + 4 g + e % 4, to be summed over the half's 32 rows.  At every step a lane
+    // hands over one half of its keys and keeps the other; lanes 2 e and 2 e + 1 end with key e.
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < KT; ++u) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
+      for (int n = 8; n >= 1; n /= 2) {
+        const bool upper = (r & (2 * n)) != 0;
 #pragma unroll
-        for (int step = 1; step < 32; step <<= 1) sum[u][e] += __shfl_xor(sum[u][e], step, kWave);
-        const int key = key0 + 32 * u + 8 * (e / 4) + 4 * g + e % 4;
-        if (r == e && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + sum[u][e];
+        for (int e = 0; e < n; ++e) {
+          const float keep = upper ? sum[u][e + n] : sum[u][e], give = upper ? sum[u][e] : sum[u][e + n];
+          sum[u][e] = keep + __shfl_xor(give, 2 * n, kWave);
+        }
       }
+      const float total = sum[u][0] + __shfl_xor(sum[u][0], 1, kWave);
+      const int e = r / 2, key = key0 + 32 * u + 8 * (e / 4) + 4 * g + e % 4;
+      if (r % 2 == 0 && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + total;
+    }
   }
 }
 

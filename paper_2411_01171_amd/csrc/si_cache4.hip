@@ -145,20 +145,20 @@ static si_status enqueue_copy(const si_heads* k, const si_heads* v, const si_cac
 struct CachePlan {
   int group, tile_rows;  // query heads of a key head; rows of a tile: up to 32 by the few kernel, 128 and 256 by the other
   int64_t runs, run_len, tiles_per_run, work, rows, weight_chunks;
-  int weight_keys;  // of a workgroup of the weights' kernel
+  int weight_rows;  // that the weights' kernel keeps, or 0: it keeps keys
   int nsplit;
   size_t part_bytes, stat_bytes, row_bytes;
   size_t bytes() const { return part_bytes + stat_bytes + row_bytes + 256; }
 };
 
-// Into how many shares the keys of a tile are dealt out.  Few rows: until there are four workgroups for every CU, 256 keys at least to
-// each.  Many: the busiest CU's number of workgroups bounds the time (360 tiles on 256 CUs: 2 of 1.4, and 1.5 of 1.4 in two shares), and
+// Into how many shares the keys of a tile are dealt out.  Few rows: as many workgroups as the chip holds at once, 256 keys at least to
+// each (a third more than that: one token of 32 heads against 115200 slots 110 us, and 99 now).  Many: the busiest CU's number of workgroups bounds the time (360 tiles on 256 CUs: 2 of 1.4, and 1.5 of 1.4 in two shares), and
 // the shares cost their way through memory; one workgroup alone on a CU takes three quarters of the time that two take.  A workgroup's
 // 64 keys of a row and channel take 0.073 ns at the rate of a whole chip's.
-static int64_t shares_of_tiles(int64_t tiles, int tile_rows, int64_t capacity, int64_t rows, int64_t d) {
+static int64_t shares_of_tiles(int64_t tiles, int tile_rows, int held, int64_t capacity, int64_t rows, int64_t d) {
   if (tiles == 0) return 1;
   const int64_t most = std::min<int64_t>(64, std::max<int64_t>(1, capacity / 256));
-  if (tile_rows <= 32) return tiles <= 512 ? std::min<int64_t>(1024 / tiles, most) : 1;
+  if (tile_rows <= 32) return std::max<int64_t>(1, std::min<int64_t>(256 * held / tiles, most));
   int64_t best = 1;
   double least = 0.0;
   for (int64_t n = 1; n <= most && n * tiles <= 4096; ++n) {
@@ -189,14 +189,19 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   const double tiles = (double)(c->B * c->heads) * (double)p->runs * (double)p->tiles_per_run;
   if (tiles >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
   const int64_t t = (int64_t)tiles;
-  p->nsplit = (int)shares_of_tiles(t, p->tile_rows, c->capacity, q->B * q->N * q->heads, q->dim_head);
+  const int groups = cache_groups(c), held = p->tile_rows == 32 ? (groups == 1 ? 3 : 2) : q->dtype == SI_BF16 ? (groups <= 2 ? 4 : 3) : groups == 1 ? 4 : groups == 2 ? 3 : 2;
+  p->nsplit = (int)shares_of_tiles(t, p->tile_rows, held, c->capacity, q->B * q->N * q->heads, q->dim_head);
   p->work = t * p->nsplit;
   p->rows = q->B * q->N * q->heads;
   p->part_bytes = p->nsplit > 1 ? align_up((size_t)(p->rows * p->nsplit * q->dim_head) * 4, 256) : 0;
   p->stat_bytes = p->nsplit > 1 ? align_up((size_t)(p->rows * p->nsplit) * 16, 256) : 0;
   p->row_bytes = weights ? align_up((size_t)p->rows * 8, 256) : 0;
-  p->weight_keys = q->dtype == SI_BF16 && p->group * q->N > 64 ? 256 : 128;
-  p->weight_chunks = (c->capacity + p->weight_keys - 1) / p->weight_keys;
+  // Weights: rows that fit operands are kept, and the keys dealt out like those of the attention (eight tokens of 32 heads, 57600 padded slots, all
+  // of the call: 63 us with 768 workgroups, 65 with 512, 71 with 1024); otherwise keys are kept.
+  p->weight_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 0;
+  const int64_t lists = c->B * c->heads;
+  if (p->weight_rows) p->weight_chunks = std::min<int64_t>(std::max<int64_t>(1, 768 / lists), std::max<int64_t>(1, (c->capacity + 255) / 256));
+  else p->weight_chunks = q->dtype == SI_BF16 ? (c->capacity + 128 * kWeightTiles - 1) / (128 * kWeightTiles) : (c->capacity + 127) / 128;
   if ((double)(c->B * c->heads) * (double)p->weight_chunks >= 4294967296.0 - kGridMost) return SI_ERR_SHAPE;
   return SI_OK;
 }
@@ -223,12 +228,14 @@ static si_status launch_cache_attn(const CacheAttnArgs& a, const CacheWeightArgs
     if (p.nsplit > 1) cache4_join_kernel<T><<<(unsigned)((p.rows + 3) / 4), 256, 0, st>>>(a, (int)p.rows);
     SI_CHECK_LAUNCH();
   }
-  if (w && w->work > 0) {
+  if (w && w->work > 0 && c->capacity > 0) {
     StageScope scope("cache4_weight", st);
     const unsigned grid = grid_of(w->work);
     by_groups(c, [&](auto g) {
-      if (sizeof(T) == 2 && p.weight_keys == 256) cache4_weight_many_kernel<g.value><<<grid, 256, 0, st>>>(*w);
-      else cache4_weight_kernel<T, g.value><<<grid, 256, 0, st>>>(*w);
+      if (p.weight_rows == 16) cache4_weight_few_kernel<T, g.value, 1><<<grid, 256, 0, st>>>(*w);
+      else if (p.weight_rows == 32) cache4_weight_few_kernel<T, g.value, 2><<<grid, 256, 0, st>>>(*w);
+      else if constexpr (sizeof(T) == 4) cache4_weight_rows_kernel<T, g.value><<<grid, 256, 0, st>>>(*w);
+      else cache4_weight_many_kernel<g.value><<<grid, 256, 0, st>>>(*w);
     });
     SI_CHECK_LAUNCH();
   }
