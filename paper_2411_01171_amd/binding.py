@@ -388,7 +388,7 @@ def _call(name: str, stream, tensors, args) -> None:
     else:
         st = _stream_ptr(stream)
     fn = getattr(lib(), name)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():  # torch.cuda.current_device(); torch has been initialised, a tensor is on the GPU
         status = fn(*args, st)
     else:
         with torch.cuda.device(index):
@@ -473,7 +473,14 @@ class Cache4:
                 raise ValueError(f"codes and scales must be contiguous uint8 tensors [B, heads, capacity, {groups}] and [.., {room}]")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = self.tensors
         self.dim_head = dim_head
-        self.struct = _Cache4(*(t.data_ptr() for t in self.tensors), *k_codes.shape[:3], dim_head)
+        self.shape = (*k_codes.shape[:3], dim_head)  # B, heads, capacity, dim_head
+        self.slots = self.shape[:3]
+        self.struct = _Cache4(*(t.data_ptr() for t in self.tensors), *self.shape)
+        index = {t.get_device() for t in self.tensors}
+        self.index = index.pop() if len(index) == 1 else -1  # the GPU that holds all of it
+
+    def get_device(self) -> int:
+        return self.index
 
     @staticmethod
     def row_bytes(dim_head: int) -> Tuple[int, int]:
@@ -489,18 +496,13 @@ class Cache4:
         codes, scales = cls.row_bytes(dim_head)
         return cls(*(torch.empty(B, heads, capacity, n, dtype=torch.uint8, device=device) for n in (codes, scales, codes, scales)), dim_head)
 
-    @property
-    def shape(self) -> Tuple[int, int, int, int]:
-        """B, heads, capacity, dim_head."""
-        return (*self.k_codes.shape[:3], self.dim_head)
-
 
 def _weights(t, cache: Cache4, what: str) -> Optional[int]:
     if t is None:
         return None
     import torch
-    if t.dtype != torch.float32 or tuple(t.shape) != cache.shape[:3] or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous float32 tensor {list(cache.shape[:3])}")
+    if t.dtype != torch.float32 or t.shape != cache.slots or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 tensor {list(cache.slots)}")
     return t.data_ptr()
 
 
@@ -509,14 +511,14 @@ def si_cache4_store(k, v, cache: Cache4, first=None, length=None, weight=None, s
     weight: zeroed at these slots."""
     B = cache.shape[0]
     args = (C.byref(_heads(k)), C.byref(_heads(v)), _lengths(first, B), _lengths(length, B), C.byref(cache.struct), _weights(weight, cache, "weight"))
-    _call("si_cache4_store", stream, (k, v, first, length, weight, *cache.tensors), args)
+    _call("si_cache4_store", stream, (k, v, cache, first, length, weight), args)
 
 
 def si_cache4_load(cache: Cache4, k, v, first=None, length=None, stream=None) -> None:
     """Writes what slots first[b] + n stand for to the tokens of k and v."""
     B = cache.shape[0]
     args = (C.byref(cache.struct), _lengths(first, B), _lengths(length, B), C.byref(_heads(k)), C.byref(_heads(v)))
-    _call("si_cache4_load", stream, (k, v, first, length, *cache.tensors), args)
+    _call("si_cache4_load", stream, (k, v, cache, first, length), args)
 
 
 def si_cache4_attn_workspace_bytes(q, cache: Cache4, run: int = 0, weights: bool = False) -> int:
@@ -531,7 +533,7 @@ def si_cache4_attn_forward(q, cache: Cache4, out, workspace, scale: Optional[flo
     args = (C.byref(_heads(q)), C.byref(cache.struct), q.shape[3] ** -0.5 if scale is None else scale, run, _lengths(q_len, B), _lengths(k_len, B),
             _weights(weight_in, cache, "weight_in"), decay, _weights(weight_out, cache, "weight_out"), C.byref(_heads(out)),
             workspace.data_ptr(), workspace.nbytes)
-    _call("si_cache4_attn_forward", stream, (q, out, workspace, q_len, k_len, weight_in, weight_out, *cache.tensors), args)
+    _call("si_cache4_attn_forward", stream, (q, out, cache, workspace, q_len, k_len, weight_in, weight_out), args)
 
 
 def si_cache4_evict_workspace_bytes(cache: Cache4, keep: int) -> int:
@@ -548,7 +550,7 @@ def si_cache4_evict(cache: Cache4, weight, keep: int, out: Cache4, weight_out, k
         raise ValueError(f"kept must be a contiguous int32 tensor {[B, heads, keep]}")
     args = (C.byref(cache.struct), _lengths(k_len, B), _weights(weight, cache, "weight"), keep, first, last, C.byref(out.struct),
             _weights(weight_out, out, "weight_out"), kept.data_ptr(), _lengths(out_len, B), workspace.data_ptr(), workspace.nbytes)
-    _call("si_cache4_evict", stream, (weight, weight_out, kept, out_len, workspace, k_len, *cache.tensors, *out.tensors), args)
+    _call("si_cache4_evict", stream, (weight, weight_out, cache, out, kept, out_len, workspace, k_len), args)
 
 
 class AttnOptions:
