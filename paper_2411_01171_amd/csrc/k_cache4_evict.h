@@ -36,8 +36,9 @@ __device__ __forceinline__ unsigned weight_key(float x) {
 }
 
 constexpr int kEvictThreads = 1024;
-constexpr int kEvictPer = 16;                                // weights of a thread at a time
-constexpr int kEvictBatch = kEvictThreads * kEvictPer;
+constexpr int kEvictPer = 16;                                // weights of a thread at a time, at most
+constexpr int kEvictPart = kEvictThreads * kEvictPer;         // longer lists are searched by several workgroups
+constexpr unsigned kEvictParts = 16;                         // so many at most
 constexpr int kEvictChunk = kEvictThreads;                   // slots that are counted together; the second kernel's piece
 constexpr int kEvictBins = 2048;                             // digits of 11, 11 and 10 bits
 
@@ -78,8 +79,8 @@ __device__ __forceinline__ EvictSearch evict_digit(EvictShared& sh, EvictSearch 
   int upto = wave_upto(h0 + h1);
   if (lane == kWave - 1) sh.wave_total[wave] = upto;
   __syncthreads();
-#pragma unroll
-  for (int v = 0; v < kEvictThreads / kWave; ++v) upto += v < wave ? sh.wave_total[v] : 0;
+  // the wavefronts before this one, a lane each
+  upto += __builtin_amdgcn_readlane(wave_upto(lane < wave ? sh.wave_total[lane & 15] : 0), 15);
   const int before = upto - h0 - h1;
   if (before < at.left && at.left <= upto) {  // one thread's
     const bool second = before + h0 < at.left;
@@ -90,11 +91,11 @@ __device__ __forceinline__ EvictSearch evict_digit(EvictShared& sh, EvictSearch 
   return sh.found;
 }
 
-// A batch: slots base + 1024 j + t, which of them there are and which weights count, from its first slot on.
+// A batch of up to 16384 slots, base + 1024 j + t: which of them there are and which weights count, from its first slot on.
 struct EvictBatch {
   int there, lo, hi;
   __device__ __forceinline__ EvictBatch(const EvictArgs& a, int n, int64_t base, int64_t end) {
-    auto from_base = [&](int64_t i) { return (int)min(max(i - base, (int64_t)0), (int64_t)kEvictBatch); };
+    auto from_base = [&](int64_t i) { return (int)min(max(i - base, (int64_t)0), (int64_t)kEvictPart); };
     there = from_base(end);
     lo = min(from_base(a.first), there);
     hi = max(lo, min(from_base((int64_t)n - a.last), there));
@@ -104,22 +105,24 @@ struct EvictBatch {
 };
 
 // The weights in their order; 0: no weight that counts.
-__device__ __forceinline__ void evict_load(const EvictArgs& a, const float* w, const EvictBatch& of, int64_t base, unsigned (&key)[kEvictPer]) {
-  float x[kEvictPer];
+template <int PER>
+__device__ __forceinline__ void evict_load(const EvictArgs& a, const float* w, const EvictBatch& of, int64_t base, unsigned (&key)[PER]) {
+  float x[PER];
 #pragma unroll
-  for (int j = 0; j < kEvictPer; ++j) {
+  for (int j = 0; j < PER; ++j) {
     const int i = j * kEvictThreads + (int)threadIdx.x;
     x[j] = 0.f;
     if (of.any(j) && i < of.there) x[j] = w[base + i];
   }
 #pragma unroll
-  for (int j = 0; j < kEvictPer; ++j) key[j] = of.any(j) && of.open(j * kEvictThreads + (int)threadIdx.x) ? weight_key(x[j]) : 0u;
+  for (int j = 0; j < PER; ++j) key[j] = of.any(j) && of.open(j * kEvictThreads + (int)threadIdx.x) ? weight_key(x[j]) : 0u;
 }
 
 // Adds the weights that share the digits found so far to sh.hist, which is zero.
-__device__ __forceinline__ void evict_count(EvictShared& sh, const unsigned (&key)[kEvictPer], const EvictBatch& of, EvictSearch at, int digit) {
+template <int PER>
+__device__ __forceinline__ void evict_count(EvictShared& sh, const unsigned (&key)[PER], const EvictBatch& of, EvictSearch at, int digit) {
 #pragma unroll
-  for (int j = 0; j < kEvictPer; ++j) {
+  for (int j = 0; j < PER; ++j) {
     if (!of.any(j)) continue;
     const bool counts = key[j] != 0u && (digit == 0 || (key[j] ^ at.least) >> evict_shift(digit - 1) == 0u);
     if (counts) atomicAdd(&sh.hist[(key[j] >> evict_shift(digit)) & (digit == 2 ? 1023u : 2047u)], 1);
@@ -127,13 +130,14 @@ __device__ __forceinline__ void evict_count(EvictShared& sh, const unsigned (&ke
 }
 
 // For every 1024 slots from `base` on, those that stay without question and those that equal the threshold.
-__device__ __forceinline__ void evict_counts(const EvictArgs& a, EvictShared& sh, const unsigned (&key)[kEvictPer], const EvictBatch& of, unsigned least, unsigned list,
+template <int PER>
+__device__ __forceinline__ void evict_counts(const EvictArgs& a, EvictShared& sh, const unsigned (&key)[PER], const EvictBatch& of, unsigned least, unsigned list,
                                              int64_t base) {
   const int tid = threadIdx.x;
-  if (tid < 2 * kEvictPer) sh.count[tid / 2][tid % 2] = 0;
+  if (tid < 2 * PER) sh.count[tid / 2][tid % 2] = 0;
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kEvictPer; ++j) {
+  for (int j = 0; j < PER; ++j) {
     if (!of.any(j)) continue;
     const int i = j * kEvictThreads + tid;
     const int above = (int)__popcll(__builtin_amdgcn_ballot_w64(of.open(i) ? key[j] > least : i < of.there));  // of slots that are not open all stay
@@ -144,7 +148,7 @@ __device__ __forceinline__ void evict_counts(const EvictArgs& a, EvictShared& sh
     }
   }
   __syncthreads();
-  if (tid < kEvictPer && of.any(tid)) a.counts[(int64_t)list * a.chunks + (unsigned)(base / kEvictChunk) + tid] = make_int2(sh.count[tid][0], sh.count[tid][1]);
+  if (tid < PER && of.any(tid)) a.counts[(int64_t)list * a.chunks + (unsigned)(base / kEvictChunk) + tid] = make_int2(sh.count[tid][0], sh.count[tid][1]);
   __syncthreads();
 }
 
@@ -161,7 +165,9 @@ __device__ __forceinline__ EvictSearch evict_begin(const EvictArgs& a) {
   return EvictSearch{left > 0 ? 0u : ~0u, left};
 }
 
-// Lists of up to 16384 slots, one workgroup each; the weights stay in registers.  A chain of latencies: 4096 slots.
+// Lists of up to 1024 PER slots, one workgroup each; the weights stay in registers.  A chain of latencies, that of fetching the code among
+// them: the digits are a loop, and short lists have a form of their own.
+template <int PER>
 __global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a) {
   __shared__ EvictShared sh;
   const int tid = threadIdx.x;
@@ -172,14 +178,14 @@ __global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a)
       if (tid == 0) a.least[list] = make_uint2(0u, 0u);
       continue;
     }
-    unsigned key[kEvictPer];
+    unsigned key[PER];
     const EvictBatch of(a, n, 0, n);
     evict_load(a, a.weight + (int64_t)list * a.from.cap, of, 0, key);
     sh.hist[tid] = 0;
     sh.hist[tid + kEvictThreads] = 0;
     EvictSearch at = evict_begin(a);
     if (at.left > 0)
-#pragma unroll
+#pragma unroll 1
       for (int digit = 0; digit < 3; ++digit) {
         __syncthreads();
         evict_count(sh, key, of, at, digit);
@@ -194,8 +200,8 @@ __global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a)
 }
 
 // Longer lists, a workgroup for each of a.parts pieces of one.  STEP 0, 1, 2: the counts of that digit of a piece's weights; 1, 2, 3: before
-// that, the digit before it from all pieces' counts; 3: the counts of every 1024 slots.  A launch per step: 115200 slots of 32 lists in one
-// workgroup each took 98 us.
+// that, the digit before it from all pieces' counts; 3: the counts of every 1024 slots.  A launch per step, 9 to 12 us each for 32 lists
+// of 115200 slots: latencies of memory, and of fetching the code (pieces of 4096 and 8192 slots are slower; a workgroup per list took 98 us).
 template <int STEP>
 __global__ __launch_bounds__(kEvictThreads) void cache4_search_kernel(EvictArgs a) {
   __shared__ EvictShared sh;
@@ -212,7 +218,7 @@ __global__ __launch_bounds__(kEvictThreads) void cache4_search_kernel(EvictArgs 
     unsigned key[kEvictPer];
     const float* w = a.weight + (int64_t)list * a.from.cap;
     EvictBatch of(a, n, begin, end);
-    evict_load(a, w, of, begin, key);  // on its way while the digit is found
+    evict_load(a, w, of, begin, key);      // on its way while the digit is found
     __syncthreads();                       // the piece before has been counted
     if (STEP < 3) {
       sh.hist[tid] = 0;
@@ -223,17 +229,26 @@ __global__ __launch_bounds__(kEvictThreads) void cache4_search_kernel(EvictArgs 
       if (STEP > 1) at = a.search[(STEP % 2) * a.lists + list];
       const int2* counts = reinterpret_cast<const int2*>(a.hist[(STEP + 1) % 2] + (int64_t)list * a.parts * kEvictBins) + (kEvictThreads - 1 - tid);
       int h0 = 0, h1 = 0;
-      for (unsigned p = 0; p < a.parts; ++p) {
-        const int2 v = counts[(int64_t)p * (kEvictBins / 2)];
-        h1 += v.x;
-        h0 += v.y;
+#pragma unroll 1
+      for (unsigned p0 = 0; p0 < a.parts; p0 += 8) {
+        int2 v[8];
+#pragma unroll
+        for (unsigned p = 0; p < 8; ++p)
+          if (p0 + p < a.parts) v[p] = counts[(p0 + p) * (kEvictBins / 2)];
+#pragma unroll
+        for (unsigned p = 0; p < 8; ++p)
+          if (p0 + p < a.parts) {
+            h1 += v[p].x;
+            h0 += v[p].y;
+          }
       }
       at = evict_digit(sh, at, STEP - 1, h0, h1);
       if (part == 0 && tid == 0) a.search[((STEP + 1) % 2) * a.lists + list] = at;
     }
     if (STEP == 3 && part == 0 && tid == 0) a.least[list] = make_uint2(at.least, (unsigned)at.left);
     __syncthreads();
-    for (int64_t base = begin; base < end; base += kEvictBatch) {
+#pragma unroll 1
+    for (int64_t base = begin; base < end; base += kEvictPart) {
       if (base != begin) {
         of = EvictBatch(a, n, base, end);
         evict_load(a, w, of, base, key);

@@ -259,9 +259,9 @@ static si_status plan_evict(const si_cache4* c, int64_t keep, EvictPlan* p) {
   p->count_bytes = align_up((size_t)(p->lists * p->chunks) * sizeof(int2), 256);
   p->least_bytes = align_up((size_t)p->lists * sizeof(uint2), 256);
   // Lists that do not fit a workgroup's registers are cut into up to 16 parts, as long as there are few lists: every part adds up all parts' counts.
-  p->parts = c->capacity <= kEvictBatch ? 0 : std::min<int64_t>(std::min<int64_t>(16, (c->capacity + kEvictBatch - 1) / kEvictBatch), std::max<int64_t>(1, 1024 / p->lists));
-  const int64_t batches = (c->capacity + kEvictBatch - 1) / kEvictBatch;
-  p->part_slots = p->parts ? (batches + p->parts - 1) / p->parts * kEvictBatch : 0;
+  const int64_t batches = (c->capacity + kEvictPart - 1) / kEvictPart;
+  p->parts = c->capacity <= kEvictPart ? 0 : std::min<int64_t>(std::min<int64_t>(kEvictParts, batches), std::max<int64_t>(1, 1024 / p->lists));
+  p->part_slots = p->parts ? (batches + p->parts - 1) / p->parts * kEvictPart : 0;
   p->search_bytes = p->parts ? align_up((size_t)p->lists * 2 * sizeof(EvictSearch), 256) : 0;
   p->hist_bytes = (size_t)(p->lists * p->parts) * kEvictBins * sizeof(int);
   p->bytes = p->count_bytes + p->least_bytes + p->search_bytes + 2 * p->hist_bytes + 256;
@@ -401,7 +401,9 @@ si_status si_cache4_evict(const si_cache4* cache, const int32_t* k_len, const fl
   const hipStream_t st = static_cast<hipStream_t>(stream);
   si::StageScope scope("cache4_evict", st);
   if (p.parts == 0) {
-    si::cache4_pick_kernel<<<(unsigned)std::min<int64_t>(p.lists, si::kGridMost), si::kEvictThreads, 0, st>>>(a);
+    const unsigned grid = (unsigned)std::min<int64_t>(p.lists, si::kGridMost);
+    if (cache->capacity <= 4 * si::kEvictThreads) si::cache4_pick_kernel<4><<<grid, si::kEvictThreads, 0, st>>>(a);
+    else si::cache4_pick_kernel<si::kEvictPer><<<grid, si::kEvictThreads, 0, st>>>(a);
   } else {
     const unsigned grid = (unsigned)std::min<int64_t>(p.lists * p.parts, si::kGridMost);
     si::cache4_search_kernel<0><<<grid, si::kEvictThreads, 0, st>>>(a);
