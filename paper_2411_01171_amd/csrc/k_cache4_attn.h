@@ -90,26 +90,27 @@ __device__ __forceinline__ void bf16_parts(float lo, float hi, unsigned (&out)[T
   }
 }
 
-// Eight query channels as column operands.
+// Eight float32 channels as operands.
+template <int TERMS>
+__device__ __forceinline__ void query_parts(const f32x4_t& x, const f32x4_t& y, u32x4_t (&out)[TERMS]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned w[TERMS];
+    const float lo = i < 2 ? x[2 * i] : y[2 * i - 4], hi = i < 2 ? x[2 * i + 1] : y[2 * i - 3];
+    bf16_parts<TERMS>(lo, hi, w);
+    // an infinity's rest would be a NaN: it has none
+    if (__builtin_isinf(lo) || __builtin_isinf(hi))
+#pragma unroll
+      for (int t = 1; t < TERMS; ++t) w[t] &= (__builtin_isinf(lo) ? 0xFFFF0000u : ~0u) & (__builtin_isinf(hi) ? 0x0000FFFFu : ~0u);
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) out[t][i] = w[t];
+  }
+}
+// The same of a query's row in either type.
 template <typename T, int TERMS>
 __device__ __forceinline__ void query_parts(const T* p, u32x4_t (&out)[TERMS]) {
-  if constexpr (sizeof(T) == 2) {
-    out[0] = *reinterpret_cast<const u32x4_t*>(p);
-  } else {
-    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p), y = *reinterpret_cast<const f32x4_t*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      unsigned w[TERMS];
-      const float lo = i < 2 ? x[2 * i] : y[2 * i - 4], hi = i < 2 ? x[2 * i + 1] : y[2 * i - 3];
-      bf16_parts<TERMS>(lo, hi, w);
-      // an infinity's rest would be a NaN: it has none
-      if (__builtin_isinf(lo) || __builtin_isinf(hi))
-#pragma unroll
-        for (int t = 1; t < TERMS; ++t) w[t] &= (__builtin_isinf(lo) ? 0xFFFF0000u : ~0u) & (__builtin_isinf(hi) ? 0x0000FFFFu : ~0u);
-#pragma unroll
-      for (int t = 0; t < TERMS; ++t) out[t][i] = w[t];
-    }
-  }
+  if constexpr (sizeof(T) == 2) out[0] = *reinterpret_cast<const u32x4_t*>(p);
+  else query_parts(*reinterpret_cast<const f32x4_t*>(p), *reinterpret_cast<const f32x4_t*>(p + 4), out);
 }
 
 // The codes of two tiles of 16 keys as the lanes of a row operand hold them: lane (r, g) channels 8 G g .. 8 G g + 8 G - 1 of keys
@@ -754,7 +755,7 @@ __global__ __launch_bounds__(256) void cache4_join_kernel(CacheAttnArgs a, int r
   else *reinterpret_cast<f32x4_t*>(dst) = o;
 }
 
-constexpr int kWeightTiles = 2;  // of 32 keys, that a wavefront of the kernel for many rows keeps
+constexpr int kWeightTiles = 2;  // of 32 keys, that a wavefront of the kernel for many rows keeps (1, 3 and 4 are up to 4 % slower)
 
 struct CacheWeightArgs {
   const void* q;
@@ -762,7 +763,7 @@ struct CacheWeightArgs {
   Cache4View c;
   const int *q_len, *k_len;
   int Nq, group, d, run;
-  int chunks;                // pieces of a head's keys: of 128, of 128 kWeightTiles, or shares
+  int chunks;                // pieces of a head's keys: of 128 kWeightTiles, or shares
   unsigned work;             // B * heads * chunks
   float scale_log2, decay;
   const float2* row_stat;
@@ -867,106 +868,42 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (NT == 1 ? 4 : 3) : 2) void c
   }
 }
 
-// The same for more rows than that in float32: a wavefront keeps 32 keys and walks the rows.
+// The same for more rows.  A wavefront keeps 32 KT keys as bf16 column operands and walks the rows in tiles of 32 that the
+// workgroup's four share in LDS (direct global->LDS loads, one tile ahead), with their statistics.  A lane holds one key of every 32, so that a
+// sum over the rows is one register.  Bound by the vector ALUs: an fma, an exponential and an fma for every score, beside 2 G
+// matrix instructions of 32 clocks for 16 of a lane's.  A row's address and statistics are found by steps from tile to tile, without a division.
 template <typename T, int G>
-__global__ __launch_bounds__(256) void cache4_weight_rows_kernel(CacheWeightArgs a) {
-  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
-  constexpr int SB = cache4_scale_bytes(G);
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int r = lane % 16, g = lane / 16;
-  const unsigned part = (a.work + 7) / 8, part_end = min(a.work, (blockIdx.x % 8 + 1) * part);
-  for (unsigned work = blockIdx.x % 8 * part + blockIdx.x / 8; work < part_end; work += gridDim.x / 8) {
-    const unsigned bh = work / (unsigned)a.chunks;
-    const int b = (int)(bh / (unsigned)a.c.heads), hk = (int)(bh % (unsigned)a.c.heads);
-    const int q_len = a.q_len ? min(max(a.q_len[b], 0), a.Nq) : a.Nq, k_len = a.k_len ? min(max(a.k_len[b], 0), a.c.cap) : a.c.cap;
-    const int64_t key64 = (int64_t)(work % (unsigned)a.chunks) * 128 + wave * 32;
-    if (key64 >= k_len) continue;
-    const int key0 = (int)key64;
-    const int64_t head = ((int64_t)b * a.c.heads + hk) * a.c.cap;
-    KeyCodes<G> k;
-    k.load(a.c.kc + head * (16 * G), a.c.ks + head * SB, key0, k_len, r, g);
-    bf16x8_t kf[2][G];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < G; ++i) kf[u][i] = __builtin_bit_cast(bf16x8_t, k.operand(u, i, g));
-    f32x4_t sum[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
-    const int64_t rows = (int64_t)q_len * a.group;
-    for (int64_t rho0 = 0; rho0 < rows; rho0 += 16) {
-      const int64_t rho = min(rho0 + r, rows - 1);
-      const int n = (int)(rho / a.group), h = hk * a.group + (int)(rho % a.group);
-      const int seen = CacheTile::cache_seen(a.run, n, q_len, k_len);
-      float2 stat = a.row_stat[((int64_t)b * a.Nq + n) * (a.c.heads * a.group) + h];
-      if (rho0 + r >= rows) stat = make_float2(INFINITY, 0.f);  // no row: 2^-inf
-      const T* row = static_cast<const T*>(a.q) + b * a.qb + (int64_t)n * a.qn + (int64_t)h * a.qh;
-      f32x4_t sc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-      for (int i = 0; i < G; ++i) {
-        const int ch = 8 * (G * g + i);
-        u32x4_t q[TERMS];
-#pragma unroll
-        for (int x = 0; x < TERMS; ++x) q[x] = u32x4_t{0, 0, 0, 0};
-        if (ch < a.d) query_parts<T, TERMS>(row + ch, q);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int x = TERMS - 1; x >= 0; --x)
-            sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u][i], __builtin_bit_cast(bf16x8_t, q[x]), sc[u], 0, 0, 0);
-      }
-      const int lim = rho0 + r >= rows ? 0 : seen - key0 - 4 * g;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][j], a.scale_log2, -stat.x)) * stat.y;
-          sum[u][j] += 16 * u + j < lim ? p : 0.f;
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int step = 1; step < 16; step <<= 1) sum[u][j] += __shfl_xor(sum[u][j], step, kWave);
-      // lane (r, g) holds keys 4 g + j of the tile: lanes r < 4 write them
-      const int key = key0 + 16 * u + 4 * g + r;
-      const float mine = r == 0 ? sum[u][0] : r == 1 ? sum[u][1] : r == 2 ? sum[u][2] : sum[u][3];
-      if (r < 4 && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + mine;
-    }
-  }
-}
-
-// The same for more rows in bf16.  A wavefront keeps 64 keys as bf16 operands, a workgroup 256, and walks the rows in tiles of 32
-// that all four share in LDS (direct global->LDS loads, one tile ahead).  Bound by the vector ALUs: an fma, an exponential and an fma
-// for every score, beside 2 G matrix instructions of 32 clocks for 32 of them.
-// A row's address and statistics are found by steps from tile to tile, without a division.
-template <int G>
-__global__ __launch_bounds__(256, G <= 2 ? 3 : 2) void cache4_weight_many_kernel(CacheWeightArgs a) {
-  using Geo = SparseGeo<bf16, 2 * G, 4>;
-  constexpr int KT = kWeightTiles;
+__global__ __launch_bounds__(256, sizeof(T) == 2 && G <= 2 ? 3 : 2) void cache4_weight_many_kernel(CacheWeightArgs a) {
+  using Geo = SparseGeo<T, 2 * G, 4>;
+  constexpr int KT = kWeightTiles, TERMS = sizeof(T) == 2 ? 1 : 3;
   constexpr int ROW = Geo::ROW, TILE = 32 * ROW, KS = 2 * G, SB = cache4_scale_bytes(G);
   constexpr int LOADS = TILE / 4096 > 0 ? TILE / 4096 : 1;  // of a wavefront and tile, 1 KiB each; tiles of 2 KiB leave two wavefronts without
   __shared__ __align__(1024) u32x4_t ring[2 * TILE / 16];
+  __shared__ __align__(16) float maxima[2][32], factors[2][32];
+  __shared__ __align__(16) int ends[2][32];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 32, g = lane / 32, heads = a.c.heads * a.group;
-  const unsigned qat = lds0 + r * ROW + (g ^ Geo::swizzle(r)) * 16;  // piece 2 s + g: ^ 32 s
+  // piece 2 s + g (float32: pieces 4 s + 2 g and one more) of row r: ^ 32 s (^ 64 s, and ^ 16)
+  const unsigned qat = lds0 + r * ROW + ((sizeof(T) == 2 ? g : 2 * g) ^ Geo::swizzle(r)) * 16;
   const int step_n = 32 / a.group, step_sub = 32 % a.group;          // from a tile to the next
   // Row rho of a key head, as a token and one of its query heads, and an offset that grows with both.
   struct Row {
-    int rho, sub;
+    int rho, n, sub;
     int64_t at;
     __device__ __forceinline__ Row(int rho_, int group, int64_t per_token, int64_t per_head) : rho(rho_) {
-      const int n = group > 1 ? rho / group : rho;
+      n = group > 1 ? rho / group : rho;
       sub = rho - n * group;
       at = n * per_token + sub * per_head;
     }
-    __device__ __forceinline__ void step(int group, int n, int s, int64_t per_token, int64_t per_head) {
+    __device__ __forceinline__ void step(int group, int dn, int s, int64_t per_token, int64_t per_head) {
       rho += 32;
+      n += dn;
       sub += s;
-      at += n * per_token + s * per_head;
+      at += dn * per_token + s * per_head;
       if (sub >= group) {
         sub -= group;
+        ++n;
         at += per_token - group * per_head;
       }
     }
@@ -991,11 +928,9 @@ __global__ __launch_bounds__(256, G <= 2 ? 3 : 2) void cache4_weight_many_kernel
       for (int s = 0; s < KS; ++s)
         kf[u][s] = cache4_bf16x8(*reinterpret_cast<const unsigned*>(codes + (16 * s + 8 * g) / 2), __uint_as_float((unsigned)a.c.ks[key * SB + s / 2] << 23));
     }
-    f32x16_t sum[KT];
+    float sum[KT];
 #pragma unroll
-    for (int u = 0; u < KT; ++u)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sum[u][e] = 0.f;
+    for (int u = 0; u < KT; ++u) sum[u] = 0.f;
 
     // ---- rows: q_len tokens times `group` heads; the first that see one of these keys
     const int rows = q_len * a.group;
@@ -1007,40 +942,73 @@ __global__ __launch_bounds__(256, G <= 2 ? 3 : 2) void cache4_weight_many_kernel
     }
     const int tiles = rows > begin ? (rows - begin + 31) / 32 : 0;
     // what a wavefront's loads bring: rows of 16-byte pieces, by neighbouring lanes
-    const bf16* q0 = static_cast<const bf16*>(a.q) + b * a.qb + (int64_t)hk * a.group * a.qh;
+    const T* q0 = static_cast<const T*>(a.q) + b * a.qb + (int64_t)hk * a.group * a.qh;
     auto load_row = [&](int l) { return (wave + 4 * l) * (64 / Geo::PR) + lane / Geo::PR; };
     auto load_piece = [&](int l) {
       const int at = (lane % Geo::PR) ^ Geo::swizzle(load_row(l));
-      return at * 8 < a.d ? at * 8 : 0;
+      return at * Geo::VEC < a.d ? at * Geo::VEC : 0;
     };
-    Row of[2] = {Row(begin + load_row(0), a.group, a.qn, a.qh), Row(begin + load_row(LOADS - 1), a.group, a.qn, a.qh)};
-    Row mine(begin + r, a.group, heads, 1);  // whose statistics this lane holds
+    Row of(begin + load_row(0), a.group, a.qn, a.qh);
+    Row mine(begin + r, a.group, heads, 1);  // whose statistics the first wavefront's lanes bring
     const float2* stat0 = a.row_stat + (int64_t)b * a.Nq * heads + hk * a.group;
-    float2 next_stat;
+    float2 stat = make_float2(INFINITY, 0.f);
+    int end = 0;
     auto issue = [&](unsigned slot) {
-      next_stat = stat0[mine.rho < rows ? mine.at : 0];
-      if (mine.rho >= rows) next_stat = make_float2(INFINITY, 0.f);  // no row: 2^-inf
-      mine.step(a.group, step_n, step_sub, heads, 1);
+      if (wave == 0) {
+        stat = stat0[mine.rho < rows ? mine.at : 0];
+        end = CacheTile::cache_seen(a.run, mine.n, q_len, k_len);
+        if (mine.rho >= rows) {  // no row: 2^-inf
+          stat = make_float2(INFINITY, 0.f);
+          end = 0;
+        }
+        mine.step(a.group, step_n, step_sub, heads, 1);
+      }
 #pragma unroll
       for (int l = 0; l < LOADS; ++l) {
+        const Row row = l == 0 ? of : Row(of.rho + load_row(l) - load_row(0), a.group, a.qn, a.qh);
         if (TILE >= 4096 || wave * 1024 < TILE)
-          load_to_lds(q0 + (of[l].rho < rows ? of[l].at : 0) + load_piece(l), lds0 + slot * TILE + (wave + 4 * l) * 1024);
-        of[l].step(a.group, step_n, step_sub, a.qn, a.qh);
+          load_to_lds(q0 + (row.rho < rows ? row.at : 0) + load_piece(l), lds0 + slot * TILE + (wave + 4 * l) * 1024);
+      }
+      of.step(a.group, step_n, step_sub, a.qn, a.qh);
+    };
+    auto put_stat = [&](unsigned slot) {
+      if (wave == 0 && g == 0) {
+        maxima[slot][r] = stat.x;
+        factors[slot][r] = stat.y;
+        ends[slot][r] = end;
       }
     };
     __syncthreads();  // nobody reads the ring of the piece before
-    if (tiles > 0) issue(0);
+    if (tiles > 0) {
+      issue(0);
+      put_stat(0);
+    }
     for (int i = 0; i < tiles; ++i) {
       const int slot = i & 1;
-      const float2 stat = next_stat;
       __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // tile i
       __syncthreads();
       if (i + 1 < tiles) issue(slot ^ 1);
-      u32x4_t qf[KS];
+      u32x4_t qf[KS][TERMS];
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        qf[s] = lds_read<u32x4_t>((qat ^ (32 * s)) + slot * TILE);
-        if (s >= 2 * G - 2 && 16 * s + 8 * g >= a.d) qf[s] = u32x4_t{0, 0, 0, 0};  // d is more than 32 (G - 1)
+        if constexpr (TERMS == 1) {
+          qf[s][0] = lds_read<u32x4_t>((qat ^ (32 * s)) + slot * TILE);
+        } else {
+          query_parts(lds_read<f32x4_t>((qat ^ (64 * s)) + slot * TILE), lds_read<f32x4_t>((qat ^ (64 * s) ^ 16) + slot * TILE), qf[s]);
+        }
+      }
+      if (a.d < 32 * G) {  // channels past the head
+#pragma unroll
+        for (int s = KS - 2; s < KS; ++s)
+          if (16 * s + 8 * g >= a.d)
+#pragma unroll
+            for (int x = 0; x < TERMS; ++x) qf[s][x] = u32x4_t{0, 0, 0, 0};
+      }
+      f32x4_t top[4], factor[4];  // of rows 8 p + 4 g + j, as registers 4 p + j of the scores lie
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        top[p] = *reinterpret_cast<const f32x4_t*>(&maxima[slot][8 * p + 4 * g]);
+        factor[p] = *reinterpret_cast<const f32x4_t*>(&factors[slot][8 * p + 4 * g]);
       }
       f32x16_t sc[KT];
 #pragma unroll
@@ -1050,43 +1018,35 @@ __global__ __launch_bounds__(256, G <= 2 ? 3 : 2) void cache4_weight_many_kernel
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int u = 0; u < KT; ++u)
-          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[u][s]), __builtin_bit_cast(bf16x8_t, qf[s]), sc[u], 0, 0, 0);
+        for (int x = TERMS - 1; x >= 0; --x)  // the smallest part first
+#pragma unroll
+          for (int u = 0; u < KT; ++u)
+            sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, qf[s][x]), __builtin_bit_cast(bf16x8_t, kf[u][s]), sc[u], 0, 0, 0);
 #pragma unroll
       for (int u = 0; u < KT; ++u)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[u][e] = __builtin_amdgcn_exp2f(fmaf(sc[u][e], a.scale_log2, -stat.x));
-      // is there a last row among these, or one, then the first, that does not see all of the workgroup's keys
-      const int rho0 = begin + 32 * i;
-      if (rho0 + 32 > rows || (a.run && CacheTile::cache_seen(a.run, rho0 / a.group, q_len, k_len) < last_key)) {
-        const int lim = rho0 + r < rows ? CacheTile::cache_seen(a.run, (rho0 + r) / a.group, q_len, k_len) - key0 - 4 * g : 0;
+        for (int e = 0; e < 16; ++e) sc[u][e] = __builtin_amdgcn_exp2f(fmaf(sc[u][e], a.scale_log2, -top[e / 4][e % 4]));
+      // Is one of these rows behind the last, or is there one, then the first, that does not see all of the workgroup's keys?
+      if (begin + 32 * i + 32 > rows || (a.run && __builtin_amdgcn_readfirstlane(ends[slot][0]) < last_key)) {
 #pragma unroll
-        for (int u = 0; u < KT; ++u)
+        for (int e = 0; e < 16; ++e) {
+          const int lim = ends[slot][8 * (e / 4) + 4 * g + e % 4] - key0 - r;
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (32 * u + 8 * (e / 4) + e % 4 >= lim) sc[u][e] = 0.f;
-      }
-#pragma unroll
-      for (int u = 0; u < KT; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sum[u][e] = fmaf(sc[u][e], stat.y, sum[u][e]);
-    }
-    // Register e of tile u, lanes of half g: key 32 u + 8 (e / 4) + 4 g + e % 4, to be summed over the half's 32 rows.  At every step a lane
-    // hands over one half of its keys and keeps the other; lanes 2 e and 2 e + 1 end with key e.
-#pragma unroll
-    for (int u = 0; u < KT; ++u) {
-#pragma unroll
-      for (int n = 8; n >= 1; n /= 2) {
-        const bool upper = (r & (2 * n)) != 0;
-#pragma unroll
-        for (int e = 0; e < n; ++e) {
-          const float keep = upper ? sum[u][e + n] : sum[u][e], give = upper ? sum[u][e] : sum[u][e + n];
-          sum[u][e] = keep + __shfl_xor(give, 2 * n, kWave);
+          for (int u = 0; u < KT; ++u)
+            if (32 * u >= lim) sc[u][e] = 0.f;
         }
       }
-      const float total = sum[u][0] + __shfl_xor(sum[u][0], 1, kWave);
-      const int e = r / 2, key = key0 + 32 * u + 8 * (e / 4) + 4 * g + e % 4;
-      if (r % 2 == 0 && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + total;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int u = 0; u < KT; ++u) sum[u] = fmaf(sc[u][e], factor[e / 4][e % 4], sum[u]);
+      if (i + 1 < tiles) put_stat(slot ^ 1);
+    }
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+      const float total = sum[u] + __shfl_xor(sum[u], 32, kWave);
+      const int key = key0 + 32 * u + r;
+      if (g == 0 && key < k_len) a.out[head + key] = (a.in ? a.decay * a.in[head + key] : 0.f) + total;
     }
   }
 }

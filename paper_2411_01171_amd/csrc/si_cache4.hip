@@ -201,7 +201,7 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   p->weight_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 0;
   const int64_t lists = c->B * c->heads;
   if (p->weight_rows) p->weight_chunks = std::min<int64_t>(std::max<int64_t>(1, 768 / lists), std::max<int64_t>(1, (c->capacity + 255) / 256));
-  else p->weight_chunks = q->dtype == SI_BF16 ? (c->capacity + 128 * kWeightTiles - 1) / (128 * kWeightTiles) : (c->capacity + 127) / 128;
+  else p->weight_chunks = (c->capacity + 128 * kWeightTiles - 1) / (128 * kWeightTiles);
   if ((double)(c->B * c->heads) * (double)p->weight_chunks >= 4294967296.0 - kGridMost) return SI_ERR_SHAPE;
   return SI_OK;
 }
@@ -234,8 +234,7 @@ static si_status launch_cache_attn(const CacheAttnArgs& a, const CacheWeightArgs
     by_groups(c, [&](auto g) {
       if (p.weight_rows == 16) cache4_weight_few_kernel<T, g.value, 1><<<grid, 256, 0, st>>>(*w);
       else if (p.weight_rows == 32) cache4_weight_few_kernel<T, g.value, 2><<<grid, 256, 0, st>>>(*w);
-      else if constexpr (sizeof(T) == 4) cache4_weight_rows_kernel<T, g.value><<<grid, 256, 0, st>>>(*w);
-      else cache4_weight_many_kernel<g.value><<<grid, 256, 0, st>>>(*w);
+      else cache4_weight_many_kernel<T, g.value><<<grid, 256, 0, st>>>(*w);
     });
     SI_CHECK_LAUNCH();
   }
