@@ -492,9 +492,9 @@ si_status si_cache4_load(const si_cache4* cache, const int32_t* first, const int
  * workspace: device, 256-byte aligned, contents ignored; calls that overlap in time
  * must not share one.  (q->heads / cache->heads) * N is below 2^31 - 2^20, and so are
  * the row tiles (of 16 rows and more) of all key heads (SI_ERR_SHAPE).
- * si_cache4_attn_workspace_bytes: weights != 0 where weight_out will be given; 0 if
- * the arguments are invalid.  Host-only. */
-size_t si_cache4_attn_workspace_bytes(const si_heads* q, const si_cache4* cache, int64_t run, int32_t weights);
+ * si_cache4_attn_workspace_bytes: for every run; weights != 0 where weight_out will
+ * be given; 0 if the arguments are invalid.  Host-only. */
+size_t si_cache4_attn_workspace_bytes(const si_heads* q, const si_cache4* cache, int32_t weights);
 si_status si_cache4_attn_forward(const si_heads* q, const si_cache4* cache, float scale, int64_t run, const int32_t* q_len,
                                  const int32_t* k_len, const float* weight_in, float decay, float* weight_out, si_heads* out,
                                  void* workspace, size_t workspace_bytes, void* stream);

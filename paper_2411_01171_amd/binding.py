@@ -137,7 +137,7 @@ def lib() -> C.CDLL:
     L.si_cache4_load.restype = i32
     L.si_cache4_load.argtypes = [pc, vp, vp, ph, ph, vp]
     L.si_cache4_attn_workspace_bytes.restype = sz
-    L.si_cache4_attn_workspace_bytes.argtypes = [ph, pc, i64, i32]
+    L.si_cache4_attn_workspace_bytes.argtypes = [ph, pc, i32]
     L.si_cache4_attn_forward.restype = i32
     L.si_cache4_attn_forward.argtypes = [ph, pc, C.c_float, i64, vp, vp, vp, C.c_float, vp, ph, vp, sz, vp]
     L.si_cache4_evict_workspace_bytes.restype = sz
@@ -521,8 +521,8 @@ def si_cache4_load(cache: Cache4, k, v, first=None, length=None, stream=None) ->
     _call("si_cache4_load", stream, (k, v, cache, first, length), args)
 
 
-def si_cache4_attn_workspace_bytes(q, cache: Cache4, run: int = 0, weights: bool = False) -> int:
-    return int(lib().si_cache4_attn_workspace_bytes(C.byref(_heads(q)), C.byref(cache.struct), run, int(bool(weights))))
+def si_cache4_attn_workspace_bytes(q, cache: Cache4, weights: bool = False) -> int:
+    return int(lib().si_cache4_attn_workspace_bytes(C.byref(_heads(q)), C.byref(cache.struct), int(bool(weights))))
 
 
 def si_cache4_attn_forward(q, cache: Cache4, out, workspace, scale: Optional[float] = None, q_len=None, k_len=None, run: int = 0,

@@ -186,12 +186,15 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   p->run_len = own ? run : std::max<int64_t>(q->N, 1);
   p->runs = q->N == 0 ? 0 : (q->N + p->run_len - 1) / p->run_len;
   p->tiles_per_run = (p->group * p->run_len + p->tile_rows - 1) / p->tile_rows;
-  const double tiles = (double)(c->B * c->heads) * (double)p->runs * (double)p->tiles_per_run;
+  const int64_t lists = c->B * c->heads;
+  const double tiles = (double)lists * (double)p->runs * (double)p->tiles_per_run;
   if (tiles >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
-  const int64_t t = (int64_t)tiles;
+  // The shares, and with them the workspace, do not depend on the runs.
+  const int64_t whole = q->N == 0 ? 0 : lists * ((rows + p->tile_rows - 1) / p->tile_rows);
   const int groups = cache_groups(c), held = p->tile_rows == 32 ? (groups == 1 ? 3 : 2) : q->dtype == SI_BF16 ? (groups <= 2 ? 4 : 3) : groups == 1 ? 4 : groups == 2 ? 3 : 2;
-  p->nsplit = (int)shares_of_tiles(t, p->tile_rows, held, c->capacity, q->B * q->N * q->heads, q->dim_head);
-  p->work = t * p->nsplit;
+  p->nsplit = (int)shares_of_tiles(whole, p->tile_rows, held, c->capacity, q->B * q->N * q->heads, q->dim_head);
+  if (tiles * p->nsplit >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
+  p->work = (int64_t)tiles * p->nsplit;
   p->rows = q->B * q->N * q->heads;
   p->part_bytes = p->nsplit > 1 ? align_up((size_t)(p->rows * p->nsplit * q->dim_head) * 4, 256) : 0;
   p->stat_bytes = p->nsplit > 1 ? align_up((size_t)(p->rows * p->nsplit) * 16, 256) : 0;
@@ -199,7 +202,6 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   // Weights: rows that fit operands are kept, and the keys dealt out like those of the attention (eight tokens of 32 heads, 57600 padded slots, all
   // of the call: 63 us with 768 workgroups, 65 with 512, 71 with 1024); otherwise keys are kept.
   p->weight_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 0;
-  const int64_t lists = c->B * c->heads;
   if (p->weight_rows) p->weight_chunks = std::min<int64_t>(std::max<int64_t>(1, 768 / lists), std::max<int64_t>(1, (c->capacity + 255) / 256));
   else p->weight_chunks = (c->capacity + 128 * kWeightTiles - 1) / (128 * kWeightTiles);
   if ((double)(c->B * c->heads) * (double)p->weight_chunks >= 4294967296.0 - kGridMost) return SI_ERR_SHAPE;
@@ -288,9 +290,9 @@ si_status si_cache4_load(const si_cache4* cache, const int32_t* first, const int
   return si::enqueue_copy(k, v, cache, first, length, nullptr, true, chunks, static_cast<hipStream_t>(stream));
 }
 
-size_t si_cache4_attn_workspace_bytes(const si_heads* q, const si_cache4* cache, int64_t run, int32_t weights) {
+size_t si_cache4_attn_workspace_bytes(const si_heads* q, const si_cache4* cache, int32_t weights) {
   si::CachePlan p;
-  return si::plan_cache_attn(q, cache, run, weights != 0, &p) == SI_OK ? p.bytes() : 0;
+  return si::plan_cache_attn(q, cache, 0, weights != 0, &p) == SI_OK ? p.bytes() : 0;
 }
 
 si_status si_cache4_attn_forward(const si_heads* q, const si_cache4* cache, float scale, int64_t run, const int32_t* q_len,

@@ -77,7 +77,7 @@ def test_sizes_of_the_cache(bad):
     assert load(k=heads(**like), v=heads(FAR, **like), c=cache(**bad)) == SHAPE
     assert attn(q=heads(**like), out=heads(FAR, **like), c=cache(**bad)) == SHAPE
     assert evict(c=cache(**bad)) == SHAPE
-    assert si.lib().si_cache4_attn_workspace_bytes(by(heads(**like)), by(cache(**bad)), 0, 0) == 0
+    assert si.lib().si_cache4_attn_workspace_bytes(by(heads(**like)), by(cache(**bad)), 0) == 0
     assert si.lib().si_cache4_evict_workspace_bytes(by(cache(**bad)), 10) == 0
 
 
@@ -118,7 +118,7 @@ def test_arguments():
 def test_workspaces():
     L = si.lib()
     one, long = heads(N=1, H=32, Bn=1, d=128), cache(cap=100000, H=8, Bn=1, d=128)
-    plain, weights = (L.si_cache4_attn_workspace_bytes(by(one), by(long), 0, w) for w in (0, 1))
+    plain, weights = (L.si_cache4_attn_workspace_bytes(by(one), by(long), w) for w in (0, 1))
     assert weights > plain > 1 << 16                                             # the shares of a token that is dealt out
     out = heads(FAR, N=1, H=32, Bn=1, d=128)
     assert attn(q=one, c=long, out=out, nbytes=plain - 1) == WORKSPACE

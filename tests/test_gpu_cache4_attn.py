@@ -15,7 +15,7 @@ pytestmark = pytest.mark.gpu
 
 
 def _forward(q, cache, out, run=0, stream=None, **kw):
-    n = si.si_cache4_attn_workspace_bytes(q, cache, run, weights=kw.get("weight_out") is not None)
+    n = si.si_cache4_attn_workspace_bytes(q, cache, weights=kw.get("weight_out") is not None)
     assert n > 0
     buf, ws = guarded(n)
     si.si_cache4_attn_forward(q, cache, out, ws, run=run, stream=stream, **kw)
@@ -245,7 +245,7 @@ def test_same_bits_every_time_on_any_stream_and_in_a_graph(N):
     rng = np.random.default_rng(6)
     cache, _ = device_cache(random_cache(rng, 2, 2, 9000, 64), 64)
     q = torch.randn(2, N, 8, 64, device="cuda", dtype=torch.bfloat16)
-    ws = torch.empty(si.si_cache4_attn_workspace_bytes(q, cache, 0, True), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(si.si_cache4_attn_workspace_bytes(q, cache, True), dtype=torch.uint8, device="cuda")
     k_len = lengths([9000, 777])
     ref, out = torch.empty_like(q), torch.empty_like(q)
     w_ref, w = torch.zeros(2, 2, 9000, device="cuda"), torch.zeros(2, 2, 9000, device="cuda")

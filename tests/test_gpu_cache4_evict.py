@@ -149,7 +149,7 @@ def test_a_stream_of_frames(dtype):
         n_dev.add_(frame)
         out = torch.empty(B, frame, Hq, d, device="cuda", dtype=dq.dtype)
         if ws_attn is None:
-            ws_attn = torch.empty(si.si_cache4_attn_workspace_bytes(dq, cache, 0, True), dtype=torch.uint8, device="cuda")
+            ws_attn = torch.empty(si.si_cache4_attn_workspace_bytes(dq, cache, True), dtype=torch.uint8, device="cuda")
             ws_evict = torch.empty(si.si_cache4_evict_workspace_bytes(cache, keep), dtype=torch.uint8, device="cuda")
         si.si_cache4_attn_forward(dq, cache, out, ws_attn, k_len=n_dev, weight_in=weight, weight_out=weight, decay=0.5)
         for b in range(B):
