@@ -431,7 +431,8 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
  * shorter; G = ceil(dim_head / 32)): channel c of a group as an e2m1 code -- 0, 0.5,
  * 1, 1.5, 2, 3, 4, 6 for 0 .. 7, bit 3 the sign -- in the low (c even) or high half
  * of byte c / 2, and one byte s for the group; the value is code * 2^(s - 127), and
- * NaN where s is 255.  Device arrays
+ * NaN where s is 255 (other bytes than 2 .. 252 and 255 are not written, and not
+ * allowed).  Device arrays
  *   codes   [B][heads][capacity][16 G]
  *   scales  [B][heads][capacity][S], S = 1, 2, 4, 4 for G = 1 .. 4
  * each for keys and for values, 16-byte aligned, contiguous: 16 G + S bytes for a

@@ -162,8 +162,12 @@ __device__ __forceinline__ void note_nan(int* bad_key, int group, int key, u32x4
   scale = 127u;
 }
 
-// Rows of up to 32 of a tile: four wavefronts that each take every fourth step of 32 keys.
+// Rows of up to 32 of a tile: four wavefronts that each take every fourth step of 32 keys, on their own until the end.
 // T: of queries and outputs.  G: groups of 32 channels of a head.  NT: columns of rows, 16 each.
+// One token of 32 heads against 115200 slots of 8 heads of 128, four batch entries: 502 MB in 93 us, 5.4 TB/s, bound by HBM (with
+// registers spilled to scratch, whose reloads wait for every load in flight, 197 us).  Eight such tokens, 32 rows, 57600 slots and fewer, two batch
+// entries: 116 MB in 36 us: a step's chain of latencies on two wavefronts per SIMD.  float32, 4050 rows of 8 heads of 80 over
+// 14175 slots: 415 us, 329 TFLOP/s of the operation's own, 990 with the three parts; the matrix cores 47 % busy, the vector ALUs 59 %.
 template <typename T, int G, int NT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 2) void cache4_attn_few_kernel(CacheAttnArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
@@ -442,6 +446,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
 // fetched into registers one stage ahead, a quarter of a key's and of a value's row to a thread, and become bf16 in LDS while
 // the stage before is multiplied.
 // W: the sums of the unrounded weights are wanted too.
+// 9216 tokens of 5 heads of 64 over 64512 slots, two batch entries: 1558 us, 977 TFLOP/s; matrix cores 40 % and vector ALUs 57 % of the cycles.
+// Power bounds it: with wavefronts of 32 rows at twice the number (four per SIMD), with keys read a piece ahead, without the
+// scheduling barriers it takes 1575 to 1650, with products and exponentials of neighbouring pieces interleaved instruction by
+// instruction 1960.  Heads of 96 and 128: 850 and 800 to 860 TFLOP/s.
 template <int G, int CT, bool W>
 __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_many_kernel(CacheAttnArgs a) {
   using Geo = SparseGeo<bf16, 2 * G, 4>;  // rows of LDS and their swizzle
@@ -709,7 +717,7 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
   }
 }
 
-// The shares of a query row joined: weights 2^(m - max m).  A wavefront per row: its lanes hold one share's maximum and sums
+// The shares of a query row joined: weights 2^(m - max m).  92160 rows of 7 shares: 35 us, HBM.  A wavefront per row: its lanes hold one share's maximum and sums
 // each (nsplit <= 64), then 64 / (d / 4) shares' outputs at a time, four channels per lane; the order of the sums is fixed.
 template <typename T>
 __global__ __launch_bounds__(256) void cache4_join_kernel(CacheAttnArgs a, int rows) {
@@ -775,7 +783,8 @@ struct CacheWeightArgs {
 // taken again, against the rows' maxima and sums of the whole call: keys come from memory a second time, where keeping
 // the scores would write and read 8 bytes of every row.
 //   S[row, key] = Q K^T         row operand: rows, column operand: keys
-// Up to 16 NT rows, kept as operands with their statistics; a wavefront walks every fourth step of 32 keys of its workgroup's share.
+// Up to 16 NT rows, kept as operands with their statistics; a wavefront walks every fourth step of 32 keys of its workgroup's share.  32 rows, 57600
+// slots and fewer of 8 heads of 128, two batch entries: 61 MB in 22 us.
 template <typename T, int G, int NT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? (NT == 1 ? 4 : 3) : 2) void cache4_weight_few_kernel(CacheWeightArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
@@ -872,6 +881,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (NT == 1 ? 4 : 3) : 2) void c
 // workgroup's four share in LDS (direct global->LDS loads, one tile ahead), with their statistics.  A lane holds one key of every 32, so that a
 // sum over the rows is one register.  Bound by the vector ALUs: an fma, an exponential and an fma for every score, beside 2 G
 // matrix instructions of 32 clocks for 16 of a lane's.  A row's address and statistics are found by steps from tile to tile, without a division.
+// 1024 rows over 26624 slots of 10 heads of 64, two batch entries: 118 us (every key's sum in registers of its own: 134; with divisions: 155).
 template <typename T, int G>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && G <= 2 ? 3 : 2) void cache4_weight_many_kernel(CacheWeightArgs a) {
   using Geo = SparseGeo<T, 2 * G, 4>;

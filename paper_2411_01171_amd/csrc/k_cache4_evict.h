@@ -166,7 +166,7 @@ __device__ __forceinline__ EvictSearch evict_begin(const EvictArgs& a) {
 }
 
 // Lists of up to 1024 PER slots, one workgroup each; the weights stay in registers.  A chain of latencies, that of fetching the code among
-// them: the digits are a loop, and short lists have a form of their own.
+// them: the digits are a loop, and short lists have a form of their own (4096 slots 7 us; with digits unrolled and 16 weights of a thread 12).
 template <int PER>
 __global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a) {
   __shared__ EvictShared sh;
@@ -269,7 +269,8 @@ __global__ __launch_bounds__(kEvictThreads) void cache4_search_kernel(EvictArgs 
 
 constexpr int kMoveThreads = 256;
 
-// The slots of a chunk that stay: listed in LDS in their order, then moved, 16 bytes of codes to a thread.
+// The slots of a chunk that stay: listed in LDS in their order, then moved, 16 bytes of codes to a thread.  Bound by HBM: a quarter of 115200 slots and fewer
+// of 32 heads of 128 in 78 us, 233 MB read (rows of 64 bytes in lines of 128) and 134 written, 4.7 TB/s.
 template <int G>
 __global__ __launch_bounds__(kMoveThreads) void cache4_move_kernel(EvictArgs a) {
   constexpr int WAVES = kMoveThreads / kWave, PER = kEvictChunk / kMoveThreads, S = cache4_scale_bytes(G);

@@ -151,10 +151,13 @@ struct CachePlan {
   size_t bytes() const { return part_bytes + stat_bytes + row_bytes + 256; }
 };
 
-// Into how many shares the keys of a tile are dealt out.  Few rows: as many workgroups as the chip holds at once, 256 keys at least to
-// each (a third more than that: one token of 32 heads against 115200 slots 110 us, and 99 now).  Many: the busiest CU's number of workgroups bounds the time (360 tiles on 256 CUs: 2 of 1.4, and 1.5 of 1.4 in two shares), and
-// the shares cost their way through memory; one workgroup alone on a CU takes three quarters of the time that two take.  A workgroup's
-// 64 keys of a row and channel take 0.073 ns at the rate of a whole chip's.
+// Into how many shares the keys of a tile are dealt out.
+// Few rows: as many workgroups as the chip holds at once (`held` per CU), 256 keys at least to each; a third more than that took 110 us for one
+// token of 32 heads against 115200 slots, and takes 99 so.
+// Many: the busiest CU's number of workgroups bounds the time, and the shares cost their way through memory.  360 tiles on 256 CUs leave the
+// busiest with 2 where the mean is 1.4 (9216 tokens of 5 heads over 64512 slots, two batch entries: 2214 us); in seven shares it has 10 of
+// 9.8 (1639).  A workgroup alone on a CU is taken for three quarters of the time that two take, and 64 keys of a row and channel for
+// 0.073 ns, the rate of a whole chip's.
 static int64_t shares_of_tiles(int64_t tiles, int tile_rows, int held, int64_t capacity, int64_t rows, int64_t d) {
   if (tiles == 0) return 1;
   const int64_t most = std::min<int64_t>(64, std::max<int64_t>(1, capacity / 256));
