@@ -354,6 +354,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
       // ---- O^T += V^T P^T: slots e < 4 of group g are keys 4 g + e, the others 16 + 4 g + e - 4
 #pragma unroll
       for (int i = 0; i < 2 * G; ++i) {
+        if (i == 2 * G - 1 && a.d <= 16 * i) break;  // no channels of the head
         const int row = 4 * g + r / 4, piece = 2 * i + (r % 4) / 2;
         const uint2 x = lds_read_tr(vals + row * ROW + (piece ^ swizzle(row)) * 16 + (r % 2) * 8);
         const uint2 y = lds_read_tr(vals + (16 + row) * ROW + (piece ^ swizzle(16 + row)) * 16 + (r % 2) * 8);
