@@ -22,7 +22,7 @@ struct EvictArgs {
   unsigned work;     // lists * chunks
   int2* counts;      // [lists][chunks]: slots that stay without question, slots that equal the threshold
   uint2* least;      // [lists]: the threshold, and how many of those that equal it stay
-  unsigned parts;    // workgroups of a list of more than 16384 slots
+  unsigned parts;    // workgroups of a list of more than 32768 slots
   int64_t part_slots;
   int* hist[2];      // [lists][parts][2048], of one step and the next
   struct EvictSearch* search;  // [2][lists]
@@ -36,8 +36,9 @@ __device__ __forceinline__ unsigned weight_key(float x) {
 }
 
 constexpr int kEvictThreads = 1024;
-constexpr int kEvictPer = 16;                                // weights of a thread at a time, at most
-constexpr int kEvictPart = kEvictThreads * kEvictPer;         // longer lists are searched by several workgroups
+constexpr int kEvictPer = 16, kEvictPerMost = 32;            // weights of a thread at a time; of the lists with a workgroup each at most
+constexpr int kEvictPart = kEvictThreads * kEvictPer;
+constexpr int kEvictWhole = kEvictThreads * kEvictPerMost;   // longer lists are searched by several workgroups
 constexpr unsigned kEvictParts = 16;                         // so many at most
 constexpr int kEvictChunk = kEvictThreads;                   // slots that are counted together; the second kernel's piece
 constexpr int kEvictBins = 2048;                             // digits of 11, 11 and 10 bits
@@ -57,7 +58,7 @@ struct EvictSearch {
 struct EvictShared {
   int hist[kEvictBins];
   int wave_total[kEvictThreads / kWave];
-  int count[kEvictPer][2];
+  int count[kEvictPerMost][2];
   EvictSearch found;
 };
 
@@ -91,11 +92,11 @@ __device__ __forceinline__ EvictSearch evict_digit(EvictShared& sh, EvictSearch 
   return sh.found;
 }
 
-// A batch of up to 16384 slots, base + 1024 j + t: which of them there are and which weights count, from its first slot on.
+// A batch of up to 32768 slots, base + 1024 j + t: which of them there are and which weights count, from its first slot on.
 struct EvictBatch {
   int there, lo, hi;
   __device__ __forceinline__ EvictBatch(const EvictArgs& a, int n, int64_t base, int64_t end) {
-    auto from_base = [&](int64_t i) { return (int)min(max(i - base, (int64_t)0), (int64_t)kEvictPart); };
+    auto from_base = [&](int64_t i) { return (int)min(max(i - base, (int64_t)0), (int64_t)kEvictWhole); };
     there = from_base(end);
     lo = min(from_base(a.first), there);
     hi = max(lo, min(from_base((int64_t)n - a.last), there));
@@ -167,6 +168,8 @@ __device__ __forceinline__ EvictSearch evict_begin(const EvictArgs& a) {
 
 // Lists of up to 1024 PER slots, one workgroup each; the weights stay in registers.  A chain of latencies, that of fetching the code among
 // them: the digits are a loop, and short lists have a form of their own (4096 slots 7 us; with digits unrolled and 16 weights of a thread 12).
+// With 32 weights of a thread 24000 and 32768 slots of 8 lists take 28 and 32 us with their move, in two pieces 36 and 37, with 64 of a
+// thread 38 and 43; 60000 slots take 57 with 64, and 38 in pieces.
 template <int PER>
 __global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a) {
   __shared__ EvictShared sh;

@@ -264,7 +264,7 @@ static si_status plan_evict(const si_cache4* c, int64_t keep, EvictPlan* p) {
   p->least_bytes = align_up((size_t)p->lists * sizeof(uint2), 256);
   // Lists that do not fit a workgroup's registers are cut into up to 16 parts, as long as there are few lists: every part adds up all parts' counts.
   const int64_t batches = (c->capacity + kEvictPart - 1) / kEvictPart;
-  p->parts = c->capacity <= kEvictPart ? 0 : std::min<int64_t>(std::min<int64_t>(kEvictParts, batches), std::max<int64_t>(1, 1024 / p->lists));
+  p->parts = c->capacity <= kEvictWhole ? 0 : std::min<int64_t>(std::min<int64_t>(kEvictParts, batches), std::max<int64_t>(1, 1024 / p->lists));
   p->part_slots = p->parts ? (batches + p->parts - 1) / p->parts * kEvictPart : 0;
   p->search_bytes = p->parts ? align_up((size_t)p->lists * 2 * sizeof(EvictSearch), 256) : 0;
   p->hist_bytes = (size_t)(p->lists * p->parts) * kEvictBins * sizeof(int);
@@ -407,7 +407,8 @@ si_status si_cache4_evict(const si_cache4* cache, const int32_t* k_len, const fl
   if (p.parts == 0) {
     const unsigned grid = (unsigned)std::min<int64_t>(p.lists, si::kGridMost);
     if (cache->capacity <= 4 * si::kEvictThreads) si::cache4_pick_kernel<4><<<grid, si::kEvictThreads, 0, st>>>(a);
-    else si::cache4_pick_kernel<si::kEvictPer><<<grid, si::kEvictThreads, 0, st>>>(a);
+    else if (cache->capacity <= si::kEvictPart) si::cache4_pick_kernel<si::kEvictPer><<<grid, si::kEvictThreads, 0, st>>>(a);
+    else si::cache4_pick_kernel<si::kEvictPerMost><<<grid, si::kEvictThreads, 0, st>>>(a);
   } else {
     const unsigned grid = (unsigned)std::min<int64_t>(p.lists * p.parts, si::kGridMost);
     si::cache4_search_kernel<0><<<grid, si::kEvictThreads, 0, st>>>(a);

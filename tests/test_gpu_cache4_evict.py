@@ -59,7 +59,7 @@ def test_head_widths(d):
     _check(2, 3, 200, d, 70, first=2, last=9)
 
 
-@pytest.mark.parametrize("cap", [1, 2, 63, 64, 65, 1000, 1023, 1024, 1025, 2048, 4097, 16384, 16385, 33000, 70001])
+@pytest.mark.parametrize("cap", [1, 2, 63, 64, 65, 1000, 1023, 1024, 1025, 2048, 4097, 16384, 16385, 32768, 32769, 33000, 70001])
 @pytest.mark.parametrize("share", [0.0, 0.3, 0.99, 1.0, 1.5])
 def test_lengths(cap, share):
     _check(1, 2, cap, 32, max(1, int(cap * share)), seed=cap)
