@@ -451,11 +451,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
 // Power bounds it: with wavefronts of 32 rows at twice the number (four per SIMD), with keys read a piece ahead, without the
 // scheduling barriers it takes 1575 to 1650, with products and exponentials of neighbouring pieces interleaved instruction by
 // instruction 1960.  Heads of 96 and 128: 850 and 800 to 860 TFLOP/s.
-template <int G, int CT, bool W>
-__global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_many_kernel(CacheAttnArgs a) {
+template <typename T, int G, int CT, bool W>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && G == 1 && CT == 1 ? 3 : 2) void cache4_attn_many_kernel(CacheAttnArgs a) {
   using Geo = SparseGeo<bf16, 2 * G, 4>;  // rows of LDS and their swizzle
   constexpr int ROW = Geo::ROW, HALF = 64 * ROW, KS = 2 * G, SB = cache4_scale_bytes(G);
-  constexpr int UT = CT == 1 && G < 4 ? 2 : 1;  // 32-key tiles that are in work together, as far as registers go
+  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
+  constexpr int UT = CT == 1 && G < (TERMS > 1 ? 2 : 4) ? 2 : 1;  // 32-key tiles that are in work together, as far as registers go
   __shared__ __align__(1024) u32x4_t ring[4 * HALF / 16];
   __shared__ int bad_key[4];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)(&ring[0]);
@@ -482,17 +483,18 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
     const int64_t last = min(min((int64_t)t.run * a.run_len + min((rho0 + 128 * CT - 1) / a.group, a.run_len - 1), (int64_t)t.q_len - 1), (int64_t)a.Nq - 1);
     const int all = t.seen(a, first), any = t.seen(a, (int)last);
     int token[CT], sub[CT], seen[CT];
-    u32x4_t q[CT][KS];
+    u32x4_t q[CT][KS][TERMS];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       token[c] = t.token(a, rho0 + (wave * CT + c) * 32 + r, sub[c]);
       seen[c] = token[c] < 0 ? any : t.seen(a, token[c]);
-      const bf16* row = static_cast<const bf16*>(a.q) + t.b * a.qb + (int64_t)max(token[c], 0) * a.qn + (int64_t)(t.hk * a.group + (token[c] < 0 ? 0 : sub[c])) * a.qh;
+      const T* row = static_cast<const T*>(a.q) + t.b * a.qb + (int64_t)max(token[c], 0) * a.qn + (int64_t)(t.hk * a.group + (token[c] < 0 ? 0 : sub[c])) * a.qh;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const int ch = 16 * s + 8 * g;
-        q[c][s] = u32x4_t{0, 0, 0, 0};
-        if (ch < a.d && token[c] >= 0) q[c][s] = *reinterpret_cast<const u32x4_t*>(row + ch);
+#pragma unroll
+        for (int x = 0; x < TERMS; ++x) q[c][s][x] = u32x4_t{0, 0, 0, 0};
+        if (ch < a.d && token[c] >= 0) query_parts<T, TERMS>(row + ch, q[c][s]);
       }
     }
     const int64_t head = ((int64_t)t.b * a.c.heads + t.hk) * a.c.cap;
@@ -590,12 +592,16 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[c][u][e] = 0.f;
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < KS; ++s) {
+          if (TERMS > 1 && s == KS - 1 && a.d <= 16 * s) break;  // no channels of the head
 #pragma unroll
           for (int u = 0; u < UT; ++u)
 #pragma unroll
             for (int c = 0; c < CT; ++c)
-              sc[c][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s][u]), __builtin_bit_cast(bf16x8_t, q[c][s]), sc[c][u], 0, 0, 0);
+#pragma unroll
+              for (int x = TERMS - 1; x >= 0; --x)  // the smallest part first
+                sc[c][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[s][u]), __builtin_bit_cast(bf16x8_t, q[c][s][x]), sc[c][u], 0, 0, 0);
+        }
         const int key0 = (int)(st * 64) + part * 32 * UT;
         if (key0 + 32 * UT > all) {
 #pragma unroll
@@ -620,7 +626,7 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
         __builtin_amdgcn_sched_barrier(0);
 
         // ---- probabilities, as in the kernel above
-        u32x4_t pk[CT][2 * UT];
+        u32x4_t pk[CT][2 * UT][TERMS];
         float rs[CT], rw[CT];
         auto exponentiate = [&]() {
 #pragma unroll
@@ -631,9 +637,12 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
 #pragma unroll
               for (int e = 0; e < 16; e += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[c][u][e], a.scale_log2, -mref[c])), p1 = __builtin_amdgcn_exp2f(fmaf(sc[c][u][e + 1], a.scale_log2, -mref[c]));
-                const unsigned w = pack_bf16x2(p0, p1);
-                pk[c][2 * u + e / 8][e % 8 / 2] = w;
-                rs[c] = dot2_ones(w, rs[c]);
+                unsigned w[TERMS];
+                bf16_parts<TERMS>(p0, p1, w);
+#pragma unroll
+                for (int x = 0; x < TERMS; ++x) pk[c][2 * u + e / 8][x][e % 8 / 2] = w[x];
+                if constexpr (TERMS == 1) rs[c] = dot2_ones(w[0], rs[c]);
+                else rs[c] += p0 + p1;
                 if constexpr (W) rw[c] += p0 + p1;
               }
           }
@@ -676,7 +685,9 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
             const u32x4_t vf{vlo[k16][i].x, vlo[k16][i].y, vhi[k16][i].x, vhi[k16][i].y};
 #pragma unroll
             for (int c = 0; c < CT; ++c)
-              o[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[c][k16]), o[c][i], 0, 0, 0);
+#pragma unroll
+              for (int x = TERMS - 1; x >= 0; --x)
+                o[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pk[c][k16][x]), o[c][i], 0, 0, 0);
           }
       }
       slot ^= 2 * HALF;
@@ -685,12 +696,12 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       lsum[c] += __shfl_xor(lsum[c], 32, kWave);
-      if constexpr (W) lwt[c] += __shfl_xor(lwt[c], 32, kWave);
+      lwt[c] = W ? lwt[c] + __shfl_xor(lwt[c], 32, kWave) : lsum[c];
       if (token[c] < 0) continue;
       const int h = t.hk * a.group + sub[c];
       const int64_t row = ((int64_t)t.b * a.Nq + token[c]) * (a.c.heads * a.group) + h;
       const float inv = lsum[c] == 0.f ? 0.f : 1.f / lsum[c];  // a row without keys gives zero
-      bf16* dst = static_cast<bf16*>(a.o) + t.b * a.ob + (int64_t)token[c] * a.on + (int64_t)h * a.oh;
+      T* dst = static_cast<T*>(a.o) + t.b * a.ob + (int64_t)token[c] * a.on + (int64_t)h * a.oh;
 #pragma unroll
       for (int i = 0; i < G; ++i) {
         const bool bad = seen[c] > bad_key[i];
@@ -706,12 +717,13 @@ __global__ __launch_bounds__(256, G == 1 && CT == 1 ? 3 : 2) void cache4_attn_ma
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) y[j] = lsum[c] == 0.f ? 0.f : y[j] * inv;
-          *reinterpret_cast<uint2*>(dst + ch) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst + ch) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+          else *reinterpret_cast<f32x4_t*>(dst + ch) = y;
         }
       }
       if (g == 0) {
         if (a.nsplit > 1) a.part_stat[row * a.nsplit + t.part] = f32x4_t{mref[c], lsum[c], lwt[c], 0.f};
-        else if (W) a.row_stat[row] = row_stat(mref[c], lwt[c]);
+        else if (a.row_stat) a.row_stat[row] = row_stat(mref[c], lwt[c]);
       }
     }
     __syncthreads();  // bad_key and the ring are the next tile's

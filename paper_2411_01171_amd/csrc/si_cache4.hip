@@ -143,7 +143,7 @@ static si_status enqueue_copy(const si_heads* k, const si_heads* v, const si_cac
 // ----------------------------------------------------------------------------- attention
 
 struct CachePlan {
-  int group, tile_rows;  // query heads of a key head; rows of a tile: up to 32 by the few kernel, 128 and 256 by the other
+  int group, tile_rows;  // query heads of a key head; rows of a tile: up to 32 by the few kernel, 128 and 256 (bfloat16) by the other
   int64_t runs, run_len, tiles_per_run, work, rows, weight_chunks;
   int weight_rows;  // that the weights' kernel keeps, or 0: it keeps keys
   int nsplit;
@@ -157,8 +157,9 @@ struct CachePlan {
 // Many: the busiest CU's number of workgroups bounds the time, and the shares cost their way through memory.  360 tiles on 256 CUs leave the
 // busiest with 2 where the mean is 1.4 (9216 tokens of 5 heads over 64512 slots, two batch entries: 2214 us); in seven shares it has 10 of
 // 9.8 (1639).  A workgroup alone on a CU is taken for three quarters of the time that two take, and 64 keys of a row and channel for
-// 0.073 ns, the rate of a whole chip's.
-static int64_t shares_of_tiles(int64_t tiles, int tile_rows, int held, int64_t capacity, int64_t rows, int64_t d) {
+// cell_us: 0.073 ns, the rate of a whole chip's; float32's is 0.16, but its shares cost more at their beginnings, which 0.1 stands for (1500 tokens of 8 heads of
+// 64 over 14000 slots: 120 us, with 0.16 136).
+static int64_t shares_of_tiles(int64_t tiles, int tile_rows, int held, int64_t capacity, int64_t rows, int64_t d, double cell_us) {
   if (tiles == 0) return 1;
   const int64_t most = std::min<int64_t>(64, std::max<int64_t>(1, capacity / 256));
   if (tile_rows <= 32) return std::max<int64_t>(1, std::min<int64_t>(256 * held / tiles, most));
@@ -166,7 +167,7 @@ static int64_t shares_of_tiles(int64_t tiles, int tile_rows, int held, int64_t c
   double least = 0.0;
   for (int64_t n = 1; n <= most && n * tiles <= 4096; ++n) {
     const double on_cu = (double)((tiles * n + 255) / 256);
-    const double us = std::max(on_cu, 1.5) / (double)n * (double)((capacity + 63) / 64) * (double)(tile_rows * d) * 0.073e-3 +
+    const double us = std::max(on_cu, 1.5) / (double)n * (double)((capacity + 63) / 64) * (double)(tile_rows * d) * cell_us +
                       (n > 1 ? 5.0 + (double)(rows * n) * (double)(d + 4) * 8.0 / 4e6 : 0.0);
     if (n == 1 || us < least) { least = us; best = n; }
   }
@@ -182,8 +183,9 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   p->group = (int)(q->heads / c->heads);
   if ((double)p->group * (double)q->N >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;  // rows of a key head in 31 bits
   const int64_t rows_of_run = p->group * (run > 0 && run < q->N ? run : std::max<int64_t>(q->N, 1)), rows = p->group * std::max<int64_t>(q->N, 1);
-  const bool many = q->dtype == SI_BF16 && rows > 64;
-  p->tile_rows = !many ? (rows <= 16 ? 16 : 32) : cache_groups(c) <= 2 && rows > 128 ? 256 : 128;
+  // float32 heads of 64, 8 of them over 30000 slots: 65 rows 30 us in tiles of 32, 33 in one of 128; 97 rows 35 and 33; 128 39 and 37.
+  const bool many = rows > (q->dtype == SI_BF16 ? 64 : 96);
+  p->tile_rows = !many ? (rows <= 16 ? 16 : 32) : q->dtype == SI_BF16 && cache_groups(c) <= 2 && rows > 128 ? 256 : 128;
   // A tile ends with its run, so that its rows see the same keys; runs shorter than a tile share them.
   const bool own = run > 0 && run < q->N && rows_of_run >= p->tile_rows;
   p->run_len = own ? run : std::max<int64_t>(q->N, 1);
@@ -195,7 +197,7 @@ static si_status plan_cache_attn(const si_heads* q, const si_cache4* c, int64_t 
   // The shares, and with them the workspace, do not depend on the runs.
   const int64_t whole = q->N == 0 ? 0 : lists * ((rows + p->tile_rows - 1) / p->tile_rows);
   const int groups = cache_groups(c), held = p->tile_rows == 32 ? (groups == 1 ? 3 : 2) : q->dtype == SI_BF16 ? (groups <= 2 ? 4 : 3) : groups == 1 ? 4 : groups == 2 ? 3 : 2;
-  p->nsplit = (int)shares_of_tiles(whole, p->tile_rows, held, c->capacity, q->B * q->N * q->heads, q->dim_head);
+  p->nsplit = (int)shares_of_tiles(whole, p->tile_rows, held, c->capacity, q->B * q->N * q->heads, q->dim_head, q->dtype == SI_BF16 ? 0.073e-3 : 0.1e-3);
   if (tiles * p->nsplit >= 2147483648.0 - kGridMost) return SI_ERR_SHAPE;
   p->work = (int64_t)tiles * p->nsplit;
   p->rows = q->B * q->N * q->heads;
@@ -221,10 +223,11 @@ static si_status launch_cache_attn(const CacheAttnArgs& a, const CacheWeightArgs
     by_groups(c, [&](auto g) {
       if (p.tile_rows == 16) cache4_attn_few_kernel<T, g.value, 1><<<grid, 256, 0, st>>>(a);
       else if (p.tile_rows == 32) cache4_attn_few_kernel<T, g.value, 2><<<grid, 256, 0, st>>>(a);
-      else if constexpr (sizeof(T) == 2) {
+      else if constexpr (sizeof(T) == 4) cache4_attn_many_kernel<T, g.value, 1, false><<<grid, 256, 0, st>>>(a);
+      else {
         auto launch = [&](auto ct) {
-          if (w) cache4_attn_many_kernel<g.value, ct.value, true><<<grid, 256, 0, st>>>(a);
-          else cache4_attn_many_kernel<g.value, ct.value, false><<<grid, 256, 0, st>>>(a);
+          if (w) cache4_attn_many_kernel<T, g.value, ct.value, true><<<grid, 256, 0, st>>>(a);
+          else cache4_attn_many_kernel<T, g.value, ct.value, false><<<grid, 256, 0, st>>>(a);
         };
         if (p.tile_rows == 128) launch(std::integral_constant<int, 1>());
         else if constexpr (g.value <= 2) launch(std::integral_constant<int, 2>());
