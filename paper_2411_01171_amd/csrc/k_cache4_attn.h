@@ -166,8 +166,7 @@ __device__ __forceinline__ void note_nan(int* bad_key, int group, int key, u32x4
 // T: of queries and outputs.  G: groups of 32 channels of a head.  NT: columns of rows, 16 each.
 // One token of 32 heads against 115200 slots of 8 heads of 128, four batch entries: 502 MB in 93 us, 5.4 TB/s, bound by HBM (with
 // registers spilled to scratch, whose reloads wait for every load in flight, 197 us).  Eight such tokens, 32 rows, 57600 slots and fewer, two batch
-// entries: 116 MB in 36 us: a step's chain of latencies on two wavefronts per SIMD.  float32, 4050 rows of 8 heads of 80 over
-// 14175 slots: 415 us, 329 TFLOP/s of the operation's own, 990 with the three parts; the matrix cores 47 % busy, the vector ALUs 59 %.
+// entries: 116 MB in 36 us: a step's chain of latencies on two wavefronts per SIMD.
 template <typename T, int G, int NT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 2) void cache4_attn_few_kernel(CacheAttnArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
@@ -443,14 +442,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
   }
 }
 
-// Rows by the hundred: tiles of 128 CT rows, 32 CT to each of four wavefronts, that share stages of 64 keys.  A stage's codes are
+// Rows by the hundred: tiles of 128 CT rows (float32: CT = 1), 32 CT to each of four wavefronts, that share stages of 64 keys.  A stage's codes are
 // fetched into registers one stage ahead, a quarter of a key's and of a value's row to a thread, and become bf16 in LDS while
 // the stage before is multiplied.
-// W: the sums of the unrounded weights are wanted too.
+// W: the sums of the unrounded weights are wanted too; float32's are those.
 // 9216 tokens of 5 heads of 64 over 64512 slots, two batch entries: 1558 us, 977 TFLOP/s; matrix cores 40 % and vector ALUs 57 % of the cycles.
 // Power bounds it: with wavefronts of 32 rows at twice the number (four per SIMD), with keys read a piece ahead, without the
 // scheduling barriers it takes 1575 to 1650, with products and exponentials of neighbouring pieces interleaved instruction by
 // instruction 1960.  Heads of 96 and 128: 850 and 800 to 860 TFLOP/s.
+// float32, 4050 rows of 8 heads of 80 over 14175 slots: 348 us, 392 TFLOP/s of the operation's own, 1180 with the three parts; matrix cores
+// 58 %, vector ALUs 52 % (the kernel above, which converts codes anew for every 32 rows, 395, 45 % and 60 %).  Pieces of two tiles save nothing
+// with the registers of three parts (371 us).
 template <typename T, int G, int CT, bool W>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && G == 1 && CT == 1 ? 3 : 2) void cache4_attn_many_kernel(CacheAttnArgs a) {
   using Geo = SparseGeo<bf16, 2 * G, 4>;  // rows of LDS and their swizzle
