@@ -488,8 +488,11 @@ si_status si_cache4_load(const si_cache4* cache, const int32_t* first, const int
  * scale > 0.  q and out: one dtype.  The cache's values are taken exactly.  bf16:
  * probabilities are rounded to bf16 for the second product and for the sum that
  * divides it, everything else is float32 and so are the weights; float32: float32
- * throughout.  Finite scores times scale are at most 1e9 in magnitude.  The same
- * operands give the same bits.
+ * throughout.  Finite scores times scale are at most 1e9 in magnitude, and the values
+ * that are seen at most 2^88 (2^32 where scores times scale pass 1e8): a row is
+ * divided by its weights' sum at the end, and what it holds until then is up to 256
+ * (2^64) times the largest value per slot; it is no longer finite beyond float32's
+ * range.  The same operands give the same bits.
  * workspace: device, 256-byte aligned, contents ignored; calls that overlap in time
  * must not share one.  (q->heads / cache->heads) * N is below 2^31 - 2^20, and so are
  * the row tiles (of 16 rows and more) of all key heads (SI_ERR_SHAPE).

@@ -4,6 +4,8 @@
 // (tokens times the query heads that share it) are cut into tiles, a tile's keys into steps of 32 that are dealt out to the
 // wavefronts of a workgroup and, where there are few tiles, to several workgroups.  Every wavefront keeps the running maximum
 // and sum of a softmax and its own output; they are joined in a fixed order.
+// An output is divided by its sum at the end.  Until then it is a sum over up to 2^31 slots of weights up to kSparseTrigger = 2^8 (2^64 at scores of
+// 1e9, where the maximum's own rounding is that large), so values of up to 2^88 (2^32) stay finite.
 //   S^T[key, row] = K Q^T       row operand: keys, column operand: rows
 //   O^T[chan, row] += V^T P^T   column operand: the softmax result registers as they stand
 // Codes are read once, become bf16 (exactly) in registers, and go to the matrix cores: keys straight from where they were

@@ -1,4 +1,4 @@
-"""Long sums of the attention over the cache in 4 bits: the weights that tens of thousands of rows give to a slot."""
+"""Sums of the attention over the cache in 4 bits: the weights that tens of thousands of rows give to a slot, values at the end of their range."""
 import math
 
 import numpy as np
@@ -7,8 +7,9 @@ import torch
 
 import paper_2411_01171_amd as si
 from attn_helpers import host, strided
-from cache4_helpers import device_cache
+from cache4_helpers import device_cache, random_cache
 from gpu_helpers import guarded, guards_intact
+from test_gpu_cache4_attn import _check
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +56,18 @@ def test_weights_of_many_equal_rows(dtype, d, N, group, carried):
     err = np.abs(host(out)[0] - v)  # all rows the same, and right to bf16's two roundings (spread below 6) or float32's
     assert (host(out)[0] == host(out)[0, :1, :1]).all() and err.max() <= (2.0 ** -8 * 1.01 * 12 if dtype == "bf16" else 1e-5 * 6)
     assert math.isfinite(float(w.sum()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,cap", [(1, 200), (40, 200), (100, 2000), (300, 20000)])
+def test_values_of_the_largest_magnitude(dtype, N, cap):
+    """Values of 2^88 and scores that rise slowly, so that weights pass the reference maximum by up to its margin: outputs are no infinities."""
+    rng = np.random.default_rng(13)
+    B, Hk, d = 1, 2, 64
+    arrays = [a.copy() for a in random_cache(rng, B, Hk, cap, d)]
+    arrays[0][:] = 0
+    arrays[0][..., 0] = 4                                    # 2 in channel 0 ...
+    arrays[1][..., 0] = 124 + 4 * np.arange(cap) // cap      # ... times 2^-3 .. 2^0
+    arrays[2][:], arrays[3][:] = 0x66, 127 + 86              # 4 2^86
+    arrays[2][0, 1] = rng.choice(np.array([0x66, 0x6E, 0xE6, 0xEE], np.uint8), arrays[2][0, 1].shape)
+    _check(dtype, B, N, cap, Hk, Hk, d, arrays=arrays, q=np.ones((B, N, Hk, d), np.float32), scale=2.5)
