@@ -442,8 +442,9 @@ si_status si_attn_sparse_forward(const si_heads* q, const si_heads* k, const si_
  * Tokens are kept as they come (rotated before they are stored, where positions are
  * wanted): attention does not depend on the order of what a query sees.
  * At most (SI_ERR_SHAPE beyond): B 2^24, heads 65535, B * heads 2^28, capacity
- * 2^31 - 1 - 2^22, 2^40 tokens of all heads, workgroups of 16 tokens and more below
- * 2^32 - 2^20. */
+ * 2^31 - 1 - 2^22, 2^40 tokens of all heads; of all heads, the pieces of 256, 128, 84
+ * and 64 (G = 1 .. 4) tokens that are stored or read back, and those of 256 slots that
+ * are attended to, below 2^32 - 2^20. */
 typedef struct {
   void *k_codes, *k_scales, *v_codes, *v_scales; /* device */
   int64_t B, heads, capacity, dim_head;
@@ -478,10 +479,11 @@ si_status si_cache4_load(const si_cache4* cache, const int32_t* first, const int
  * run and what lies before: j < k_len[b] - q_len[b] + min((n / run + 1) * run, q_len[b]);
  * run == 1: nothing behind itself.  q_len, k_len: device int32 [B], NULL: N,
  * capacity; clamped to [0, N], [0, capacity].  What no query sees may hold anything.
- * A row that sees no key gives zeros and adds no weight; rows at and behind q_len
- * are left as they were.  A NaN among the keys that a row sees, or a score of
- * +infinity, makes the row NaN, and the weight of all that it sees; a NaN among the
- * values that it sees makes the 32 channels of that group NaN.
+ * A row that sees no key, or only scores of -infinity, gives zeros and adds no
+ * weight; rows at and behind q_len are left as they were.  A NaN among the keys that
+ * a row sees, or a score of +infinity, makes the row NaN, and the weight of all that
+ * it sees; a NaN among the values that it sees makes the 32 channels of that group
+ * NaN.
  * weight_out NULL: no weights.  weight_in NULL: zeros; it may be weight_out itself,
  * and otherwise lies apart.  Slots at and behind k_len are left as they were.
  * decay >= 0, read with weight_in.
@@ -513,8 +515,9 @@ si_status si_cache4_attn_forward(const si_heads* q, const si_cache4* cache, floa
  *   weight_out  [B][heads][out capacity]: the weights of what stayed
  *   kept        device int32 [B][heads][keep]: the slots that it had
  *   out_len     device int32 [B]: m
- * Of weight_out and kept, what lies behind m is left as it was.  keep >= 1, first and
- * last >= 0, first + last <= keep (SI_ERR_ARG).
+ * Of weight_out and kept, what lies behind m is left as it was.  keep >= 1, at most
+ * 2^31 - 1 - 2^22, B * heads * keep below 2^40 (SI_ERR_SHAPE); first and last >= 0,
+ * first + last <= keep (SI_ERR_ARG).
  * workspace: device, 256-byte aligned, contents ignored; calls that overlap in time
  * must not share one. */
 size_t si_cache4_evict_workspace_bytes(const si_cache4* cache, int64_t keep);
