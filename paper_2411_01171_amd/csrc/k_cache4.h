@@ -127,7 +127,7 @@ struct Cache4Place {
 
 // Four lanes share a group of 32 channels, and a thread takes eight channels of four tokens, whose loads are in flight together.  Workgroups go
 // through the heads of some tokens before the next tokens, so that rows of one projection are read to their end.  Bound by HBM:
-// 230400 tokens of 5 heads of 64, two batch entries, 172 us (756 MB, 4.4 TB/s); one token 3.5 us.
+// 230400 tokens of 5 heads of 64, two batch entries, 172 us (756 MB, 4.4 TB/s); one token 3.6 us.
 template <typename T, int G>
 __global__ __launch_bounds__(kCache4Threads) void cache4_store_kernel(Cache4CopyArgs a) {
   constexpr int S = cache4_scale_bytes(G);

@@ -166,9 +166,10 @@ __device__ __forceinline__ void note_nan(int* bad_key, int group, int key, u32x4
 
 // Rows of up to 32 of a tile: four wavefronts that each take every fourth step of 32 keys, on their own until the end.
 // T: of queries and outputs.  G: groups of 32 channels of a head.  NT: columns of rows, 16 each.
-// One token of 32 heads against 115200 slots of 8 heads of 128, four batch entries: 502 MB in 93 us, 5.4 TB/s, bound by HBM (with
+// One token of 32 heads against 115200 slots of 8 heads of 128, four batch entries: 502 MB in 92 us, 5.4 TB/s, bound by HBM (with
 // registers spilled to scratch, whose reloads wait for every load in flight, 197 us).  Eight such tokens, 32 rows, 57600 slots and fewer, two batch
-// entries: 116 MB in 36 us: a step's chain of latencies on two wavefronts per SIMD.
+// entries: 116 MB in 36 us: a step's chain of latencies on two wavefronts per SIMD.  float32 rows beyond 16 of heads of 104 to 128 do spill, 29
+// registers: eight such tokens over 60000 slots take 92 us.
 template <typename T, int G, int NT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 2) void cache4_attn_few_kernel(CacheAttnArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
@@ -448,13 +449,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && NT == 1 ? (G > 2 ? 3 : 4) : 
 // fetched into registers one stage ahead, a quarter of a key's and of a value's row to a thread, and become bf16 in LDS while
 // the stage before is multiplied.
 // W: the sums of the unrounded weights are wanted too; float32's are those.
-// 9216 tokens of 5 heads of 64 over 64512 slots, two batch entries: 1558 us, 977 TFLOP/s; matrix cores 40 % and vector ALUs 57 % of the cycles.
-// Power bounds it: with wavefronts of 32 rows at twice the number (four per SIMD), with keys read a piece ahead, without the
+// 9216 tokens of 5 heads of 64 over 64512 slots, two batch entries: 1559 us, 976 TFLOP/s; matrix cores 40 % and vector ALUs 57 % of the cycles,
+// at 2.33 of 2.4 GHz.  The two add up to nearly all of them, as matrix and vector time does on this chip: fewer vector instructions would
+// help, and other orders of them do not: with wavefronts of 32 rows at twice the number (four per SIMD), with keys read a piece ahead, without the
 // scheduling barriers it takes 1575 to 1650, with products and exponentials of neighbouring pieces interleaved instruction by
 // instruction 1960.  Heads of 96 and 128: 850 and 800 to 860 TFLOP/s.
-// float32, 4050 rows of 8 heads of 80 over 14175 slots: 348 us, 392 TFLOP/s of the operation's own, 1180 with the three parts; matrix cores
-// 58 %, vector ALUs 52 % (the kernel above, which converts codes anew for every 32 rows, 395, 45 % and 60 %).  Pieces of two tiles save nothing
-// with the registers of three parts (371 us).
+// float32, 4050 rows of 8 heads of 80 over 14175 slots: 363 us, 376 TFLOP/s of the operation's own, 1130 with the three parts; matrix cores
+// 58 %, vector ALUs 53 %, at 2.12 GHz (the kernel above, which converts codes anew for every 32 rows, 395, 45 % and 60 %).  Pieces of two tiles
+// save nothing with the registers of three parts (371 us).
 template <typename T, int G, int CT, bool W>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && G == 1 && CT == 1 ? 3 : 2) void cache4_attn_many_kernel(CacheAttnArgs a) {
   using Geo = SparseGeo<bf16, 2 * G, 4>;  // rows of LDS and their swizzle
@@ -597,7 +599,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && G == 1 && CT == 1 ? 3 : 2) v
             for (int e = 0; e < 16; ++e) sc[c][u][e] = 0.f;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          if (TERMS > 1 && s == KS - 1 && a.d <= 16 * s) break;  // no channels of the head
+          if (TERMS > 1 && s == KS - 1 && a.d <= 16 * s) break;  // no channels of the head: three products less (bf16 multiplies one with zeros)
 #pragma unroll
           for (int u = 0; u < UT; ++u)
 #pragma unroll
@@ -734,7 +736,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && G == 1 && CT == 1 ? 3 : 2) v
   }
 }
 
-// The shares of a query row joined: weights 2^(m - max m).  92160 rows of 7 shares: 35 us, HBM.  A wavefront per row: its lanes hold one share's maximum and sums
+// The shares of a query row joined: weights 2^(m - max m).  92160 rows of 7 shares: 36 us, HBM.  A wavefront per row: its lanes hold one share's maximum and sums
 // each (nsplit <= 64), then 64 / (d / 4) shares' outputs at a time, four channels per lane; the order of the sums is fixed.
 template <typename T>
 __global__ __launch_bounds__(256) void cache4_join_kernel(CacheAttnArgs a, int rows) {
@@ -897,8 +899,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? (NT == 1 ? 4 : 3) : 2) void c
 // The same for more rows.  A wavefront keeps 32 KT keys as bf16 column operands and walks the rows in tiles of 32 that the
 // workgroup's four share in LDS (direct global->LDS loads, one tile ahead), with their statistics.  A lane holds one key of every 32, so that a
 // sum over the rows is one register.  Bound by the vector ALUs: an fma, an exponential and an fma for every score, beside 2 G
-// matrix instructions of 32 clocks for 16 of a lane's.  A row's address and statistics are found by steps from tile to tile, without a division.
-// 1024 rows over 26624 slots of 10 heads of 64, two batch entries: 118 us (every key's sum in registers of its own: 134; with divisions: 155).
+// matrix instructions of 32 clocks for 16 of a lane's.  A row's statistics, and the address of a wavefront's first load of a tile, are found by
+// steps from tile to tile, without a division; bfloat16 heads of up to 64 channels and float32 ones of up to 32 have that load only, others
+// divide for the second to fourth.
+// 1024 rows over 26624 slots of 10 heads of 64, two batch entries: 122 us (every key's sum in registers of its own: 134; with divisions: 155).
+// Rows are not dealt out to workgroups: short caches leave most of the chip idle (747 tokens of 16 heads over 747 slots of 2, two batch
+// entries: 149 us in 12 workgroups).
 // Equal rows give a key the same number again and again, and a running sum then rounds the same way every time: 73728 of them were 5e-4 of the
 // weight off.  A lane's 16 terms of a tile are added up first, and collected with what every rounding added (Kahan's compensated summation):
 // 4 additions for 48 instructions, below what the time can tell.

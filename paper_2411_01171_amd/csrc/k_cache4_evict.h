@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kEvictThreads) void cache4_pick_kernel(EvictArgs a)
 }
 
 // Longer lists, a workgroup for each of a.parts pieces of one.  STEP 0, 1, 2: the counts of that digit of a piece's weights; 1, 2, 3: before
-// that, the digit before it from all pieces' counts; 3: the counts of every 1024 slots.  A launch per step, 9 to 12 us each for 32 lists
+// that, the digit before it from all pieces' counts; 3: the counts of every 1024 slots.  A launch per step, 9 to 11 us each for 32 lists
 // of 115200 slots: latencies of memory, and of fetching the code (pieces of 4096 and 8192 slots are slower; a workgroup per list took 98 us).
 template <int STEP>
 __global__ __launch_bounds__(kEvictThreads) void cache4_search_kernel(EvictArgs a) {
